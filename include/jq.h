@@ -19,6 +19,8 @@
  *   jq_score_lse, jq_evict_lse    the same with caller-supplied softmax normalisers
  *   jq_score_tail, jq_evict_tail  the same with the soft tokens' own keys in the softmax
  *   jq_score_paged, jq_evict_paged  the same on a paged cache (pools + block table)
+ *   jq_attend, jq_attend_tree     attention of the newest tokens, or of a tree of drafted ones, over a pruned cache
+ *   jq_evict_weight, jq_replace_lightest   eviction by accumulated attention weight: of many rows, or of one for a new token's
  *   jq_hit_rate     critical-KV hit rate between two kept sets (Eq. 6)
  *   jq_map_mse      forward value of the training objective (Eq. 5) from two score maps
  *   jq_map_mse_fused  the same from the two query sets, neither map ever stored
@@ -364,6 +366,82 @@ int jq_evict_paged_inplace(const jq_shape* shape, const jq_pages* pages, const j
 int jq_evict_traced(const jq_shape* shape, const void* Q, const void* K, const void* V,
                     void* K_out, void* V_out, int32_t* idx_out, float* scores_out,
                     void* ws, size_t ws_bytes, void* stream, void* const* marks, int n_marks);
+
+/* ---- Decoding on a pruned cache (Section 4.3: decoding continues on the pruned cache) ------------------------
+ * The calls below work on a cache with room for more rows than it holds: sequence s has room for
+ * L_s = cu_seqlens[s+1] - cu_seqlens[s] rows, of which
+ *   lens[l, s]   (DEVICE int32 [n_layers, n_seq]; NULL: all of them)
+ * are live in layer l: the first that many of the sequence's rows.  Values outside 0..L_s are clamped into that
+ * range.  Being read on the device only, lens may grow from replay to replay of a captured call.  Per row and KV
+ * head a caller may keep
+ *   weights[l, g, cu_seqlens[s] + b]   DEVICE fp32  [n_layers, h_kv, T]  the attention that the row has received
+ *   pos    [l, g, cu_seqlens[s] + b]   DEVICE int32 [n_layers, h_kv, T]  the token that it came from
+ * in logical row order, on a paged cache too. */
+
+/* Attention of every sequence's newest n_q tokens over its live rows:
+ *   out[l,s,i,h,:] = sum_j p_j V[l,j,g,:],  p_j = exp(scale * Q[l,s,i,h,:].K[l,j,g,:] - lse[l,s,i,h]),  g = h / (h_q / h_kv)
+ *   lse[l,s,i,h]   = log sum_j exp(scale * Q[l,s,i,h,:].K[l,j,g,:])
+ * (out: DEVICE bf16, shaped like Q; lse: DEVICE fp32 [n_layers, n_seq, n_q, h_q], natural log, may be NULL).  j runs
+ * over all live rows, or, with shape->window = 1, over those that a causal mask leaves when the queries are the last
+ * n_q live rows' own tokens: query i sees the first lens - n_q + i + 1 rows.  A query that sees nothing (an empty
+ * sequence, a negative limit) gets zeros and -infinity.  With `weights` (may be NULL; at most 128 query rows n_q * h_q / h_kv
+ * per KV head, otherwise JQ_ERR_UNSUPPORTED) every live row's weight grows by the attention it receives, summed over
+ * the n_q tokens and the heads of the group: the statistic that jq_evict_weight and jq_replace_lightest evict by.
+ * With the soft tokens' own rows appended (window = 1) lse is what jq_score_lse and jq_evict_lse take: the prompt is
+ * then evicted in one pass over K.  Sums and softmax are held in fp32.  `ws` (DEVICE, 16-byte aligned) must hold
+ * jq_attend_workspace_bytes (`with_weights`: 0, or 1 for calls that pass weights).  shape->budgets is not used. */
+int jq_attend_workspace_bytes(const jq_shape* shape, int32_t with_weights, size_t* bytes);
+int jq_attend(const jq_shape* shape, const int32_t* lens, const void* Q, const void* K, const void* V, void* out,
+              float* lse, float* weights, void* ws, size_t ws_bytes, void* stream);
+int jq_attend_paged(const jq_shape* shape, const jq_pages* pages, const int32_t* lens, const void* Q, const void* K_pool,
+                    const void* V_pool, void* out, float* lse, float* weights, void* ws, size_t ws_bytes, void* stream);
+
+/* The same for a tree of drafted tokens: n_q (<= JQ_MAX_DRAFT, <= L_s) tokens whose own rows are the last n_q live ones,
+ * drafted token j in row lens - n_q + j.  Every token sees all rows before those, and drafted token i sees drafted token j
+ * where bit j % 32 of seen[s, i, j / 32] is set (DEVICE uint32 [n_seq, n_q, ceil(n_q / 32)]; its own bit too if it is to
+ * see itself; bits from n_q on are ignored).  A sequence that drafted fewer tokens leaves the others' bits clear: rows
+ * that a token does not see do not reach its output, whatever they hold.  shape->window must be 0.  Workspace:
+ * jq_attend_workspace_bytes with 0. */
+#define JQ_MAX_DRAFT 1024
+int jq_attend_tree(const jq_shape* shape, const int32_t* lens, const uint32_t* seen, const void* Q, const void* K,
+                   const void* V, void* out, float* lse, void* ws, size_t ws_bytes, void* stream);
+int jq_attend_tree_paged(const jq_shape* shape, const jq_pages* pages, const int32_t* lens, const uint32_t* seen,
+                         const void* Q, const void* K_pool, const void* V_pool, void* out, float* lse, void* ws,
+                         size_t ws_bytes, void* stream);
+
+/* Eviction by accumulated attention weight (the accumulated-attention baseline of Section 5.1).  Of the live rows of
+ * every (layer, sequence, KV head) the budgets[s] (layer_budgets[l, s]) heaviest stay, ties towards the lower row, in
+ * order; among them always those of positions below keep_first and above newest - keep_last, where newest is the
+ * largest position among the live rows.  `pos` NULL: a row's number is its position.  Kept row b goes to row b of the
+ * sequence's own segment:
+ *   K_out[l, cu_seqlens[s] + b, g, :] = K[l, cu_seqlens[s] + idx_out[l, g, cu_budgets[s] + b], g, :]
+ * likewise V_out, weights_out and pos_out (shaped like K, V, weights and pos; pos_out may be NULL if pos is).  All of
+ * them may be the inputs themselves -- the eviction then needs no second cache -- or none may overlap any input.
+ * A sequence of no more live rows than its budget keeps them all.  Rows and slots behind the kept ones are left as
+ * they were; the caller sets lens to min(lens, budget).  idx_out may be NULL.  Paged: the outputs are pools of the
+ * inputs' shape behind the same block table.  shape->window must be 0; pool_k, n_q, h_q and scale (beyond their checks) do not matter.
+ * `ws` must hold jq_evict_weight_workspace_bytes. */
+int jq_evict_weight_workspace_bytes(const jq_shape* shape, size_t* bytes);
+int jq_evict_weight(const jq_shape* shape, const int32_t* lens, const void* K, const void* V, const float* weights,
+                    const int32_t* pos, void* K_out, void* V_out, float* weights_out, int32_t* pos_out,
+                    int32_t* idx_out, void* ws, size_t ws_bytes, void* stream);
+int jq_evict_weight_paged(const jq_shape* shape, const jq_pages* pages, const int32_t* lens, const void* K_pool,
+                          const void* V_pool, const float* weights, const int32_t* pos, void* K_out, void* V_out,
+                          float* weights_out, int32_t* pos_out, int32_t* idx_out, void* ws, size_t ws_bytes, void* stream);
+
+/* The same for a single token: k_new, v_new (DEVICE bf16 [n_layers, n_seq, h_kv, d]) of the tokens at positions
+ * token[s] (DEVICE int32 [n_seq]) become rows of the cache.  While a sequence has room (lens[l, s] < L_s) the row is
+ * appended; then it takes the place of the head's lightest row (ties: the lowest), never one of a position below
+ * keep_first or above token[s] - keep_last: keep_first + max(keep_last, 1) <= L_s, otherwise JQ_ERR_BUDGET.  The row's
+ * weight starts at 0 and its position is token[s].  slot_out (DEVICE int32 [n_layers, n_seq, h_kv], may be NULL) takes
+ * the row's number.  shape->window must be 0.  The caller sets lens to min(lens + 1, L_s) before the next call.  Rows are no longer in the order of
+ * their positions then: pos says which they are, to jq_evict_weight too. */
+int jq_replace_lightest(const jq_shape* shape, const int32_t* lens, const void* k_new, const void* v_new,
+                        const int32_t* token, void* K, void* V, float* weights, int32_t* pos, int32_t* slot_out,
+                        void* stream);
+int jq_replace_lightest_paged(const jq_shape* shape, const jq_pages* pages, const int32_t* lens, const void* k_new,
+                              const void* v_new, const int32_t* token, void* K_pool, void* V_pool, float* weights,
+                              int32_t* pos, int32_t* slot_out, void* stream);
 
 /* Measurement aid, not part of the method: a plain device-to-device copy kernel of
  * `bytes` bytes (a multiple of 16; 16-byte aligned, non-overlapping DEVICE buffers).

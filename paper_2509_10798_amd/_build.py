@@ -10,8 +10,9 @@ ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libjq.so")
 OBJ = os.path.join(PKG, "_build")
-# one translation unit (csrc/jq_lib.hip says why); the other .hip files are its parts
-SOURCES = ["jq_lib.hip"]
+# the eviction path is one translation unit (csrc/jq_lib.hip says why), the kernels of decoding on a pruned cache another; the
+# other .hip files are their parts
+SOURCES = ["jq_lib.hip", "jq_decode.hip"]
 FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall",
     "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",

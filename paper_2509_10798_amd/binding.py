@@ -22,6 +22,8 @@ JQ_MAX_SEQ = 128
 STATUS = {0: "JQ_OK", -1: "JQ_ERR_NULL", -2: "JQ_ERR_SHAPE", -3: "JQ_ERR_BUDGET", -4: "JQ_ERR_UNSUPPORTED",
           -5: "JQ_ERR_WORKSPACE", -6: "JQ_ERR_ALIAS", -7: "JQ_ERR_LAUNCH"}
 EXPORTS = ("jq_workspace_bytes", "jq_score", "jq_score_lse", "jq_evict_lse", "jq_score_tail", "jq_evict_tail", "jq_pool", "jq_select_topk", "jq_compact", "jq_compact_inplace_workspace_bytes", "jq_compact_inplace", "jq_evict", "jq_evict_inplace_workspace_bytes", "jq_evict_inplace", "jq_evict_stream", "jq_evict_static", "jq_score_paged", "jq_evict_paged", "jq_evict_paged_inplace_workspace_bytes", "jq_evict_paged_inplace", "jq_evict_traced", "jq_hit_rate", "jq_map_mse", "jq_map_mse_fused_workspace_bytes", "jq_map_mse_fused",
+           "jq_attend_workspace_bytes", "jq_attend", "jq_attend_paged", "jq_attend_tree", "jq_attend_tree_paged",
+           "jq_evict_weight_workspace_bytes", "jq_evict_weight", "jq_evict_weight_paged", "jq_replace_lightest", "jq_replace_lightest_paged",
            "jq_copy_probe", "jq_reload_knobs", "jq_status_string")
 TRACE_KERNELS = ("jq_stats_kernel", "jq_score_kernel", "jq_pool_kernel", "jq_select_finalize_kernel")
 TRACE_MARKS = 2 * len(TRACE_KERNELS)
@@ -86,6 +88,16 @@ def lib() -> ctypes.CDLL:
         L.jq_evict_paged_inplace_workspace_bytes.argtypes = [shp, pgp, ctypes.POINTER(sz)]
         L.jq_evict_paged_inplace.argtypes = [shp, pgp, pgp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
         L.jq_evict_traced.argtypes = [shp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp, ctypes.POINTER(vp), ctypes.c_int]
+        L.jq_attend_workspace_bytes.argtypes = [shp, ctypes.c_int32, ctypes.POINTER(sz)]
+        L.jq_attend.argtypes = [shp] + [vp] * 8 + [sz, vp]
+        L.jq_attend_paged.argtypes = [shp, pgp] + [vp] * 8 + [sz, vp]
+        L.jq_attend_tree.argtypes = [shp] + [vp] * 8 + [sz, vp]
+        L.jq_attend_tree_paged.argtypes = [shp, pgp] + [vp] * 8 + [sz, vp]
+        L.jq_evict_weight_workspace_bytes.argtypes = [shp, ctypes.POINTER(sz)]
+        L.jq_evict_weight.argtypes = [shp] + [vp] * 11 + [sz, vp]
+        L.jq_evict_weight_paged.argtypes = [shp, pgp] + [vp] * 11 + [sz, vp]
+        L.jq_replace_lightest.argtypes = [shp] + [vp] * 10
+        L.jq_replace_lightest_paged.argtypes = [shp, pgp] + [vp] * 10
         L.jq_copy_probe.argtypes = [vp, vp, sz, vp]
         L.jq_reload_knobs.argtypes = []
         L.jq_status_string.argtypes = [ctypes.c_int]
@@ -456,6 +468,193 @@ def map_mse_fused(shape: Shape, Q_a, Q_b, K, mse=None, ws=None, stream=None):
     _check(lib().jq_map_mse_fused(ctypes.byref(cs), _ptr(Q_a), _ptr(Q_b), n_q_b, _ptr(K), _ptr(mse), _ptr(ws), ws.numel(),
                                   _stream(stream)), "jq_map_mse_fused")
     return mse
+
+
+# ---- decoding on a pruned cache ---------------------------------------------------------------------------------
+
+def _tensor(name, t, dtype, size, device=None):
+    """Checks one argument of the calls below, which read and write raw memory: its type, its size, that it is dense and where it
+    lies.  Returns its address (None for None)."""
+    if t is None:
+        return None
+    if t.dtype != dtype or tuple(t.shape) != tuple(size):
+        raise ValueError("%s: %s of %s is wanted, got %s of %s" % (name, dtype, tuple(size), t.dtype, tuple(t.shape)))
+    if not t.is_contiguous():
+        raise ValueError("%s is not contiguous" % name)
+    if not t.is_cuda or (device is not None and t.device != device):
+        raise ValueError("%s lies on %s%s" % (name, t.device, "" if device is None else ", the cache on %s" % device))
+    return int(t.data_ptr())
+
+
+def _cache_size(shape: Shape, pages):
+    if pages is None:
+        return (shape.n_layers, shape.T, shape.h_kv, shape.d)
+    return (shape.n_layers, pages.n_pages, pages.page_size, shape.h_kv, shape.d)
+
+
+def _pages_arg(shape: Shape, pages, device):
+    """The argument in front of lens: nothing for a dense cache."""
+    if pages is None:
+        return ()
+    import torch
+    bt = pages.block_table
+    if bt is not None:
+        _tensor("block_table", bt, torch.int32, (shape.n_seq, int(bt.shape[-1])), device)
+    return (ctypes.byref(pages.c_struct()),)
+
+
+def _workspace(ws, need, device):
+    import torch
+    if ws is None:
+        ws = torch.empty(need(), dtype=torch.uint8, device=device)
+    return _tensor("ws", ws, torch.uint8, (ws.numel(),), device), ws.numel(), ws
+
+
+def _stream_on(stream, device) -> Optional[int]:
+    """The stream that a call on `device` goes to: the given one, or the current one of that device."""
+    import torch
+    s = torch.cuda.current_stream(device) if stream is None else stream
+    if s.device != device:
+        raise ValueError("the stream belongs to %s, the cache to %s" % (s.device, device))
+    return int(s.cuda_stream) or None
+
+
+def attend_workspace_bytes(shape: Shape, weights: bool = False) -> int:
+    n = ctypes.c_size_t(0)
+    _check(lib().jq_attend_workspace_bytes(ctypes.byref(shape.c_struct()), int(bool(weights)), ctypes.byref(n)), "jq_attend_workspace_bytes")
+    return int(n.value)
+
+
+def alloc_attend_workspace(shape: Shape, weights: bool = False, device="cuda"):
+    import torch
+    return torch.empty(attend_workspace_bytes(shape, weights), dtype=torch.uint8, device=device)
+
+
+def _attend(name, shape: Shape, pages, seen, Q, K, V, lens, out, lse, want_lse, weights, ws, stream):
+    import torch
+    dev, bf, f32, i32 = K.device, torch.bfloat16, torch.float32, torch.int32
+    q_size = (shape.n_layers, shape.n_seq, shape.n_q, shape.h_q, shape.d)
+    kv = _cache_size(shape, pages)
+    qp, kp, vp = _tensor("Q", Q, bf, q_size, dev), _tensor("K", K, bf, kv, dev), _tensor("V", V, bf, kv, dev)
+    lp = _tensor("lens", lens, i32, (shape.n_layers, shape.n_seq), dev)
+    wp = _tensor("weights", weights, f32, (shape.n_layers, shape.h_kv, shape.T), dev)
+    if out is None:
+        out = torch.empty_like(Q)
+    if lse is None and want_lse:
+        lse = torch.empty(q_size[:4], dtype=f32, device=dev)
+    op, ep = _tensor("out", out, bf, q_size, dev), _tensor("lse", lse, f32, q_size[:4], dev)
+    sp, n, ws = _workspace(ws, lambda: attend_workspace_bytes(shape, weights is not None), dev)
+    mask, tail = (), (wp,)
+    if seen is not None:
+        mask, tail = (_tensor("seen", seen, i32, (shape.n_seq, shape.n_q, -(-shape.n_q // 32)), dev),), ()
+    with torch.cuda.device(dev):
+        _check(getattr(lib(), name)(ctypes.byref(shape.c_struct()), *_pages_arg(shape, pages, dev), lp, *mask, qp, kp, vp, op, ep, *tail, sp, n,
+                                    _stream_on(stream, dev)), name)
+    return out, lse
+
+
+def attend(shape: Shape, Q, K, V, lens=None, weights=None, out=None, lse=None, ws=None, stream=None, want_lse=True):
+    """Attention of every sequence's newest shape.n_q tokens over its live rows.  Q [n_layers, n_seq, n_q, h_q, d]; K, V
+    [n_layers, T, h_kv, d] with room for shape.seq_lens rows, of which lens [n_layers, n_seq] int32 are live (None: all).
+    shape.window: the queries are the last n_q live rows' own tokens, causal among themselves.  `weights`
+    [n_layers, h_kv, T] fp32 grows in place by the attention every row receives.  Returns (out, log-sum-exps)."""
+    return _attend("jq_attend", shape, None, None, Q, K, V, lens, out, lse, want_lse, weights, ws, stream)
+
+
+def attend_paged(shape: Shape, pages: Pages, Q, K_pool, V_pool, lens=None, weights=None, out=None, lse=None, ws=None, stream=None,
+                 want_lse=True):
+    """attend() on a paged cache: pools [n_layers, n_pages, page_size, h_kv, d]; `weights` in logical row order."""
+    return _attend("jq_attend_paged", shape, pages, None, Q, K_pool, V_pool, lens, out, lse, want_lse, weights, ws, stream)
+
+
+def attend_tree(shape: Shape, seen, Q, K, V, lens=None, out=None, lse=None, ws=None, stream=None, want_lse=True):
+    """Attention of a tree of shape.n_q drafted tokens whose rows are the last n_q live ones: each sees every row before
+    those, and drafted token j where bit j % 32 of seen[s, i, j // 32] is set (int32 [n_seq, n_q, ceil(n_q / 32)])."""
+    if seen is None:
+        raise JQError(-1, "jq_attend_tree")
+    return _attend("jq_attend_tree", shape, None, seen, Q, K, V, lens, out, lse, want_lse, None, ws, stream)
+
+
+def attend_tree_paged(shape: Shape, pages: Pages, seen, Q, K_pool, V_pool, lens=None, out=None, lse=None, ws=None, stream=None,
+                      want_lse=True):
+    """attend_tree() on a paged cache."""
+    if seen is None:
+        raise JQError(-1, "jq_attend_tree_paged")
+    return _attend("jq_attend_tree_paged", shape, pages, seen, Q, K_pool, V_pool, lens, out, lse, want_lse, None, ws, stream)
+
+
+def evict_weight_workspace_bytes(shape: Shape) -> int:
+    n = ctypes.c_size_t(0)
+    _check(lib().jq_evict_weight_workspace_bytes(ctypes.byref(shape.c_struct()), ctypes.byref(n)), "jq_evict_weight_workspace_bytes")
+    return int(n.value)
+
+
+def alloc_evict_weight_workspace(shape: Shape, device="cuda"):
+    import torch
+    return torch.empty(evict_weight_workspace_bytes(shape), dtype=torch.uint8, device=device)
+
+
+def _evict_weight(name, shape: Shape, pages, K, V, weights, pos, lens, K_out, V_out, weights_out, pos_out, idx_out, ws, stream):
+    import torch
+    dev, bf, f32, i32 = K.device, torch.bfloat16, torch.float32, torch.int32
+    kv, per_row = _cache_size(shape, pages), (shape.n_layers, shape.h_kv, shape.T)
+    if K_out is None and V_out is None and weights_out is None and pos_out is None:  # within the cache
+        K_out, V_out, weights_out, pos_out = K, V, weights, pos
+    if idx_out is None:
+        idx_out = torch.empty((shape.n_layers, shape.h_kv, shape.TB), dtype=i32, device=dev)
+    args = [_tensor("lens", lens, i32, (shape.n_layers, shape.n_seq), dev), _tensor("K", K, bf, kv, dev), _tensor("V", V, bf, kv, dev),
+            _tensor("weights", weights, f32, per_row, dev), _tensor("pos", pos, i32, per_row, dev), _tensor("K_out", K_out, bf, kv, dev),
+            _tensor("V_out", V_out, bf, kv, dev), _tensor("weights_out", weights_out, f32, per_row, dev),
+            _tensor("pos_out", pos_out, i32, per_row, dev), _tensor("idx_out", idx_out, i32, (shape.n_layers, shape.h_kv, shape.TB), dev)]
+    _tensor("layer_budgets", shape.layer_budgets, i32, (shape.n_layers, shape.n_seq), dev)
+    sp, n, ws = _workspace(ws, lambda: evict_weight_workspace_bytes(shape), dev)
+    with torch.cuda.device(dev):
+        _check(getattr(lib(), name)(ctypes.byref(shape.c_struct()), *_pages_arg(shape, pages, dev), *args, sp, n, _stream_on(stream, dev)), name)
+    return K_out, V_out, weights_out, pos_out, idx_out
+
+
+def evict_weight(shape: Shape, K, V, weights, pos=None, lens=None, K_out=None, V_out=None, weights_out=None, pos_out=None, idx_out=None,
+                 ws=None, stream=None):
+    """The shape.budgets heaviest live rows of every (layer, sequence, KV head), by accumulated attention weight, move to the
+    front of the sequence's segment: within K, V, weights and pos themselves when no output is given, otherwise into the
+    outputs (of the same sizes).  Positions below shape.keep_first and the newest shape.keep_last always stay.  Afterwards
+    min(lens, budget) rows are live.  Returns (K_out, V_out, weights_out, pos_out, idx_out)."""
+    return _evict_weight("jq_evict_weight", shape, None, K, V, weights, pos, lens, K_out, V_out, weights_out, pos_out, idx_out, ws, stream)
+
+
+def evict_weight_paged(shape: Shape, pages: Pages, K_pool, V_pool, weights, pos=None, lens=None, K_out=None, V_out=None, weights_out=None,
+                       pos_out=None, idx_out=None, ws=None, stream=None):
+    """evict_weight() on a paged cache; outputs are pools of the same shape behind the same block table."""
+    return _evict_weight("jq_evict_weight_paged", shape, pages, K_pool, V_pool, weights, pos, lens, K_out, V_out, weights_out, pos_out, idx_out,
+                         ws, stream)
+
+
+def _replace(name, shape: Shape, pages, k_new, v_new, token, K, V, weights, pos, lens, slot_out, stream):
+    import torch
+    dev, bf, f32, i32 = K.device, torch.bfloat16, torch.float32, torch.int32
+    kv, per_row, new = _cache_size(shape, pages), (shape.n_layers, shape.h_kv, shape.T), (shape.n_layers, shape.n_seq, shape.h_kv)
+    if slot_out is None:
+        slot_out = torch.empty(new, dtype=i32, device=dev)
+    args = [_tensor("lens", lens, i32, new[:2], dev), _tensor("k_new", k_new, bf, new + (shape.d,), dev),
+            _tensor("v_new", v_new, bf, new + (shape.d,), dev), _tensor("token", token, i32, (shape.n_seq,), dev), _tensor("K", K, bf, kv, dev),
+            _tensor("V", V, bf, kv, dev), _tensor("weights", weights, f32, per_row, dev), _tensor("pos", pos, i32, per_row, dev),
+            _tensor("slot_out", slot_out, i32, new, dev)]
+    with torch.cuda.device(dev):
+        _check(getattr(lib(), name)(ctypes.byref(shape.c_struct()), *_pages_arg(shape, pages, dev), *args, _stream_on(stream, dev)), name)
+    return slot_out
+
+
+def replace_lightest(shape: Shape, k_new, v_new, token, K, V, weights, pos, lens=None, slot_out=None, stream=None):
+    """One new token's row per (layer, sequence, KV head) [n_layers, n_seq, h_kv, d], at position token [n_seq]: appended while
+    lens leaves room, then in the place of the lightest row, the first shape.keep_first positions and the newest
+    shape.keep_last (the new token among them) aside.  K, V, weights and pos change in place.  Returns the slots taken."""
+    return _replace("jq_replace_lightest", shape, None, k_new, v_new, token, K, V, weights, pos, lens, slot_out, stream)
+
+
+def replace_lightest_paged(shape: Shape, pages: Pages, k_new, v_new, token, K_pool, V_pool, weights, pos, lens=None, slot_out=None,
+                           stream=None):
+    """replace_lightest() on a paged cache."""
+    return _replace("jq_replace_lightest_paged", shape, pages, k_new, v_new, token, K_pool, V_pool, weights, pos, lens, slot_out, stream)
 
 
 def reload_knobs() -> None:

@@ -692,6 +692,167 @@ int jq_map_mse_fused(const jq_shape* shape, const void* Q_a, const void* Q_b, in
     return launch_status(e);
 }
 
+// ---- decoding on a pruned cache --------------------------------------------------------------------------------
+
+namespace {
+struct Buf {
+    const void* p;
+    size_t n;
+};
+// Whether any of the `n_out` buffers overlaps any of the `n_in` or another of its own (null ones aside).
+bool any_overlap(const Buf* outs, int n_out, const Buf* ins, int n_in) {
+    for (int o = 0; o < n_out; ++o) {
+        if (!outs[o].p) continue;
+        for (int i = 0; i < n_in; ++i)
+            if (ins[i].p && overlaps(outs[o].p, outs[o].n, ins[i].p, ins[i].n)) return true;
+        for (int o2 = o + 1; o2 < n_out; ++o2)
+            if (outs[o2].p && overlaps(outs[o].p, outs[o].n, outs[o2].p, outs[o2].n)) return true;
+    }
+    return false;
+}
+size_t lens_bytes(const Plan& p) { return (size_t)p.n_layers * p.n_seq * 4; }
+
+int attend_plan(const jq_shape* shape, bool weights, Plan* p, AttendPlan* ap) {
+    const int rc = make_plan(shape, false, p, false);
+    if (rc != JQ_OK) return rc;
+    if (weights && p->rows > kMaxWeighRows) return JQ_ERR_UNSUPPORTED;
+    plan_attend(*p, weights, ap);
+    return attend_fits(*p, *ap) ? JQ_OK : JQ_ERR_UNSUPPORTED;
+}
+}  // namespace
+
+int jq_attend_workspace_bytes(const jq_shape* shape, int32_t with_weights, size_t* bytes) {
+    if (!bytes) return JQ_ERR_NULL;
+    Plan p;
+    AttendPlan ap;
+    const int rc = attend_plan(shape, with_weights != 0, &p, &ap);
+    if (rc != JQ_OK) return rc;
+    *bytes = ap.ws_bytes;
+    return JQ_OK;
+}
+
+static int attend_impl(const jq_shape* shape, const jq_pages* pages, bool paged, const int32_t* lens, const uint32_t* seen, bool tree, const void* Q,
+                       const void* K, const void* V, void* out, float* lse, float* weights, void* ws, size_t ws_bytes, void* stream) {
+    Plan p;
+    AttendPlan ap;
+    int rc = attend_plan(shape, weights != nullptr, &p, &ap);
+    if (rc != JQ_OK) return rc;
+    if (paged && (rc = apply_pages(pages, &p)) != JQ_OK) return rc;
+    if (tree) {
+        if (p.window) return JQ_ERR_SHAPE;  // the tree says what a drafted token sees
+        if (p.n_q > JQ_MAX_DRAFT) return JQ_ERR_UNSUPPORTED;
+        for (int s = 0; s < p.n_seq; ++s)
+            if (p.tab.cu_seq[s + 1] - p.tab.cu_seq[s] < p.n_q) return JQ_ERR_SHAPE;  // no room for the drafted tokens' rows
+    }
+    if (!Q || !K || !V || !out || (tree && !seen) || !ws) return JQ_ERR_NULL;
+    if (misaligned(ws, 16) || ws_bytes < ap.ws_bytes) return JQ_ERR_WORKSPACE;
+    if (misaligned(Q, 16) || misaligned(K, 16) || misaligned(V, 16) || misaligned(out, 16) || (lse && misaligned(lse, 4)) ||
+        (weights && misaligned(weights, 4)) || (lens && misaligned(lens, 4)) || (seen && misaligned(seen, 4)))
+        return JQ_ERR_UNSUPPORTED;
+    const Buf ins[6] = {{Q, q_bytes(p)}, {K, kv_bytes(p)}, {V, kv_bytes(p)}, {lens, lens_bytes(p)},
+                        {seen, (size_t)p.n_seq * p.n_q * ((p.n_q + 31) / 32) * 4}, {p.block_table, table_bytes(p)}};
+    const Buf outs[4] = {{out, q_bytes(p)}, {lse, lse_bytes(p)}, {weights, score_bytes(p)}, {ws, ap.ws_bytes}};
+    if (any_overlap(outs, 4, ins, 6)) return JQ_ERR_ALIAS;
+    return launch_status(launch_attend(p, ap, lens, seen, Q, K, V, out, lse, weights, (char*)ws, (hipStream_t)stream));
+}
+
+int jq_attend(const jq_shape* shape, const int32_t* lens, const void* Q, const void* K, const void* V, void* out, float* lse, float* weights, void* ws,
+              size_t ws_bytes, void* stream) {
+    return attend_impl(shape, nullptr, false, lens, nullptr, false, Q, K, V, out, lse, weights, ws, ws_bytes, stream);
+}
+
+int jq_attend_paged(const jq_shape* shape, const jq_pages* pages, const int32_t* lens, const void* Q, const void* K_pool, const void* V_pool, void* out,
+                    float* lse, float* weights, void* ws, size_t ws_bytes, void* stream) {
+    return attend_impl(shape, pages, true, lens, nullptr, false, Q, K_pool, V_pool, out, lse, weights, ws, ws_bytes, stream);
+}
+
+int jq_attend_tree(const jq_shape* shape, const int32_t* lens, const uint32_t* seen, const void* Q, const void* K, const void* V, void* out, float* lse,
+                   void* ws, size_t ws_bytes, void* stream) {
+    return attend_impl(shape, nullptr, false, lens, seen, true, Q, K, V, out, lse, nullptr, ws, ws_bytes, stream);
+}
+
+int jq_attend_tree_paged(const jq_shape* shape, const jq_pages* pages, const int32_t* lens, const uint32_t* seen, const void* Q, const void* K_pool,
+                         const void* V_pool, void* out, float* lse, void* ws, size_t ws_bytes, void* stream) {
+    return attend_impl(shape, pages, true, lens, seen, true, Q, K_pool, V_pool, out, lse, nullptr, ws, ws_bytes, stream);
+}
+
+int jq_evict_weight_workspace_bytes(const jq_shape* shape, size_t* bytes) {
+    if (!bytes) return JQ_ERR_NULL;
+    Plan p;
+    const int rc = make_plan(shape, true, &p, false);
+    if (rc != JQ_OK) return rc;
+    *bytes = align_up(idx_bytes(p));
+    return JQ_OK;
+}
+
+static int evict_weight_impl(const jq_shape* shape, const jq_pages* pages, bool paged, const int32_t* lens, const void* K, const void* V,
+                             const float* weights, const int32_t* pos, void* K_out, void* V_out, float* weights_out, int32_t* pos_out, int32_t* idx_out,
+                             void* ws, size_t ws_bytes, void* stream) {
+    Plan p;
+    int rc = make_plan(shape, true, &p, false);
+    if (rc != JQ_OK) return rc;
+    if (p.window) return JQ_ERR_SHAPE;  // no queries here
+    if (paged && (rc = apply_pages(pages, &p)) != JQ_OK) return rc;
+    if ((uint64_t)p.n_layers * p.TB * p.h_kv * 16 > UINT32_MAX) return JQ_ERR_UNSUPPORTED;
+    if (!K || !V || !weights || !K_out || !V_out || !weights_out || (pos && !pos_out) || !ws) return JQ_ERR_NULL;
+    const size_t need = align_up(idx_bytes(p));
+    if (misaligned(ws, 16) || ws_bytes < need) return JQ_ERR_WORKSPACE;
+    if (misaligned(K, 16) || misaligned(V, 16) || misaligned(K_out, 16) || misaligned(V_out, 16) || misaligned(weights, 4) || misaligned(weights_out, 4) ||
+        (pos && misaligned(pos, 4)) || (pos_out && misaligned(pos_out, 4)) || (idx_out && misaligned(idx_out, 4)) || (lens && misaligned(lens, 4)))
+        return JQ_ERR_UNSUPPORTED;
+    // within one cache: every output is its input; otherwise none of them touches any
+    const bool inplace = K_out == K && V_out == V && weights_out == weights && (!pos || pos_out == pos);
+    const size_t nkv = kv_bytes(p), nw = score_bytes(p);
+    const Buf ins[7] = {{lens, lens_bytes(p)}, {p.block_table, table_bytes(p)}, {p.layer_budgets, lb_bytes(p)}, {inplace ? nullptr : K, nkv},
+                        {inplace ? nullptr : V, nkv}, {inplace ? nullptr : weights, nw}, {inplace ? nullptr : pos, nw}};
+    const Buf outs[6] = {{K_out, nkv}, {V_out, nkv}, {weights_out, nw}, {pos_out, nw}, {idx_out, idx_bytes(p)}, {ws, need}};
+    if (any_overlap(outs, 6, ins, 7)) return JQ_ERR_ALIAS;
+    return launch_status(launch_evict_weight(p, lens, K, V, weights, pos, K_out, V_out, weights_out, pos_out, idx_out ? idx_out : (int32_t*)ws,
+                                             (hipStream_t)stream));
+}
+
+int jq_evict_weight(const jq_shape* shape, const int32_t* lens, const void* K, const void* V, const float* weights, const int32_t* pos, void* K_out,
+                    void* V_out, float* weights_out, int32_t* pos_out, int32_t* idx_out, void* ws, size_t ws_bytes, void* stream) {
+    return evict_weight_impl(shape, nullptr, false, lens, K, V, weights, pos, K_out, V_out, weights_out, pos_out, idx_out, ws, ws_bytes, stream);
+}
+
+int jq_evict_weight_paged(const jq_shape* shape, const jq_pages* pages, const int32_t* lens, const void* K_pool, const void* V_pool, const float* weights,
+                          const int32_t* pos, void* K_out, void* V_out, float* weights_out, int32_t* pos_out, int32_t* idx_out, void* ws,
+                          size_t ws_bytes, void* stream) {
+    return evict_weight_impl(shape, pages, true, lens, K_pool, V_pool, weights, pos, K_out, V_out, weights_out, pos_out, idx_out, ws, ws_bytes, stream);
+}
+
+static int replace_impl(const jq_shape* shape, const jq_pages* pages, bool paged, const int32_t* lens, const void* k_new, const void* v_new,
+                        const int32_t* token, void* K, void* V, float* weights, int32_t* pos, int32_t* slot_out, void* stream) {
+    Plan p;
+    int rc = make_plan(shape, false, &p, false);
+    if (rc != JQ_OK) return rc;
+    if (p.window) return JQ_ERR_SHAPE;
+    if (paged && (rc = apply_pages(pages, &p)) != JQ_OK) return rc;
+    for (int s = 0; s < p.n_seq; ++s)  // a row that may go has to be there, the new token aside
+        if ((int64_t)p.keep_first + std::max(p.keep_last, 1) > p.tab.cu_seq[s + 1] - p.tab.cu_seq[s]) return JQ_ERR_BUDGET;
+    if (!k_new || !v_new || !token || !K || !V || !weights || !pos) return JQ_ERR_NULL;
+    if (misaligned(k_new, 16) || misaligned(v_new, 16) || misaligned(K, 16) || misaligned(V, 16) || misaligned(token, 4) || misaligned(weights, 4) ||
+        misaligned(pos, 4) || (slot_out && misaligned(slot_out, 4)) || (lens && misaligned(lens, 4)))
+        return JQ_ERR_UNSUPPORTED;
+    const size_t new_bytes = (size_t)p.n_layers * p.n_seq * p.h_kv * p.d * 2;
+    const Buf ins[5] = {{lens, lens_bytes(p)}, {p.block_table, table_bytes(p)}, {k_new, new_bytes}, {v_new, new_bytes}, {token, (size_t)p.n_seq * 4}};
+    const Buf outs[5] = {{K, kv_bytes(p)}, {V, kv_bytes(p)}, {weights, score_bytes(p)}, {pos, score_bytes(p)},
+                         {slot_out, (size_t)p.n_layers * p.n_seq * p.h_kv * 4}};
+    if (any_overlap(outs, 5, ins, 5)) return JQ_ERR_ALIAS;
+    return launch_status(launch_replace(p, lens, k_new, v_new, token, K, V, weights, pos, slot_out, (hipStream_t)stream));
+}
+
+int jq_replace_lightest(const jq_shape* shape, const int32_t* lens, const void* k_new, const void* v_new, const int32_t* token, void* K, void* V,
+                        float* weights, int32_t* pos, int32_t* slot_out, void* stream) {
+    return replace_impl(shape, nullptr, false, lens, k_new, v_new, token, K, V, weights, pos, slot_out, stream);
+}
+
+int jq_replace_lightest_paged(const jq_shape* shape, const jq_pages* pages, const int32_t* lens, const void* k_new, const void* v_new,
+                              const int32_t* token, void* K_pool, void* V_pool, float* weights, int32_t* pos, int32_t* slot_out, void* stream) {
+    return replace_impl(shape, pages, true, lens, k_new, v_new, token, K_pool, V_pool, weights, pos, slot_out, stream);
+}
+
 int jq_copy_probe(const void* src, void* dst, size_t bytes, void* stream) {
     if (!src || !dst) return JQ_ERR_NULL;
     if (bytes == 0 || bytes % 16 != 0) return JQ_ERR_SHAPE;

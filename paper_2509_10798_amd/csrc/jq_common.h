@@ -350,4 +350,23 @@ hipError_t launch_hit_rate(const Plan& p, const int32_t* cu_ref_budgets, int64_t
                            const int32_t* ref, float* rate, hipStream_t st);
 hipError_t launch_copy_probe(const void* src, void* dst, size_t bytes, hipStream_t st);
 
+// Decoding on a pruned cache (jq_attend.hip, jq_weight.hip).  How a call's sequences are shared out and where its workspace's pieces lie:
+constexpr int kMaxWeighRows = 128;  // most query rows per KV head whose weights are accumulated: their logits are kept until all sums are known
+struct AttendPlan {
+    int32_t row_tiles, row_groups;      // tiles of 16 query rows a workgroup takes, workgroups over the same keys
+    int32_t cu_split[JQ_MAX_SEQ + 1];   // workgroups that share a sequence (per layer, KV head and group of rows), summed up
+    int64_t logit_T;
+    size_t off_stats, off_part, off_logits, ws_bytes;
+};
+void plan_attend(const Plan& p, bool weights, AttendPlan* ap);
+bool attend_fits(const Plan& p, const AttendPlan& ap);  // every launch stays below 2^32 threads
+// `lens`, `seen`, `lse`, `weights` may be null; with `seen` the queries are drafted tokens, otherwise p.window says whether they are causal.
+hipError_t launch_attend(const Plan& p, const AttendPlan& ap, const int32_t* lens, const uint32_t* seen, const void* Q, const void* K, const void* V,
+                         void* out, float* lse, float* weights, char* ws, hipStream_t st);
+// K_out == K (then V_out == V, weights_out == weights and pos_out == pos too): within one cache.  `idx` [n_layers][h_kv][TB] takes the kept rows.
+hipError_t launch_evict_weight(const Plan& p, const int32_t* lens, const void* K, const void* V, const float* weights, const int32_t* pos,
+                               void* K_out, void* V_out, float* weights_out, int32_t* pos_out, int32_t* idx, hipStream_t st);
+hipError_t launch_replace(const Plan& p, const int32_t* lens, const void* k_new, const void* v_new, const int32_t* token, void* K, void* V, float* weights,
+                          int32_t* pos, int32_t* slot, hipStream_t st);
+
 }  // namespace jq
