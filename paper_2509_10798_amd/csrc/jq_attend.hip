@@ -16,6 +16,8 @@
 // is V transposed: lane l loads 16 bytes (d = 8 * (l % 16) .. + 7) of the rows 4 * (l / 16) + e, a wave's load covers whole rows, and
 // byte permutes inside the lane pair the rows up: no value passes through LDS, and no workgroup barrier stands in the sweep.
 // out comes out transposed too: lane l holds d = 32 * (l / 16) .. + 31 of query row l % 16, in line with m and z.
+#include <type_traits>
+
 #include "jq_common.h"
 
 namespace jq {
@@ -28,6 +30,7 @@ constexpr int kAttendWaves = 4;
 constexpr int kAttendThreads = 64 * kAttendWaves;
 constexpr int kTileRows = 16;   // query rows of one MFMA tile
 constexpr int kOutStride = kHeadDim + 4;  // floats a row of partial output takes in LDS: rows of 128 would meet in the same banks
+constexpr int kMostHeld = 65536;  // bytes of logits that a workgroup holds in LDS
 constexpr float kSlack = 8.0f;  // a row's running maximum may lag this far (in powers of two) behind before its sums are rescaled
 
 // Which cache rows a query row sees, apart from the live ones' end.
@@ -43,8 +46,11 @@ struct AttendArgs {
     float2* stats;         // their (m, z), [n_layers][splits][h_kv][rows]; m in powers of two
     float* logits;         // with weights: scale * log2(e) * q . k, [n_layers][h_kv][rows][logit_T]
     int32_t n_layers, n_seq, n_q, h_q, h_kv, group, rows, row_groups, units, n_splits, words;
+    int32_t hold_keys;     // rows of the cache whose logits a workgroup holds in LDS at most (those of more than 32 query rows are not held)
     float scale2;          // scale * log2(e)
     int64_t T, logit_T;
+    uint64_t* arrived;     // one launch: [n_layers][n_seq][h_kv][row_groups], `tag` and the number of workgroups done
+    uint64_t tag;          // 40 bits of the call's own above 24 of zeros; 0: another launch joins
     PageMap pm;
     int32_t cu_seq[JQ_MAX_SEQ + 1];
     int32_t cu_split[JQ_MAX_SEQ + 1];
@@ -56,6 +62,27 @@ __device__ __forceinline__ int32_t live_rows(const int32_t* lens, int n_seq, int
 
 // First entry of a sequence's logits in a row of logit_T: whole tiles of 32 keys have room in front of the next sequence's.
 __device__ __forceinline__ int64_t logit_at(const int32_t* cu_seq, int s) { return 32 * ((int64_t)(cu_seq[s] / 32) + s); }
+
+// What one workgroup leaves for another of the same launch: stored and loaded past the caches that the XCDs do not share.
+__device__ __forceinline__ void put_pair(float* p, float x, float y) {
+    __hip_atomic_store((uint64_t*)p, (uint64_t)__float_as_uint(x) | (uint64_t)__float_as_uint(y) << 32, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ float2 get_pair(const float* p) {
+    const uint64_t v = __hip_atomic_load((const uint64_t*)p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    return make_float2(__uint_as_float((uint32_t)v), __uint_as_float((uint32_t)(v >> 32)));
+}
+
+// The sequence that a split belongs to: all of the table's entries at once, where a binary search would wait for one after the other.
+__device__ __forceinline__ int seq_of_split(const AttendArgs& a, int split, int lane) {
+    if (a.n_seq == 1) return 0;
+    int s = __popcll(__ballot(lane + 1 < a.n_seq && a.cu_split[min(lane + 1, a.n_seq)] <= split));
+    if (a.n_seq > 64) s += __popcll(__ballot(lane + 65 < a.n_seq && a.cu_split[min(lane + 65, a.n_seq)] <= split));
+    return s;
+}
+
+// log2 of a sum: v_log_f32 rounds towards zero and is off by more the larger its result, so it only sees the mantissa.
+__device__ __forceinline__ float log2_of(float z) { return (float)__builtin_amdgcn_frexp_expf(z) + __builtin_amdgcn_logf(__builtin_amdgcn_frexp_mantf(z)); }
+constexpr float kLn2 = 0.69314718055994531f;
 
 __device__ __forceinline__ float max4(f32x4 x) { return fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])); }
 
@@ -98,7 +125,7 @@ struct RowState {
 // One tile of 32 keys.  MASKED: some row may not see some key of it, or the tile reaches past the live rows.
 template <int RT, bool MASKED, int MASK, bool KEEP>
 __device__ __forceinline__ void tile_step(RowState<RT>& st, KvTile& t, const AttendArgs& a, int lane, int key0, int n, const int* row_limit,
-                                          const uint32_t* const* row_seen, float* const* row_logits) {
+                                          const uint32_t* const* row_seen, float* hold) {
     uint32_t bad[2][4];  // keys whose V is not finite, by the lanes that hold their 16 pieces
     if (MASKED) {
         // What a query row does not see must not reach it, not even times zero: such values count as zeros, and every row
@@ -143,12 +170,12 @@ __device__ __forceinline__ void tile_step(RowState<RT>& st, KvTile& t, const Att
                     s[r][i][e] = see ? (bad[i][e] ? __builtin_nanf("") : s[r][i][e]) : -__builtin_inff();
                 }
     }
-    if (KEEP) {
+    if (KEEP) {  // `hold`: the lane's place in the tile's part of the held logits, null for the lanes past the last query row
 #pragma unroll
         for (int r = 0; r < RT; ++r)
-            if (row_logits[r]) {
+            if (hold && r * kTileRows + (lane & 15) < a.rows) {
 #pragma unroll
-                for (int i = 0; i < 2; ++i) *(f32x4*)(row_logits[r] + key0 + 16 * i + 4 * (lane >> 4)) = s[r][i];
+                for (int i = 0; i < 2; ++i) *(f32x4*)(hold + r * kTileRows * a.hold_keys + 16 * i) = s[r][i];
             }
     }
     // Running maximum: raised, and the sums rescaled, only when a score passes it by more than kSlack; terms stay below 2^8.
@@ -199,6 +226,57 @@ __device__ __forceinline__ void tile_step(RowState<RT>& st, KvTile& t, const Att
     }
 }
 
+// Four dimensions of a query row's output out of its sums; a row that has seen nothing: zeros, and -inf for its log-sum-exp.
+__device__ __forceinline__ void store_out(const AttendArgs& a, int layer, int s, int g, int row, int d, f32x4 o, float m, float z) {
+    const int i = row / a.group, h = g * a.group + row - i * a.group;
+    const int64_t q_row = (((int64_t)layer * a.n_seq + s) * a.n_q + i) * a.h_q + h;
+    const float inv = z == 0.0f ? 0.0f : 1.0f / z;
+    __bf16 y[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) y[e] = (__bf16)(o[e] * inv);
+    *(uint2*)(a.out + q_row * kHeadDim + d) = *(const uint2*)y;
+    if (a.lse && d == 0) a.lse[q_row] = z == 0.0f ? -__builtin_inff() : (m + log2_of(z)) * kLn2;
+}
+
+// weights[j] += sum_r 2^(x[r,j] - lse2[r]) for the rows j from `begin` to `end` of the cache, all threads of the workgroup together;
+// the logits may have been left by other workgroups of the launch.
+__device__ __forceinline__ void add_weights(const AttendArgs& a, int layer, int s, int g, const float* lse2, int begin, int end) {
+    const float* x = a.logits + ((int64_t)layer * a.h_kv + g) * a.rows * a.logit_T + logit_at(a.cu_seq, s);
+    float* w = a.weights + ((int64_t)layer * a.h_kv + g) * a.T + a.cu_seq[s];
+    constexpr int kPairs = 4;  // of rows, a thread: sixteen loads under way at a time
+    for (int j0 = begin + 2 * (int)threadIdx.x; j0 < end; j0 += 2 * kPairs * kAttendThreads) {
+        float2 sum[kPairs];
+#pragma unroll
+        for (int k = 0; k < kPairs; ++k) sum[k] = make_float2(0.0f, 0.0f);
+        for (int r0 = 0; r0 < a.rows; r0 += 4) {
+            float2 y[kPairs][4];
+#pragma unroll
+            for (int k = 0; k < kPairs; ++k)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const int j = j0 + 2 * k * kAttendThreads;
+                    y[k][r] = get_pair(x + min(r0 + r, a.rows - 1) * a.logit_T + (j < end ? j : j0));
+                }
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+                if (r0 + r < a.rows) {
+                    const float l = lse2[r0 + r];
+#pragma unroll
+                    for (int k = 0; k < kPairs; ++k) {
+                        sum[k].x += __builtin_amdgcn_exp2f(y[k][r].x - l);
+                        sum[k].y += __builtin_amdgcn_exp2f(y[k][r].y - l);
+                    }
+                }
+        }
+#pragma unroll
+        for (int k = 0; k < kPairs; ++k) {
+            const int j = j0 + 2 * k * kAttendThreads;
+            if (j < end) w[j] += sum[k].x;
+            if (j + 1 < end) w[j + 1] += sum[k].y;
+        }
+    }
+}
+
 template <int RT, int MASK, bool KEEP>
 __global__ __launch_bounds__(kAttendThreads, RT == 1 ? 3 : 2) void jq_attend_kernel(AttendArgs a) {
     extern __shared__ __align__(16) float lds[];  // [waves][16 RT][kOutStride], then (m, z) [waves][16 RT]
@@ -208,16 +286,21 @@ __global__ __launch_bounds__(kAttendThreads, RT == 1 ? 3 : 2) void jq_attend_ker
     const int u = (int)blockIdx.x / per * 8 + ((int)blockIdx.x & 7), rg = ((int)blockIdx.x % per) >> 3;
     if (u >= a.units) return;
     const int layer = blockIdx.y, split = u / a.h_kv, g = u - split * a.h_kv;
-    const int s = find_seq(a.cu_split, a.n_seq, split);
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+    const int s = seq_of_split(a, split, lane);
     const int ns = a.cu_split[s + 1] - a.cu_split[s], mine = split - a.cu_split[s];
     const int n = live_rows(a.lens, a.n_seq, layer, s, a.cu_seq[s + 1] - a.cu_seq[s]);
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
     const int row0 = rg * RT * kTileRows;
+    // The sequence's count of finished workgroups starts at zero for this call: it holds the call's tag or is given it here.
+    uint64_t* arrived = a.arrived + (((int64_t)layer * a.n_seq + s) * a.h_kv + g) * a.row_groups + rg;
+    if (a.tag && ns > 1 && threadIdx.x == 0) {
+        uint64_t was = __hip_atomic_load(arrived, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        if ((was ^ a.tag) >> 24) __hip_atomic_compare_exchange_strong(arrived, &was, a.tag, __ATOMIC_RELAXED, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    }
 
     RowState<RT> st;
     int row_limit[RT];
     const uint32_t* row_seen[RT];
-    float* row_logits[RT];
 #pragma unroll
     for (int r = 0; r < RT; ++r) {
         const int row = min(row0 + r * kTileRows + (lane & 15), a.rows - 1);  // rows past the last repeat it and are not stored
@@ -231,9 +314,6 @@ __global__ __launch_bounds__(kAttendThreads, RT == 1 ? 3 : 2) void jq_attend_ker
         st.z[r] = 0.0f;
         row_limit[r] = n - a.n_q + i + 1;
         row_seen[r] = MASK == kSeeTree ? a.seen + ((int64_t)s * a.n_q + i) * a.words : nullptr;
-        row_logits[r] = nullptr;
-        if (KEEP && row0 + r * kTileRows + (lane & 15) < a.rows)
-            row_logits[r] = a.logits + (((int64_t)layer * a.h_kv + g) * a.rows + row) * a.logit_T + logit_at(a.cu_seq, s);
     }
 
     // Tiles of 32 keys, dealt to the sequence's waves in turn, so that all of them sweep one moving window of the cache.
@@ -252,15 +332,20 @@ __global__ __launch_bounds__(kAttendThreads, RT == 1 ? 3 : 2) void jq_attend_ker
     const int open = MASK == kSeeAll ? n : max(n - a.n_q + (MASK == kSeeCausal ? 1 : 0), 0);
     const int step = 32 * kAttendWaves * ns;
     int key = 32 * (kAttendWaves * mine + wave);
-    // One tile at a time: the waves of a SIMD take turns waiting, and together they ask for far more than memory needs to be asked for.
+    // With weights every row's logits stay in LDS until its sums are known, [rows][hold_keys], a wave's tiles four apart.  (Written
+    // out as they are formed they kept reads from being under way: 32 sequences of 2048 rows 71.7 us a call, without weights 58.3.)
+    float* held = (float*)(lds_stats + kAttendWaves * RT * kTileRows);
+    float* hold = KEEP ? held + (lane & 15) * a.hold_keys + 32 * wave + 4 * (lane >> 4) : nullptr;
     KvTile t;
     for (; key + 32 <= open; key += step) {
         load_tile(t, K, V, tile_row(key), 31, stride, lane);
-        tile_step<RT, false, MASK, KEEP>(st, t, a, lane, key, n, row_limit, row_seen, row_logits);
+        tile_step<RT, false, MASK, KEEP>(st, t, a, lane, key, n, row_limit, row_seen, hold);
+        if (KEEP) hold += 32 * kAttendWaves;
     }
     for (; key < n; key += step) {
         load_tile(t, K, V, tile_row(key), n - 1 - key, stride, lane);
-        tile_step<RT, true, MASK, KEEP>(st, t, a, lane, key, n, row_limit, row_seen, row_logits);
+        tile_step<RT, true, MASK, KEEP>(st, t, a, lane, key, n, row_limit, row_seen, hold);
+        if (KEEP) hold += 32 * kAttendWaves;
     }
 
     // The four waves' sums, in wave order.
@@ -290,9 +375,9 @@ __global__ __launch_bounds__(kAttendThreads, RT == 1 ? 3 : 2) void jq_attend_ker
     }
     __syncthreads();
     const int64_t part_row = (((int64_t)layer * a.n_splits + split) * a.h_kv + g) * a.rows;
-    for (int item = threadIdx.x; item < RT * kTileRows * 32; item += kAttendThreads) {
+    const int rows_here = min(a.rows - row0, RT * kTileRows);
+    for (int item = threadIdx.x; item < rows_here * 32; item += kAttendThreads) {
         const int r = item >> 5, d = (item & 31) * 4, row = row0 + r;
-        if (row >= a.rows) break;
         float m = -__builtin_inff(), z = 0.0f;
 #pragma unroll
         for (int w = 0; w < kAttendWaves; ++w) m = fmaxf(m, lds_stats[w * RT * kTileRows + r].x);
@@ -303,130 +388,598 @@ __global__ __launch_bounds__(kAttendThreads, RT == 1 ? 3 : 2) void jq_attend_ker
             z += mz.x == m ? mz.y : mz.y * __builtin_amdgcn_exp2f(mz.x - m);
             o += *(const f32x4*)(lds + (w * RT * kTileRows + r) * kOutStride + d);
         }
-        if (ns > 1 || KEEP) {
-            if (ns > 1) *(f32x4*)(a.part + (part_row + row) * kHeadDim + d) = o;
-            if (d == 0) a.stats[part_row + row] = make_float2(m, z);
-        }
         if (ns == 1) {
-            const int i = row / a.group, h = g * a.group + row - i * a.group;
-            const int64_t q_row = (((int64_t)layer * a.n_seq + s) * a.n_q + i) * a.h_q + h;
-            const float inv = z == 0.0f ? 0.0f : 1.0f / z;  // a row that sees nothing: zeros, and -inf for its log-sum-exp
-            __bf16 y[4];
+            store_out(a, layer, s, g, row, d, o, m, z);
+        } else {
+            float* to = a.part + (part_row + row) * kHeadDim + d;
+            put_pair(to, o[0], o[1]);
+            put_pair(to + 2, o[2], o[3]);
+        }
+        if (d == 0 && (ns > 1 || KEEP)) put_pair((float*)(a.stats + part_row + row), m, z);
+    }
+    if (KEEP && ns == 1) {  // all of the sequence is here
+        float* lse2 = lds;  // (the sums above have been read by the threads that wait here)
+        __syncthreads();
+        if ((int)threadIdx.x < a.rows) {
+            float m = -__builtin_inff(), z = 0.0f;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) y[e] = (__bf16)(o[e] * inv);
-            *(uint2*)(a.out + q_row * kHeadDim + d) = *(const uint2*)y;
-            if (a.lse && d == 0) a.lse[q_row] = z == 0.0f ? -__builtin_inff() : (m + __builtin_amdgcn_logf(z)) * 0.69314718055994531f;
+            for (int w = 0; w < kAttendWaves; ++w) m = fmaxf(m, lds_stats[w * RT * kTileRows + threadIdx.x].x);
+#pragma unroll
+            for (int w = 0; w < kAttendWaves; ++w) {
+                const float2 mz = lds_stats[w * RT * kTileRows + threadIdx.x];
+                z += mz.x == m ? mz.y : mz.y * __builtin_amdgcn_exp2f(mz.x - m);
+            }
+            lse2[threadIdx.x] = z == 0.0f ? 0.0f : m + log2_of(z);
+        }
+        __syncthreads();
+        float* w = a.weights + ((int64_t)layer * a.h_kv + g) * a.T + a.cu_seq[s];
+        for (int j = threadIdx.x; j < n; j += kAttendThreads) {  // (one workgroup: row j of the cache is held at j)
+            float sum = 0.0f;
+            for (int r = 0; r < a.rows; ++r) sum += __builtin_amdgcn_exp2f(held[r * a.hold_keys + j] - lse2[r]);
+            w[j] += sum;
+        }
+        return;
+    }
+    if (KEEP) {  // the whole share's logits at once, to where the workgroup that weighs finds them
+        const int64_t to = ((int64_t)layer * a.h_kv + g) * a.rows * a.logit_T + logit_at(a.cu_seq, s);
+        const int pairs = a.hold_keys / 2;
+        for (int item = threadIdx.x; item < a.rows * pairs; item += kAttendThreads) {
+            const int r = item / pairs, j = (item - r * pairs) * 2, tile = j >> 5;
+            const int at = ((tile >> 2) * ns + mine) * 32 * kAttendWaves + 32 * (tile & 3) + (j & 31);
+            if (at < ((n + 31) & ~31)) put_pair(a.logits + to + r * a.logit_T + at, held[r * a.hold_keys + j], held[r * a.hold_keys + j + 1]);
+        }
+    }
+    if (!a.tag || ns == 1) return;
+
+    // Whoever completes a sequence joins it; nobody waits.  Data first, then the count of those that have left theirs.
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+    int* last = (int*)lds_stats;
+    if (ns > 1) {
+        if (threadIdx.x == 0) *last = (int)(__hip_atomic_fetch_add(arrived, 1ull, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) & 0xFFFFFF) + 1 == ns;
+        __syncthreads();
+        if (!*last) return;
+        if (threadIdx.x == 0) __hip_atomic_store(arrived, 0ull, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);  // a replay of the call counts from here
+    }
+    // Factors of all shares' sums, [rows_here][ns], and the rows' (m, z).
+    float* factor = lds;
+    const int64_t first = (((int64_t)layer * a.n_splits + a.cu_split[s]) * a.h_kv + g) * a.rows + row0, next_share = (int64_t)a.h_kv * a.rows;
+    __syncthreads();
+    for (int r = wave; r < rows_here; r += kAttendWaves) {  // a wave a row, a lane a share (there are 64 at most)
+        const float2 mz = lane < ns ? get_pair((const float*)(a.stats + first + r + lane * next_share)) : make_float2(-__builtin_inff(), 0.0f);
+        float m = mz.x;
+#pragma unroll
+        for (int d = 32; d; d >>= 1) m = fmaxf(m, __shfl_xor(m, d));
+        const float f = mz.x == m ? 1.0f : __builtin_amdgcn_exp2f(mz.x - m);
+        float z = mz.y * f;
+#pragma unroll
+        for (int d = 32; d; d >>= 1) z += __shfl_xor(z, d);
+        if (lane < ns) factor[r * ns + lane] = f;
+        if (lane == 0) lds_stats[r] = make_float2(m, z);
+    }
+    __syncthreads();
+    if (ns > 1) {
+        // Sixteen bytes of output a thread; where there are few rows several threads take shares of the shares.
+        const int items = rows_here * 32;
+        int parts = 1;
+        while (2 * parts * items <= kAttendThreads && parts < 8) parts *= 2;
+        float* sums = factor + rows_here * ns;  // [parts][items] outputs of four
+        for (int t0 = 0; t0 < items * parts; t0 += kAttendThreads) {
+            const int t = t0 + threadIdx.x, part = t / items, item = t - part * items, r = item >> 5, d = (item & 31) * 4;
+            f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
+            if (part < parts) {
+                const float* from = a.part + (first + r) * kHeadDim + d;
+                for (int i = part; i < ns; i += 8 * parts) {
+                    float2 lo[8], hi[8];
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) {
+                        const float* p = from + min(i + k * parts, ns - 1) * next_share * kHeadDim;
+                        lo[k] = get_pair(p);
+                        hi[k] = get_pair(p + 2);
+                    }
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) {
+                        const float f = i + k * parts < ns ? factor[r * ns + i + k * parts] : 0.0f;
+                        o += f32x4{lo[k].x, lo[k].y, hi[k].x, hi[k].y} * f;
+                    }
+                }
+            }
+            if (parts > 1) {
+                if (part < parts) *(f32x4*)(sums + 4 * t) = o;
+                __syncthreads();
+                if (part == 0)
+                    for (int k = 1; k < parts; ++k) o += *(const f32x4*)(sums + 4 * (k * items + item));
+            }
+            if (part == 0) store_out(a, layer, s, g, row0 + r, d, o, lds_stats[r].x, lds_stats[r].y);
+        }
+    }
+    if (KEEP) {
+        __syncthreads();
+        if ((int)threadIdx.x < rows_here) {
+            const float2 mz = lds_stats[threadIdx.x];
+            ((float*)(lds_stats + rows_here))[threadIdx.x] = mz.y == 0.0f ? 0.0f : mz.x + log2_of(mz.y);
+        }
+        __syncthreads();
+        add_weights(a, layer, s, g, (const float*)(lds_stats + rows_here), 0, n);
+    }
+}
+
+// Many query rows (more than 32 a KV head).  A wave still holds 32 of them, but the waves of a workgroup share the keys: R waves over
+// all rows of a group times KW over 32 keys each.  K and V go through LDS, where every wave reads all of its keys' rows: requested
+// into registers two stages ahead, written to one of two buffers, one barrier a stage.
+//   K's rows are read sixteen lanes a row of 256 bytes, piece p of row k at p ^ (k & 15), so that eight lanes' pieces meet in eight
+//   different bank groups; V is read transposed (ds_read_b64_tr_b16: a lane receives four keys' values of one dimension out of four
+//   rows of sixteen), piece p of row k at p ^ 2 (k & 7) for the same reason.  A wave reads 16 KB a stage for 32 rows, which takes
+//   LDS about as long as the matrix cores take for them.
+template <int R>
+struct Wide {
+    static constexpr int kWaves = 8, kThreads = 64 * kWaves, kRows = 32 * R;
+    static constexpr int KW = kWaves / R;                      // waves over the same rows, each with keys of its own
+    static constexpr int kKeys = KW == 1 ? 64 : 128;           // of a stage
+    static constexpr int kTiles = kKeys / 32 / KW;             // of 32 keys, a wave and stage
+    static constexpr int kAhead = KW == 1 ? 2 : 1;             // stages requested ahead: 64 KB
+    static constexpr bool kExact = R == 2;                     // probabilities in two bf16 parts
+    static constexpr int kRequests = kKeys / 2 / kWaves;       // of 1 KB, a wave and stage
+    static constexpr int kBuffer = 2 * kKeys * 256;            // K, then V
+    static constexpr int kMerge = (kWaves - R) * 32 * (kOutStride * 4 + 8);
+    static constexpr int kLds = 2 * kBuffer + 2 * kKeys > kMerge ? 2 * kBuffer + 2 * kKeys : kMerge;  // (behind the buffers a flag a key)
+};
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) s16x4* lds_s16x4;
+
+template <int R, int MASK, bool KEEP>
+__global__ __launch_bounds__(Wide<R>::kThreads, 2) void jq_attend_wide_kernel(AttendArgs a) {
+    using W = Wide<R>;
+    constexpr int KW = W::KW;
+    extern __shared__ __align__(16) char wide_lds[];
+    uint8_t* bad_keys = (uint8_t*)wide_lds + 2 * W::kBuffer;  // [2][kKeys]
+    const int per = 8 * a.row_groups;
+    const int u = (int)blockIdx.x / per * 8 + ((int)blockIdx.x & 7), rg = ((int)blockIdx.x % per) >> 3;
+    if (u >= a.units) return;
+    const int layer = blockIdx.y, split = u / a.h_kv, g = u - split * a.h_kv;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+    const int s = seq_of_split(a, split, lane);
+    const int ns = a.cu_split[s + 1] - a.cu_split[s], mine = split - a.cu_split[s];
+    const int n = live_rows(a.lens, a.n_seq, layer, s, a.cu_seq[s + 1] - a.cu_seq[s]);
+    const int rw = wave % R, kw = wave / R;
+    const int row0 = rg * W::kRows + 32 * rw;
+
+    bf16x8 q[2][4];
+    f32x4 o[2][8];  // d = 16 r + 4 (l / 16) + e of query row l % 16 in o[i][r][e]
+    float m[2], z[2];
+    int token[2];   // the query rows' tokens
+#pragma unroll
+    for (int r = 0; r < 2; ++r) {
+        const int row = min(row0 + r * kTileRows + (lane & 15), a.rows - 1);
+        const int i = row / a.group, h = g * a.group + row - i * a.group;
+        const char* from = a.Q + ((((int64_t)layer * a.n_seq + s) * a.n_q + i) * a.h_q + h) * (kHeadDim * 2);
+#pragma unroll
+        for (int c = 0; c < 4; ++c) q[r][c] = __builtin_bit_cast(bf16x8, *(const au32x4*)(from + 64 * c + 16 * (lane >> 4)));
+#pragma unroll
+        for (int d = 0; d < 8; ++d) o[r][d] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+        m[r] = -__builtin_inff();
+        z[r] = 0.0f;
+        token[r] = i;
+    }
+
+    const uint32_t stride = (uint32_t)a.h_kv * (kHeadDim * 2);
+    const int64_t first_row = a.pm.block_table ? ((int64_t)layer * a.pm.n_pages) << a.pm.page_shift : (int64_t)layer * a.T + a.cu_seq[s];
+    const_i32_ptr table = (const_i32_ptr)(a.pm.block_table ? a.pm.block_table + (int64_t)s * a.pm.max_pages : nullptr);
+    const int shift = a.pm.page_shift, n_pages = a.pm.n_pages;
+    const bool paged = a.pm.block_table != nullptr;
+    const int open = MASK == kSeeAll ? n : max(n - a.n_q + (MASK == kSeeCausal ? 1 : 0), 0);
+
+    // This wave's requests of a stage: kRequests times four rows of K or of V, all in one tile of 32 keys.
+    constexpr int kPerTile = 8 / W::kRequests;  // waves that share the requests of a tile
+    const bool is_v = wave >= W::kWaves / 2;
+    const int in_half = wave % (W::kWaves / 2), my_tile = in_half / kPerTile;
+    const int my_row = in_half % kPerTile * W::kRequests * 4 + (lane >> 4);  // the first request's row within the tile, 4 apart
+    const char* base = (is_v ? a.V : a.K) + first_row * stride + g * (kHeadDim * 2) + (lane & 15) * 16;
+    // where the requests go: the pieces of rows 4 apart are exchanged by amounts that differ
+    int to_lds[W::kRequests];
+#pragma unroll
+    for (int i = 0; i < W::kRequests; ++i) {
+        const int row = my_row + 4 * i, piece = is_v ? (lane & 15) ^ 2 * (row & 7) : (lane & 15) ^ (row & 15);
+        to_lds[i] = (is_v ? W::kKeys * 256 : 0) + (my_tile * 32 + row) * 256 + piece * 16;
+    }
+    auto request = [&](au32x4* to, int stage) {
+        int key = (mine + stage * ns) * W::kKeys + 32 * my_tile;
+        key = min(key, (n - 1) & ~31);  // (a stage may reach past the last tile)
+        const int last = n - 1 - key;
+        const uint32_t row0 = !paged ? (uint32_t)key : ((uint32_t)clamp_page(table[key >> shift], n_pages) << shift) + (uint32_t)(key & ((1 << shift) - 1));
+#pragma unroll
+        for (int i = 0; i < W::kRequests; ++i) to[i] = *(const au32x4*)(base + (row0 + (uint32_t)min(my_row + 4 * i, last)) * stride);
+    };
+    // Addresses of a wave's reads in buffer 0: K by chunk of the dimensions (16 keys further on: + 4096), V by block of sixteen.
+    int k_at[4], v_at[8];
+    {
+        const int vrow = 4 * (lane >> 4) + ((lane & 15) >> 2);
+#pragma unroll
+        for (int c = 0; c < 4; ++c) k_at[c] = kw * W::kTiles * 8192 + (lane & 15) * 256 + ((4 * c + (lane >> 4)) ^ (lane & 15)) * 16;
+#pragma unroll
+        for (int d = 0; d < 8; ++d)
+            v_at[d] = W::kKeys * 256 + kw * W::kTiles * 8192 + vrow * 256 + ((2 * d + ((lane & 3) >> 1)) ^ 2 * (vrow & 7)) * 16 + (lane & 1) * 8;
+    }
+    auto deposit = [&](au32x4* from, int stage, int buf) {
+        // Where some row does not see some key, values of V that are not finite count as zeros, and the rows that do see the key
+        // are told.
+        if (is_v && (mine + stage * ns) * W::kKeys + W::kKeys > open) {
+#pragma unroll
+            for (int k = 0; k < W::kRequests; ++k) {
+                bool ok = true;
+#pragma unroll
+                for (int w = 0; w < 4; ++w) ok = ok && finite_pair(from[k][w]);
+                const bool bad = ((uint32_t)(__ballot(!ok) >> (16 * (lane >> 4))) & 0xFFFFu) != 0;
+                if (bad) from[k] = au32x4{0u, 0u, 0u, 0u};
+                if ((lane & 15) == 0) bad_keys[buf * W::kKeys + my_tile * 32 + my_row + 4 * k] = bad;
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < W::kRequests; ++k) *(au32x4*)(wide_lds + buf * W::kBuffer + to_lds[k]) = from[k];
+    };
+    auto work = [&](int key0, int at) {  // the wave's keys of a stage, from key0; `at`: the buffer's place in LDS
+        constexpr int T = W::kTiles;
+        f32x4 x[T][2][2];  // by tile, row tile, half tile
+#pragma unroll
+        for (int t = 0; t < T; ++t)
+#pragma unroll
+            for (int c = 0; c < 4; ++c)
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    const bf16x8 k = *(const bf16x8*)(wide_lds + k_at[c] + at + t * 8192 + i * 4096);
+#pragma unroll
+                    for (int r = 0; r < 2; ++r)
+                        x[t][r][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, q[r][c], c ? x[t][r][i] : f32x4{0.0f, 0.0f, 0.0f, 0.0f}, 0, 0, 0);
+                }
+        if (key0 + 32 * T > open) {
+#pragma unroll
+            for (int t = 0; t < T; ++t)
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    const uint32_t bad = *(const uint32_t*)(bad_keys + at / W::kBuffer * W::kKeys + 32 * (T * kw + t) + 16 * i + 4 * (lane >> 4));
+#pragma unroll
+                    for (int r = 0; r < 2; ++r)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            const int key = key0 + 32 * t + 16 * i + 4 * (lane >> 4) + e;
+                            bool see = key < n;
+                            if (MASK == kSeeCausal) see = key <= n - a.n_q + token[r];
+                            if (MASK == kSeeTree) {
+                                const int j = key - (n - a.n_q);
+                                if (see && j >= 0) see = (a.seen[((int64_t)s * a.n_q + token[r]) * a.words + (j >> 5)] >> (j & 31)) & 1u;
+                            }
+                            x[t][r][i][e] = see ? ((bad >> (8 * e)) & 1u ? __builtin_nanf("") : x[t][r][i][e]) : -__builtin_inff();
+                        }
+                }
+        }
+        if (KEEP) {
+#pragma unroll
+            for (int r = 0; r < 2; ++r) {
+                const int row = row0 + r * kTileRows + (lane & 15);
+                float* to = a.logits + (((int64_t)layer * a.h_kv + g) * a.rows + row) * a.logit_T + logit_at(a.cu_seq, s) + key0 + 4 * (lane >> 4);
+#pragma unroll
+                for (int t = 0; t < T; ++t)
+                    if (row < a.rows && key0 + 32 * t < n) {
+                        *(f32x4*)(to + 32 * t) = x[t][r][0] * a.scale2;
+                        *(f32x4*)(to + 32 * t + 16) = x[t][r][1] * a.scale2;
+                    }
+            }
+        }
+        float top[2];
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
+            top[r] = fmaxf(max4(x[0][r][0]), max4(x[0][r][1]));
+#pragma unroll
+            for (int t = 1; t < T; ++t) top[r] = fmaxf(top[r], fmaxf(max4(x[t][r][0]), max4(x[t][r][1])));
+            top[r] *= a.scale2;
+        }
+        if (__any(top[0] > m[0] + kSlack || top[1] > m[1] + kSlack)) {
+#pragma unroll
+            for (int r = 0; r < 2; ++r) {
+                float to = fmaxf(top[r], __shfl_xor(top[r], 16));
+                to = fmaxf(m[r], fmaxf(to, __shfl_xor(to, 32)));
+                const float f = m[r] == to ? 1.0f : __builtin_amdgcn_exp2f(m[r] - to);
+                m[r] = to;
+                z[r] *= f;
+#pragma unroll
+                for (int d = 0; d < 8; ++d) o[r][d] *= f;
+            }
+        }
+        float mm[2];
+#pragma unroll
+        for (int r = 0; r < 2; ++r) mm[r] = m[r] == -__builtin_inff() ? 0.0f : m[r];
+#pragma unroll
+        for (int t = 0; t < T; ++t) {
+            bf16x8 p[2], rest[2];
+#pragma unroll
+            for (int r = 0; r < 2; ++r)
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const float y = __builtin_amdgcn_exp2f(__builtin_fmaf(x[t][r][i][e], a.scale2, -mm[r]));
+                        z[r] += y;
+                        p[r][4 * i + e] = (__bf16)y;
+                        if (W::kExact) rest[r][4 * i + e] = (__bf16)(y - (float)p[r][4 * i + e]);
+                    }
+#pragma unroll
+            for (int d = 0; d < 8; ++d) {
+                s16x4 v[2];
+#pragma unroll
+                for (int i = 0; i < 2; ++i) v[i] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)(wide_lds + v_at[d] + at + t * 8192 + i * 4096));
+                const bf16x8 vt = __builtin_bit_cast(bf16x8, __builtin_shufflevector(v[0], v[1], 0, 1, 2, 3, 4, 5, 6, 7));
+#pragma unroll
+                for (int r = 0; r < 2; ++r) o[r][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vt, p[r], o[r][d], 0, 0, 0);
+                if (W::kExact) {
+#pragma unroll
+                    for (int r = 0; r < 2; ++r) o[r][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vt, rest[r], o[r][d], 0, 0, 0);
+                }
+            }
+        }
+    };
+    // Stages are dealt to the sequence's workgroups in turn; those with keys that not every row sees come last.
+    const int stages = (n + W::kKeys - 1) / W::kKeys, n_mine = stages > mine ? (stages - mine - 1) / ns + 1 : 0;
+    if (n_mine > 0) {
+        au32x4 ahead[W::kAhead][W::kRequests];
+#pragma unroll
+        for (int i = 0; i < W::kAhead; ++i) request(ahead[i], i);
+        for (int i0 = 0; i0 < n_mine; i0 += 2) {
+#pragma unroll
+            for (int buf = 0; buf < 2; ++buf) {
+                const int i = i0 + buf;
+                if (i >= n_mine) break;  // (uniform)
+                deposit(ahead[buf % W::kAhead], i, buf);
+                request(ahead[buf % W::kAhead], i + W::kAhead);
+                lds_barrier();
+                const int key0 = (mine + i * ns) * W::kKeys + 32 * W::kTiles * kw;
+                if (key0 < n) work(key0, buf * W::kBuffer);
+            }
+        }
+    }
+
+#pragma unroll
+    for (int r = 0; r < 2; ++r) {
+        z[r] += __shfl_xor(z[r], 16);
+        z[r] += __shfl_xor(z[r], 32);
+    }
+    const int64_t part_row = (((int64_t)layer * a.n_splits + split) * a.h_kv + g) * a.rows;
+    if (KW > 1) {  // the waves over other keys of the same rows
+        float* sums = (float*)wide_lds;                                         // [kWaves - R][32][kOutStride]
+        float2* stats = (float2*)(sums + (W::kWaves - R) * 32 * kOutStride);    // [kWaves - R][32]
+        __syncthreads();
+        if (kw > 0) {
+#pragma unroll
+            for (int r = 0; r < 2; ++r) {
+                const int at = (wave - R) * 32 + r * kTileRows + (lane & 15);
+                if (lane < 16) stats[at] = make_float2(m[r], z[r]);
+#pragma unroll
+                for (int d = 0; d < 8; ++d) *(f32x4*)(sums + at * kOutStride + 4 * (lane >> 4) + 16 * d) = o[r][d];
+            }
+        }
+        __syncthreads();
+        if (kw > 0) return;
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
+            const float mine_m = m[r];
+#pragma unroll
+            for (int w = 0; w < KW - 1; ++w) m[r] = fmaxf(m[r], stats[(w * R + rw) * 32 + r * kTileRows + (lane & 15)].x);
+            float f = mine_m == m[r] ? 1.0f : __builtin_amdgcn_exp2f(mine_m - m[r]);
+            z[r] *= f;
+#pragma unroll
+            for (int d = 0; d < 8; ++d) o[r][d] *= f;
+#pragma unroll
+            for (int w = 0; w < KW - 1; ++w) {
+                const int at = (w * R + rw) * 32 + r * kTileRows + (lane & 15);
+                const float2 mz = stats[at];
+                f = mz.x == m[r] ? 1.0f : __builtin_amdgcn_exp2f(mz.x - m[r]);
+                z[r] += mz.y * f;
+#pragma unroll
+                for (int d = 0; d < 8; ++d) o[r][d] += *(const f32x4*)(sums + at * kOutStride + 16 * d + 4 * (lane >> 4)) * f;
+            }
+        }
+    }
+#pragma unroll
+    for (int r = 0; r < 2; ++r) {
+        const int row = row0 + r * kTileRows + (lane & 15);
+        if (row >= a.rows) continue;
+        if (lane < 16 && (ns > 1 || KEEP)) a.stats[part_row + row] = make_float2(m[r], z[r]);
+#pragma unroll
+        for (int d = 0; d < 8; ++d) {
+            const int at = 16 * d + 4 * (lane >> 4);
+            if (ns == 1) store_out(a, layer, s, g, row, at, o[r][d], m[r], z[r]);
+            else *(f32x4*)(a.part + (part_row + row) * kHeadDim + at) = o[r][d];
         }
     }
 }
 
-// Joins the workgroups of every sequence that has several: out and lse of all query rows.  Eight rows a workgroup.
-constexpr int kJoinRows = 8;
-__global__ __launch_bounds__(kJoinRows * 32) void jq_attend_join_kernel(AttendArgs a) {
-    const int chunks = (a.rows + kJoinRows - 1) / kJoinRows;
-    const int unit = (int)blockIdx.x / chunks, row = ((int)blockIdx.x - unit * chunks) * kJoinRows + (int)(threadIdx.x >> 5);
-    const int s = unit / a.h_kv, g = unit - s * a.h_kv, layer = blockIdx.y, d = (threadIdx.x & 31) * 4;
-    const int first = a.cu_split[s], ns = a.cu_split[s + 1] - first;
-    if (ns == 1 || row >= a.rows) return;
-    const int64_t at = (((int64_t)layer * a.n_splits + first) * a.h_kv + g) * a.rows + row, step = (int64_t)a.h_kv * a.rows;
-    float m = -__builtin_inff(), z = 0.0f;
-    for (int i = 0; i < ns; ++i) m = fmaxf(m, a.stats[at + i * step].x);
-    f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
-    for (int i = 0; i < ns; ++i) {
-        const float2 mz = a.stats[at + i * step];
-        const float f = mz.x == m ? 1.0f : __builtin_amdgcn_exp2f(mz.x - m);
-        z += mz.y * f;
-        o += *(const f32x4*)(a.part + (at + i * step) * kHeadDim + d) * f;
-    }
-    const int i = row / a.group, h = g * a.group + row - i * a.group;
-    const int64_t q_row = (((int64_t)layer * a.n_seq + s) * a.n_q + i) * a.h_q + h;
-    const float inv = z == 0.0f ? 0.0f : 1.0f / z;
-    __bf16 y[4];
+// A row's statistics over the ns shares of its sequence, a lane a share: (m, z) in every lane, and the lane's own factor (of share
+// `lane`; those of further shares are formed where they are needed).
+__device__ __forceinline__ float2 merge_stats(const float2* from, int64_t step, int ns, int lane, float* factor) {
+    const float2 own = lane < ns ? from[lane * step] : make_float2(-__builtin_inff(), 0.0f);
+    float m = own.x;
+    for (int i = lane + 64; i < ns; i += 64) m = fmaxf(m, from[i * step].x);
 #pragma unroll
-    for (int e = 0; e < 4; ++e) y[e] = (__bf16)(o[e] * inv);
-    *(uint2*)(a.out + q_row * kHeadDim + d) = *(const uint2*)y;
-    if (a.lse && d == 0) a.lse[q_row] = z == 0.0f ? -__builtin_inff() : (m + __builtin_amdgcn_logf(z)) * 0.69314718055994531f;
+    for (int d = 32; d; d >>= 1) m = fmaxf(m, __shfl_xor(m, d));
+    *factor = own.x == m ? 1.0f : __builtin_amdgcn_exp2f(own.x - m);
+    float z = own.y * *factor;
+    for (int i = lane + 64; i < ns; i += 64) {
+        const float2 mz = from[i * step];
+        z += mz.x == m ? mz.y : mz.y * __builtin_amdgcn_exp2f(mz.x - m);
+    }
+#pragma unroll
+    for (int d = 32; d; d >>= 1) z += __shfl_xor(z, d);
+    return make_float2(m, z);
 }
 
-// weights[j] += sum_r p[r,j], from the logits that the sweep has kept: 1024 rows of the cache a workgroup.
+// Calls whose last workgroups would have too much to join or weigh: a second launch does it.  The first `joins` workgroups of a
+// layer take four (sequence, head, query row) each, a wave a row; the others 1024 rows of the cache of a (sequence, head).
 constexpr int kWeighKeys = 1024;
-__global__ __launch_bounds__(256) void jq_attend_weigh_kernel(AttendArgs a, int blocks_per_seq) {
+__global__ __launch_bounds__(kAttendThreads) void jq_attend_finish_kernel(AttendArgs a, int joins, int blocks_per_seq) {
     __shared__ float lse2[kMaxWeighRows];
-    const int b = (int)blockIdx.x % blocks_per_seq, unit = (int)blockIdx.x / blocks_per_seq;
-    const int s = unit / a.h_kv, g = unit - s * a.h_kv, layer = blockIdx.y;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), layer = blockIdx.y;
+    const int64_t step = (int64_t)a.h_kv * a.rows;
+    if ((int)blockIdx.x < joins) {
+        const int item = (int)blockIdx.x * kAttendWaves + wave;
+        if (item >= a.n_seq * a.h_kv * a.rows) return;
+        const int unit = item / a.rows, row = item - unit * a.rows, s = unit / a.h_kv, g = unit - s * a.h_kv;
+        const int first = a.cu_split[s], ns = a.cu_split[s + 1] - first;
+        if (ns == 1) return;
+        const int64_t at = (((int64_t)layer * a.n_splits + first) * a.h_kv + g) * a.rows + row;
+        // two shares at a time, 16 bytes a lane; the first sixteen are requested ahead of the statistics
+        const int half = lane >> 5, d = (lane & 31) * 4;
+        const float* part = a.part + at * kHeadDim + d;
+        constexpr int kFirst = 8;
+        f32x4 x[kFirst];
+#pragma unroll
+        for (int k = 0; k < kFirst; ++k) x[k] = *(const f32x4*)(part + min(half + 2 * k, ns - 1) * step * kHeadDim);
+        float factor;
+        const float2 mz = merge_stats(a.stats + at, step, ns, lane, &factor);
+        f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+        for (int k = 0; k < kFirst; ++k) {
+            const float f = __shfl(factor, half + 2 * k);
+            if (half + 2 * k < ns) o += x[k] * f;
+        }
+        for (int i0 = 2 * kFirst; i0 < ns; i0 += 2 * kFirst) {
+#pragma unroll
+            for (int k = 0; k < kFirst; ++k) x[k] = *(const f32x4*)(part + min(i0 + half + 2 * k, ns - 1) * step * kHeadDim);
+#pragma unroll
+            for (int k = 0; k < kFirst; ++k) {
+                const int i = i0 + half + 2 * k;
+                float f = __shfl(factor, i & 63);
+                if (i >= 64) {
+                    const float mi = a.stats[at + min(i, ns - 1) * step].x;
+                    f = mi == mz.x ? 1.0f : __builtin_amdgcn_exp2f(mi - mz.x);
+                }
+                if (i < ns) o += x[k] * f;
+            }
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[e] += __shfl_xor(o[e], 32);
+        if (lane < 32) store_out(a, layer, s, g, row, d, o, mz.x, mz.y);
+        return;
+    }
+    const int b = ((int)blockIdx.x - joins) % blocks_per_seq, unit = ((int)blockIdx.x - joins) / blocks_per_seq;
+    const int s = unit / a.h_kv, g = unit - s * a.h_kv;
     const int n = live_rows(a.lens, a.n_seq, layer, s, a.cu_seq[s + 1] - a.cu_seq[s]);
     if (b * kWeighKeys >= n) return;
     const int first = a.cu_split[s], ns = a.cu_split[s + 1] - first;
-    const int64_t at = (((int64_t)layer * a.n_splits + first) * a.h_kv + g) * a.rows, step = (int64_t)a.h_kv * a.rows;
-    if ((int)threadIdx.x < a.rows) {
-        float m = -__builtin_inff(), z = 0.0f;
-        for (int i = 0; i < ns; ++i) m = fmaxf(m, a.stats[at + threadIdx.x + i * step].x);
-        for (int i = 0; i < ns; ++i) {
-            const float2 mz = a.stats[at + threadIdx.x + i * step];
-            z += mz.x == m ? mz.y : mz.y * __builtin_amdgcn_exp2f(mz.x - m);
-        }
-        lse2[threadIdx.x] = z == 0.0f ? 0.0f : m + __builtin_amdgcn_logf(z);  // nothing seen: all its logits are -inf
+    if (ns == 1 && a.hold_keys) return;  // weighed by the workgroup that swept it
+    const int64_t at = (((int64_t)layer * a.n_splits + first) * a.h_kv + g) * a.rows;
+    for (int r = wave; r < a.rows; r += kAttendWaves) {
+        float factor;
+        const float2 mz = merge_stats(a.stats + at + r, step, ns, lane, &factor);
+        if (lane == 0) lse2[r] = mz.y == 0.0f ? 0.0f : mz.x + log2_of(mz.y);  // nothing seen: all its logits are -inf
     }
     __syncthreads();
-    const float* x = a.logits + ((int64_t)layer * a.h_kv + g) * a.rows * a.logit_T + logit_at(a.cu_seq, s);
-    float* w = a.weights + ((int64_t)layer * a.h_kv + g) * a.T + a.cu_seq[s];
-    for (int j = b * kWeighKeys + threadIdx.x; j < min((b + 1) * kWeighKeys, n); j += 256) {
-        float sum = 0.0f;
-        for (int r = 0; r < a.rows; ++r) sum += __builtin_amdgcn_exp2f(x[r * a.logit_T + j] - lse2[r]);
-        w[j] += sum;
-    }
+    add_weights(a, layer, s, g, lse2, b * kWeighKeys, min((b + 1) * kWeighKeys, n));
 }
 
 // ---- host ------------------------------------------------------------------------------------------------------------------
 
-// How many workgroups share each sequence: as many as make some two per CU over the whole call, none with fewer than 128 rows of
-// the cache to itself.
-static void plan_splits(const Plan& p, AttendPlan* ap) {
+// How many workgroups share each sequence: as many as make one per CU over the whole call, none with fewer than 128 rows of the
+// cache to itself.  More of them ask for no more bytes a second and leave more sums to join (us a call, workgroups 256 / 512 / 768):
+// one token over 131072 rows 100 / 109 / 106, 32 tokens behind four prompts of 52296 rows together 61 / 72 / 83, a tree of 64 over
+// 32832 rows 60 / 77 / 96.  Rounded up sequence by sequence, 256 workgroups' worth of rows became 288 for eight ragged sequences,
+// which two rounds of the chip took 63 us for; found by bisection, 47.
+constexpr int kChip = 256;
+constexpr int kMostSums = 160;       // sums of 128 dimensions that it adds up
+constexpr int kMostJoined = 64;      // shares of a sequence that its last workgroup joins: a lane each
+constexpr int64_t kMostWeighed = 16384;  // logits of a (sequence, head) that it weighs
+static void plan_splits(const Plan& p, bool weights, AttendPlan* ap) {
     const int row_tiles = (p.rows + kTileRows - 1) / kTileRows;
-    ap->row_tiles = row_tiles <= 1 ? 1 : 2;
+    ap->row_tiles = row_tiles <= 1 ? 1 : row_tiles <= 2 ? 2 : row_tiles <= 4 ? 4 : row_tiles <= 8 ? 8 : 16;
     ap->row_groups = (row_tiles + ap->row_tiles - 1) / ap->row_tiles;
-    const int64_t heads = (int64_t)p.n_layers * p.h_kv * ap->row_groups;
-    const int64_t rows_per = std::max<int64_t>(128, (p.T * heads + 511) / 512);
+    // The smallest share (in rows of the cache, whole tiles for every wave) that makes no more workgroups than there are CUs.
+    const int64_t heads = (int64_t)p.n_layers * p.h_kv * ap->row_groups, unit = 128;
+    auto workgroups = [&](int64_t share) {
+        int64_t n = 0;
+        for (int s = 0; s < p.n_seq; ++s) n += (p.tab.cu_seq[s + 1] - p.tab.cu_seq[s] + share - 1) / share;
+        return n * heads;
+    };
+    int64_t lo = 1, hi = (p.T + unit - 1) / unit;
+    if (weights && row_tiles <= 2) hi = std::min(hi, (int64_t)kMostHeld / (p.rows * 4) / unit);  // its logits have to fit the LDS that is theirs
+    while (lo < hi) {
+        const int64_t mid = (lo + hi) / 2;
+        if (workgroups(mid * unit) <= kChip) hi = mid; else lo = mid + 1;
+    }
+    const int64_t share = lo * unit;
     ap->cu_split[0] = 0;
+    int64_t most_L = 0, tiles = 0;
+    int32_t most_ns = 0;
     for (int s = 0; s < p.n_seq; ++s) {
         const int64_t L = p.tab.cu_seq[s + 1] - p.tab.cu_seq[s];
-        ap->cu_split[s + 1] = ap->cu_split[s] + (int32_t)((L + rows_per - 1) / rows_per);
+        const int32_t ns = (int32_t)((L + share - 1) / share);
+        ap->cu_split[s + 1] = ap->cu_split[s] + ns;
+        most_L = std::max(most_L, L);
+        most_ns = std::max(most_ns, ns);
+        tiles = std::max(tiles, ((L + 31) / 32 + 4 * ns - 1) / (4 * ns));  // of 32 keys, a wave
     }
+    ap->hold_keys = weights && row_tiles <= 2 ? (int32_t)(tiles * 32 * kAttendWaves) : 0;
+    ap->one_launch = row_tiles <= 2 && most_ns <= kMostJoined && most_ns * p.rows <= kMostSums && (!weights || most_ns == 1 || most_L * p.rows <= kMostWeighed);
+}
+
+// 40 bits that no other call of the process has, above 24 of zeros; never 0.
+static uint64_t next_tag() {
+    static std::atomic<uint64_t> calls{0};
+    uint64_t x = (calls.fetch_add(1, std::memory_order_relaxed) + 1) * 0x9E3779B97F4A7C15ull;  // (odd: 64-bit numbers stay distinct)
+    x &= 0xFFFFFFFFFFull;
+    return (x ? x : 1) << 24;
 }
 
 void plan_attend(const Plan& p, bool weights, AttendPlan* ap) {
-    plan_splits(p, ap);
+    plan_splits(p, weights, ap);
     const size_t parts = (size_t)p.n_layers * ap->cu_split[p.n_seq] * p.h_kv * p.rows;
     auto up = [](size_t x) { return (x + 255) / 256 * 256; };
     ap->logit_T = 32 * (p.T / 32 + p.n_seq);
-    ap->off_stats = 0;
-    ap->off_part = up(parts * sizeof(float2));
+    ap->off_arrived = 0;
+    ap->off_stats = up((size_t)p.n_layers * p.n_seq * p.h_kv * ap->row_groups * sizeof(uint64_t));
+    ap->off_part = ap->off_stats + up(parts * sizeof(float2));
     ap->off_logits = ap->off_part + up(parts * kHeadDim * sizeof(float));
     ap->ws_bytes = ap->off_logits + (weights ? up((size_t)p.n_layers * p.h_kv * p.rows * ap->logit_T * sizeof(float)) : 0);
 }
 
 bool attend_fits(const Plan& p, const AttendPlan& ap) {
     const int64_t most = UINT32_MAX;
-    const int64_t sweep = ((int64_t)ap.cu_split[p.n_seq] * p.h_kv + 8) * ap.row_groups * kAttendThreads;
-    const int64_t join = (int64_t)p.n_seq * p.h_kv * ((p.rows + kJoinRows - 1) / kJoinRows) * (kJoinRows * 32);
-    return sweep <= most && join <= most;
+    const int64_t sweep = ((int64_t)ap.cu_split[p.n_seq] * p.h_kv + 8) * ap.row_groups * (ap.row_tiles > 2 ? 512 : 256);
+    const int64_t finish = ((int64_t)p.n_seq * p.h_kv * p.rows / kAttendWaves + 1 + (p.T / kWeighKeys + p.n_seq) * (int64_t)p.n_seq * p.h_kv) * kAttendThreads;
+    return sweep <= most && finish <= most;
 }
 
 template <int RT, int MASK, bool KEEP>
 static hipError_t launch_sweep(const AttendArgs& a, hipStream_t st) {
-    constexpr int lds = kAttendWaves * RT * kTileRows * (kOutStride * 4 + 8);
-    if (lds > 65536) {
+    constexpr int most = kAttendWaves * RT * kTileRows * (kOutStride * 4 + 8) + (KEEP ? kMostHeld : 0);
+    const int lds = kAttendWaves * RT * kTileRows * (kOutStride * 4 + 8) + (KEEP ? a.rows * a.hold_keys * 4 : 0);
+    if (most > 65536) {
         static std::atomic<uint64_t> done{0};
-        const hipError_t e = allow_dynamic_lds((const void*)jq_attend_kernel<RT, MASK, KEEP>, lds, done);
+        const hipError_t e = allow_dynamic_lds((const void*)jq_attend_kernel<RT, MASK, KEEP>, most, done);
         if (e != hipSuccess) return e;
     }
     const dim3 grid((unsigned)((a.units + 7) / 8 * 8 * a.row_groups), (unsigned)a.n_layers);
     return launch_kernel(jq_attend_kernel<RT, MASK, KEEP>, grid, dim3(kAttendThreads), lds, st, nullptr, -1, a);
 }
 
+template <int R, int MASK, bool KEEP>
+static hipError_t launch_wide(const AttendArgs& a, hipStream_t st) {
+    constexpr int lds = Wide<R>::kLds;
+    if (lds > 65536) {
+        static std::atomic<uint64_t> done{0};
+        const hipError_t e = allow_dynamic_lds((const void*)jq_attend_wide_kernel<R, MASK, KEEP>, lds, done);
+        if (e != hipSuccess) return e;
+    }
+    const dim3 grid((unsigned)((a.units + 7) / 8 * 8 * a.row_groups), (unsigned)a.n_layers);
+    return launch_kernel(jq_attend_wide_kernel<R, MASK, KEEP>, grid, dim3(Wide<R>::kThreads), lds, st, nullptr, -1, a);
+}
+
 template <int MASK, bool KEEP>
 static hipError_t launch_rows(const AttendArgs& a, int row_tiles, hipStream_t st) {
-    return row_tiles == 1 ? launch_sweep<1, MASK, KEEP>(a, st) : launch_sweep<2, MASK, KEEP>(a, st);
+    switch (row_tiles) {
+        case 1: return launch_sweep<1, MASK, KEEP>(a, st);
+        case 2: return launch_sweep<2, MASK, KEEP>(a, st);
+        case 4: return launch_wide<2, MASK, KEEP>(a, st);
+        case 8: return launch_wide<4, MASK, KEEP>(a, st);
+        default: return launch_wide<8, MASK, KEEP>(a, st);
+    }
 }
 
 hipError_t launch_attend(const Plan& p, const AttendPlan& ap, const int32_t* lens, const uint32_t* seen, const void* Q, const void* K, const void* V,
@@ -442,8 +995,11 @@ hipError_t launch_attend(const Plan& p, const AttendPlan& ap, const int32_t* len
     a.n_splits = ap.cu_split[p.n_seq];
     a.units = a.n_splits * p.h_kv;
     a.words = (p.n_q + 31) / 32;
+    a.hold_keys = ap.hold_keys;
     a.scale2 = (float)(p.scale * 1.4426950408889634);
     a.T = p.T; a.logit_T = ap.logit_T;
+    a.arrived = (uint64_t*)(ws + ap.off_arrived);
+    a.tag = ap.one_launch ? next_tag() : 0;
     a.pm = p.page_map();
     for (int s = 0; s <= p.n_seq; ++s) { a.cu_seq[s] = p.tab.cu_seq[s]; a.cu_split[s] = ap.cu_split[s]; }
     // one new token sees every live row, its own among them: no mask either way
@@ -452,18 +1008,12 @@ hipError_t launch_attend(const Plan& p, const AttendPlan& ap, const int32_t* len
     else if (p.window && p.n_q > 1) e = weights ? launch_rows<kSeeCausal, true>(a, ap.row_tiles, st) : launch_rows<kSeeCausal, false>(a, ap.row_tiles, st);
     else e = weights ? launch_rows<kSeeAll, true>(a, ap.row_tiles, st) : launch_rows<kSeeAll, false>(a, ap.row_tiles, st);
     if (e != hipSuccess) return e;
-    if (a.n_splits > p.n_seq) {
-        const dim3 grid((unsigned)(p.n_seq * p.h_kv * ((p.rows + kJoinRows - 1) / kJoinRows)), (unsigned)p.n_layers);
-        e = launch_kernel(jq_attend_join_kernel, grid, dim3(kJoinRows * 32), 0, st, nullptr, -1, a);
-        if (e != hipSuccess) return e;
-    }
-    if (weights) {
-        int32_t most = 0;
-        for (int s = 0; s < p.n_seq; ++s) most = std::max(most, p.tab.cu_seq[s + 1] - p.tab.cu_seq[s]);
-        const int blocks = (most + kWeighKeys - 1) / kWeighKeys;
-        e = launch_kernel(jq_attend_weigh_kernel, dim3((unsigned)(blocks * p.n_seq * p.h_kv), (unsigned)p.n_layers), dim3(256), 0, st, nullptr, -1, a, blocks);
-    }
-    return e;
+    if (a.tag || (a.n_splits == p.n_seq && !weights)) return e;
+    int32_t most = 0;
+    for (int s = 0; s < p.n_seq; ++s) most = std::max(most, p.tab.cu_seq[s + 1] - p.tab.cu_seq[s]);
+    const int joins = a.n_splits > p.n_seq ? (p.n_seq * p.h_kv * p.rows + kAttendWaves - 1) / kAttendWaves : 0, blocks = (most + kWeighKeys - 1) / kWeighKeys;
+    const dim3 grid((unsigned)(joins + (weights ? blocks * p.n_seq * p.h_kv : 0)), (unsigned)p.n_layers);
+    return launch_kernel(jq_attend_finish_kernel, grid, dim3(kAttendThreads), 0, st, nullptr, -1, a, joins, blocks);
 }
 
 }  // namespace jq

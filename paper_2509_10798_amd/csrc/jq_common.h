@@ -353,10 +353,12 @@ hipError_t launch_copy_probe(const void* src, void* dst, size_t bytes, hipStream
 // Decoding on a pruned cache (jq_attend.hip, jq_weight.hip).  How a call's sequences are shared out and where its workspace's pieces lie:
 constexpr int kMaxWeighRows = 128;  // most query rows per KV head whose weights are accumulated: their logits are kept until all sums are known
 struct AttendPlan {
+    int32_t hold_keys;                  // rows of the cache whose logits a workgroup holds, with weights
     int32_t row_tiles, row_groups;      // tiles of 16 query rows a workgroup takes, workgroups over the same keys
     int32_t cu_split[JQ_MAX_SEQ + 1];   // workgroups that share a sequence (per layer, KV head and group of rows), summed up
+    bool one_launch;                    // the workgroup that completes a sequence joins it (and weighs)
     int64_t logit_T;
-    size_t off_stats, off_part, off_logits, ws_bytes;
+    size_t off_arrived, off_stats, off_part, off_logits, ws_bytes;
 };
 void plan_attend(const Plan& p, bool weights, AttendPlan* ap);
 bool attend_fits(const Plan& p, const AttendPlan& ap);  // every launch stays below 2^32 threads

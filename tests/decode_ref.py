@@ -4,7 +4,9 @@ Bounds, counted in roundings (u = 2^-24, half a step of fp32; 2^-8 half a step o
   score     a sum of 128 products and a scaling: off by at most 132 u S, S = scale * sum |q| |k|; the running maximum and the
             exponent add 4 roundings of a number no larger than S + 16
   exp, sum  a term is off by twice that (exponent and normaliser) and a few u; a sum of n terms by n u more
-  out       probabilities are two bf16 parts, 2^-16 off, and out is rounded to bf16 once: 2^-8 |out| + (2^-16 + ...) sum p |v|
+  out       probabilities are two bf16 parts: the first is off by at most 2^-8 p, the second rounds that rest, 2^-8 of it, so 2^-16 p
+            are left; with more than 64 query rows per KV head they are the first part alone, 2^-8 p off.  out is a sum of p v, so off
+            by that share of sum p |v|, and rounded to bf16 once, 2^-8 |out|
 """
 import numpy as np
 
@@ -77,7 +79,8 @@ def attend_ref(q, k, v, see, scale):
         w[idx] += p
         score = 132 * U * S + 4 * U * (S + 16)
         term = 2 * score + (idx.size + 400) * U
-        tol_out[r] = 2.0 ** -8 * np.abs(out[r]) + (2.0 ** -16 + term) * (p @ np.abs(v[idx])) + 1e-38
+        part = 2.0 ** -16 if rows <= 64 else 2.0 ** -8
+        tol_out[r] = 2.0 ** -8 * np.abs(out[r]) + (part + term) * (p @ np.abs(v[idx])) + 1e-38
         tol_lse[r] = score + (idx.size + 400) * U + 4 * U * abs(lse[r])
         tol_w[idx] += term * p + 1e-37  # (exp flushes what is below 2^-126)
     return out, lse, w, tol_out, tol_lse, tol_w

@@ -152,14 +152,27 @@ def test_python_checks_come_first():
     sh = shape()
     with pytest.raises(jq.JQError):
         jq.attend_tree(sh, None, None, None, None)
-    q, k = torch.zeros((2, 2, 4, 8, 128), dtype=torch.bfloat16), torch.zeros((2, 164, 2, 128), dtype=torch.bfloat16)
-    with pytest.raises(ValueError, match="Q: "):
-        jq.attend(sh, q.float(), k, k)
-    with pytest.raises(ValueError, match="Q: "):
-        jq.attend(sh, q[:1], k, k)
-    with pytest.raises(ValueError, match="contiguous"):
-        jq.attend(sh, q.transpose(0, 1), k, k)
-    with pytest.raises(ValueError, match="lies on cpu"):
-        jq.attend(sh, q, k, k)
-    with pytest.raises(ValueError, match="K: "):
-        jq.evict_weight(sh, k[:, :10], k, None)
+    k = torch.zeros((2, 164, 2, 128), dtype=torch.bfloat16)
+    for call in (lambda: jq.attend(sh, k, k, k), lambda: jq.evict_weight(sh, k, k, None), lambda: jq.replace_lightest(sh, k, k, k, k, k, k, k)):
+        with pytest.raises(ValueError, match="lies on cpu"):
+            call()
+
+
+def test_tensor_checks():
+    """What every tensor of these calls is looked at for, on tensors of the host (GPU number -1)."""
+    import torch
+    from paper_2509_10798_amd.binding import _cache_size, _tensor
+    t = torch.zeros((4, 6), dtype=torch.int32)
+    assert _tensor("t", t, torch.int32, (4, 6), -1) == t.data_ptr() and _tensor("t", None, torch.int32, (4, 6), -1) is None
+    with pytest.raises(ValueError, match="t: .*float32.*is wanted"):
+        _tensor("t", t, torch.float32, (4, 6), -1)
+    with pytest.raises(ValueError, match=r"t: .*\(6, 4\) is wanted"):
+        _tensor("t", t, torch.int32, (6, 4), -1)
+    with pytest.raises(ValueError, match="not contiguous"):
+        _tensor("t", t.T, torch.int32, (6, 4), -1)
+    with pytest.raises(ValueError, match="lies on cpu, the call runs on GPU 0"):
+        _tensor("t", t, torch.int32, (4, 6), 0)
+    pg = jq.Pages(32, 6, None)
+    assert _cache_size(shape(), pg, torch.zeros(1, 1, 1, 1, 1)) == (2, 6, 32, 2, 128)
+    assert _cache_size(shape(), pg, torch.zeros(1, 1, 1, 1)) == (2, 192, 2, 128)      # rows numbered through
+    assert _cache_size(shape(), None, t) == (2, 164, 2, 128)
