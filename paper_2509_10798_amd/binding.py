@@ -512,7 +512,7 @@ def _call(name, shape: Shape, pages, device, stream, *args):
             _tensor("block_table", bt, torch.int32, (shape.n_seq, bt.shape[-1]), device)
         front += (ctypes.byref(pages.c_struct()),)
     if stream is None:
-        s = torch.cuda.current_stream(device).cuda_stream
+        s = torch._C._cuda_getCurrentRawStream(device)  # (torch.cuda.current_stream makes an object, 1 us)
     elif stream.device.index != device:
         raise ValueError("the stream belongs to %s, the cache lies on GPU %d" % (stream.device, device))
     else:

@@ -239,43 +239,60 @@ __device__ __forceinline__ void store_out(const AttendArgs& a, int layer, int s,
 }
 
 // weights[j] += sum_r 2^(x[r,j] - lse2[r]) for the rows j from `begin` to `end` of the cache, all threads of the workgroup together;
-// the logits may have been left by other workgroups of the launch.
-__device__ __forceinline__ void add_weights(const AttendArgs& a, int layer, int s, int g, const float* lse2, int begin, int end) {
-    const float* x = a.logits + ((int64_t)layer * a.h_kv + g) * a.rows * a.logit_T + logit_at(a.cu_seq, s);
-    float* w = a.weights + ((int64_t)layer * a.h_kv + g) * a.T + a.cu_seq[s];
-    constexpr int kPairs = 4;  // of rows, a thread: sixteen loads under way at a time
-    for (int j0 = begin + 2 * (int)threadIdx.x; j0 < end; j0 += 2 * kPairs * kAttendThreads) {
-        float2 sum[kPairs];
-#pragma unroll
-        for (int k = 0; k < kPairs; ++k) sum[k] = make_float2(0.0f, 0.0f);
-        for (int r0 = 0; r0 < a.rows; r0 += 4) {
-            float2 y[kPairs][4];
-#pragma unroll
-            for (int k = 0; k < kPairs; ++k)
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const int j = j0 + 2 * k * kAttendThreads;
-                    y[k][r] = get_pair(x + min(r0 + r, a.rows - 1) * a.logit_T + (j < end ? j : j0));
-                }
-#pragma unroll
-            for (int r = 0; r < 4; ++r)
-                if (r0 + r < a.rows) {
-                    const float l = lse2[r0 + r];
-#pragma unroll
-                    for (int k = 0; k < kPairs; ++k) {
-                        sum[k].x += __builtin_amdgcn_exp2f(y[k][r].x - l);
-                        sum[k].y += __builtin_amdgcn_exp2f(y[k][r].y - l);
-                    }
-                }
-        }
+// the logits may have been left by other workgroups of the launch.  A thread takes four pairs of rows at a time, so that sixteen
+// loads are under way; the first of them may have been requested earlier (request()).
+struct Weigher {
+    static constexpr int kPairs = 4;
+    const float* x;
+    float* w;
+    int64_t logit_T;
+    int rows, end, j0;
+    float2 y[kPairs][4], old[kPairs];
+
+    __device__ __forceinline__ Weigher(const AttendArgs& a, int layer, int s, int g, int begin, int end_)
+        : x(a.logits + ((int64_t)layer * a.h_kv + g) * a.rows * a.logit_T + logit_at(a.cu_seq, s)),
+          w(a.weights + ((int64_t)layer * a.h_kv + g) * a.T + a.cu_seq[s]), logit_T(a.logit_T), rows(a.rows), end(end_),
+          j0(begin + 2 * (int)threadIdx.x) {}
+    __device__ __forceinline__ int row(int k) const { return j0 + 2 * k * kAttendThreads; }
+    __device__ __forceinline__ void request(int r0) {
+        if (j0 >= end) return;
 #pragma unroll
         for (int k = 0; k < kPairs; ++k) {
-            const int j = j0 + 2 * k * kAttendThreads;
-            if (j < end) w[j] += sum[k].x;
-            if (j + 1 < end) w[j + 1] += sum[k].y;
+            const int j = row(k) < end ? row(k) : j0;
+#pragma unroll
+            for (int r = 0; r < 4; ++r) y[k][r] = get_pair(x + min(r0 + r, rows - 1) * logit_T + j);
+            if (r0 == 0) old[k] = make_float2(w[j], j + 1 < end ? w[j + 1] : 0.0f);
         }
     }
-}
+    __device__ __forceinline__ void add(const float* lse2, bool requested) {
+        for (; j0 < end; j0 += 2 * kPairs * kAttendThreads) {
+            float2 sum[kPairs];
+            for (int r0 = 0; r0 < rows; r0 += 4) {
+                if (!requested) request(r0);
+                requested = false;
+                if (r0 == 0) {
+#pragma unroll
+                    for (int k = 0; k < kPairs; ++k) sum[k] = make_float2(0.0f, 0.0f);
+                }
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+                    if (r0 + r < rows) {
+                        const float l = lse2[r0 + r];
+#pragma unroll
+                        for (int k = 0; k < kPairs; ++k) {
+                            sum[k].x += __builtin_amdgcn_exp2f(y[k][r].x - l);
+                            sum[k].y += __builtin_amdgcn_exp2f(y[k][r].y - l);
+                        }
+                    }
+            }
+#pragma unroll
+            for (int k = 0; k < kPairs; ++k) {
+                if (row(k) < end) w[row(k)] = old[k].x + sum[k].x;
+                if (row(k) + 1 < end) w[row(k) + 1] = old[k].y + sum[k].y;
+            }
+        }
+    }
+};
 
 template <int RT, int MASK, bool KEEP>
 __global__ __launch_bounds__(kAttendThreads, RT == 1 ? 3 : 2) void jq_attend_kernel(AttendArgs a) {
@@ -289,14 +306,7 @@ __global__ __launch_bounds__(kAttendThreads, RT == 1 ? 3 : 2) void jq_attend_ker
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
     const int s = seq_of_split(a, split, lane);
     const int ns = a.cu_split[s + 1] - a.cu_split[s], mine = split - a.cu_split[s];
-    const int n = live_rows(a.lens, a.n_seq, layer, s, a.cu_seq[s + 1] - a.cu_seq[s]);
     const int row0 = rg * RT * kTileRows;
-    // The sequence's count of finished workgroups starts at zero for this call: it holds the call's tag or is given it here.
-    uint64_t* arrived = a.arrived + (((int64_t)layer * a.n_seq + s) * a.h_kv + g) * a.row_groups + rg;
-    if (a.tag && ns > 1 && threadIdx.x == 0) {
-        uint64_t was = __hip_atomic_load(arrived, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-        if ((was ^ a.tag) >> 24) __hip_atomic_compare_exchange_strong(arrived, &was, a.tag, __ATOMIC_RELAXED, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    }
 
     RowState<RT> st;
     int row_limit[RT];
@@ -312,7 +322,7 @@ __global__ __launch_bounds__(kAttendThreads, RT == 1 ? 3 : 2) void jq_attend_ker
         for (int d = 0; d < 8; ++d) st.o[r][d] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
         st.m[r] = -__builtin_inff();
         st.z[r] = 0.0f;
-        row_limit[r] = n - a.n_q + i + 1;
+        row_limit[r] = i + 1;  // (and the rows in front of the queries' own, below)
         row_seen[r] = MASK == kSeeTree ? a.seen + ((int64_t)s * a.n_q + i) * a.words : nullptr;
     }
 
@@ -328,24 +338,38 @@ __global__ __launch_bounds__(kAttendThreads, RT == 1 ? 3 : 2) void jq_attend_ker
         if (!paged) return (uint32_t)key;
         return ((uint32_t)clamp_page(table[key >> shift], n_pages) << shift) + (uint32_t)(key & ((1 << shift) - 1));
     };
+    // The first tile is requested ahead of the live count, which only decides whether it matters: rows that are not live yet are
+    // the caller's too, and masked.
+    const int step = 32 * kAttendWaves * ns, cap = a.cu_seq[s + 1] - a.cu_seq[s];
+    int key = 32 * (kAttendWaves * mine + wave);
+    KvTile t;
+    if (key < cap) load_tile(t, K, V, tile_row(key), cap - 1 - key, stride, lane);
+    const int n = live_rows(a.lens, a.n_seq, layer, s, cap);
     // keys from `open` on are not seen by every row
     const int open = MASK == kSeeAll ? n : max(n - a.n_q + (MASK == kSeeCausal ? 1 : 0), 0);
-    const int step = 32 * kAttendWaves * ns;
-    int key = 32 * (kAttendWaves * mine + wave);
+#pragma unroll
+    for (int r = 0; r < RT; ++r) row_limit[r] += n - a.n_q;
+    // The sequence's count of finished workgroups starts at zero for this call: it holds the call's tag or is given it here.
+    uint64_t* arrived = a.arrived + (((int64_t)layer * a.n_seq + s) * a.h_kv + g) * a.row_groups + rg;
+    if (a.tag && ns > 1 && threadIdx.x == 0) {
+        uint64_t was = __hip_atomic_load(arrived, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        if ((was ^ a.tag) >> 24) __hip_atomic_compare_exchange_strong(arrived, &was, a.tag, __ATOMIC_RELAXED, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    }
     // With weights every row's logits stay in LDS until its sums are known, [rows][hold_keys], a wave's tiles four apart.  (Written
     // out as they are formed they kept reads from being under way: 32 sequences of 2048 rows 71.7 us a call, without weights 58.3.)
     float* held = (float*)(lds_stats + kAttendWaves * RT * kTileRows);
     float* hold = KEEP ? held + (lane & 15) * a.hold_keys + 32 * wave + 4 * (lane >> 4) : nullptr;
-    KvTile t;
-    for (; key + 32 <= open; key += step) {
-        load_tile(t, K, V, tile_row(key), 31, stride, lane);
+    while (key + 32 <= open) {
         tile_step<RT, false, MASK, KEEP>(st, t, a, lane, key, n, row_limit, row_seen, hold);
         if (KEEP) hold += 32 * kAttendWaves;
+        key += step;
+        if (key < n) load_tile(t, K, V, tile_row(key), n - 1 - key, stride, lane);
     }
-    for (; key < n; key += step) {
-        load_tile(t, K, V, tile_row(key), n - 1 - key, stride, lane);
+    while (key < n) {
         tile_step<RT, true, MASK, KEEP>(st, t, a, lane, key, n, row_limit, row_seen, hold);
         if (KEEP) hold += 32 * kAttendWaves;
+        key += step;
+        if (key < n) load_tile(t, K, V, tile_row(key), n - 1 - key, stride, lane);
     }
 
     // The four waves' sums, in wave order.
@@ -435,15 +459,35 @@ __global__ __launch_bounds__(kAttendThreads, RT == 1 ? 3 : 2) void jq_attend_ker
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __syncthreads();
     int* last = (int*)lds_stats;
-    if (ns > 1) {
-        if (threadIdx.x == 0) *last = (int)(__hip_atomic_fetch_add(arrived, 1ull, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) & 0xFFFFFF) + 1 == ns;
-        __syncthreads();
-        if (!*last) return;
-        if (threadIdx.x == 0) __hip_atomic_store(arrived, 0ull, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);  // a replay of the call counts from here
-    }
+    if (threadIdx.x == 0) *last = (int)(__hip_atomic_fetch_add(arrived, 1ull, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) & 0xFFFFFF) + 1 == ns;
+    __syncthreads();
+    if (!*last) return;
+    if (threadIdx.x == 0) __hip_atomic_store(arrived, 0ull, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);  // a replay of the call counts from here
+    // What the join begins with is requested together, statistics, sums and logits: each of them is a round trip past the caches.
+    // Sixteen bytes of output a thread; where there are few rows several threads take shares of the shares.
+    const int64_t first = (((int64_t)layer * a.n_splits + a.cu_split[s]) * a.h_kv + g) * a.rows + row0, next_share = (int64_t)a.h_kv * a.rows;
+    const int items = rows_here * 32;
+    int parts = 1;
+    while (2 * parts * items <= kAttendThreads && parts < 8) parts *= 2;
+    constexpr int kBatch = 8;
+    float2 lo[kBatch], hi[kBatch];
+    auto request = [&](int t, int i) {  // shares i, i + parts, ... of thread t's sums
+        const int item = t % items;
+        const float* from = a.part + (first + (item >> 5)) * kHeadDim + (item & 31) * 4;
+#pragma unroll
+        for (int k = 0; k < kBatch; ++k) {
+            const float* p = from + min(i + k * parts, ns - 1) * next_share * kHeadDim;
+            lo[k] = get_pair(p);
+            hi[k] = get_pair(p + 2);
+        }
+    };
+    request(threadIdx.x, (int)threadIdx.x / items);
+    Weigher weigher(a, layer, s, g, 0, n);
+    if (KEEP) weigher.request(0);
     // Factors of all shares' sums, [rows_here][ns], and the rows' (m, z).
     float* factor = lds;
-    const int64_t first = (((int64_t)layer * a.n_splits + a.cu_split[s]) * a.h_kv + g) * a.rows + row0, next_share = (int64_t)a.h_kv * a.rows;
+    float* sums = factor + rows_here * ns;  // [parts][items] outputs of four
+    float* lse2 = (float*)(lds_stats + rows_here);
     __syncthreads();
     for (int r = wave; r < rows_here; r += kAttendWaves) {  // a wave a row, a lane a share (there are 64 at most)
         const float2 mz = lane < ns ? get_pair((const float*)(a.stats + first + r + lane * next_share)) : make_float2(-__builtin_inff(), 0.0f);
@@ -455,53 +499,34 @@ __global__ __launch_bounds__(kAttendThreads, RT == 1 ? 3 : 2) void jq_attend_ker
 #pragma unroll
         for (int d = 32; d; d >>= 1) z += __shfl_xor(z, d);
         if (lane < ns) factor[r * ns + lane] = f;
-        if (lane == 0) lds_stats[r] = make_float2(m, z);
+        if (lane == 0) {
+            lds_stats[r] = make_float2(m, z);
+            lse2[r] = z == 0.0f ? 0.0f : m + log2_of(z);  // nothing seen: all its logits are -inf
+        }
     }
     __syncthreads();
-    if (ns > 1) {
-        // Sixteen bytes of output a thread; where there are few rows several threads take shares of the shares.
-        const int items = rows_here * 32;
-        int parts = 1;
-        while (2 * parts * items <= kAttendThreads && parts < 8) parts *= 2;
-        float* sums = factor + rows_here * ns;  // [parts][items] outputs of four
-        for (int t0 = 0; t0 < items * parts; t0 += kAttendThreads) {
-            const int t = t0 + threadIdx.x, part = t / items, item = t - part * items, r = item >> 5, d = (item & 31) * 4;
-            f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
-            if (part < parts) {
-                const float* from = a.part + (first + r) * kHeadDim + d;
-                for (int i = part; i < ns; i += 8 * parts) {
-                    float2 lo[8], hi[8];
+    for (int t0 = 0; t0 < items * parts; t0 += kAttendThreads) {
+        const int t = t0 + threadIdx.x, part = t / items, item = t - part * items, r = item >> 5, d = (item & 31) * 4;
+        f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
+        if (part < parts) {
+            for (int i = part; i < ns; i += kBatch * parts) {
+                if (t0 > 0 || i > part) request(t, i);
 #pragma unroll
-                    for (int k = 0; k < 8; ++k) {
-                        const float* p = from + min(i + k * parts, ns - 1) * next_share * kHeadDim;
-                        lo[k] = get_pair(p);
-                        hi[k] = get_pair(p + 2);
-                    }
-#pragma unroll
-                    for (int k = 0; k < 8; ++k) {
-                        const float f = i + k * parts < ns ? factor[r * ns + i + k * parts] : 0.0f;
-                        o += f32x4{lo[k].x, lo[k].y, hi[k].x, hi[k].y} * f;
-                    }
+                for (int k = 0; k < kBatch; ++k) {
+                    const float f = i + k * parts < ns ? factor[r * ns + i + k * parts] : 0.0f;
+                    o += f32x4{lo[k].x, lo[k].y, hi[k].x, hi[k].y} * f;
                 }
             }
-            if (parts > 1) {
-                if (part < parts) *(f32x4*)(sums + 4 * t) = o;
-                __syncthreads();
-                if (part == 0)
-                    for (int k = 1; k < parts; ++k) o += *(const f32x4*)(sums + 4 * (k * items + item));
-            }
-            if (part == 0) store_out(a, layer, s, g, row0 + r, d, o, lds_stats[r].x, lds_stats[r].y);
         }
-    }
-    if (KEEP) {
-        __syncthreads();
-        if ((int)threadIdx.x < rows_here) {
-            const float2 mz = lds_stats[threadIdx.x];
-            ((float*)(lds_stats + rows_here))[threadIdx.x] = mz.y == 0.0f ? 0.0f : mz.x + log2_of(mz.y);
+        if (parts > 1) {
+            if (part < parts) *(f32x4*)(sums + 4 * t) = o;
+            __syncthreads();
+            if (part == 0)
+                for (int k = 1; k < parts; ++k) o += *(const f32x4*)(sums + 4 * (k * items + item));
         }
-        __syncthreads();
-        add_weights(a, layer, s, g, (const float*)(lds_stats + rows_here), 0, n);
+        if (part == 0) store_out(a, layer, s, g, row0 + r, d, o, lds_stats[r].x, lds_stats[r].y);
     }
+    if (KEEP) weigher.add(lse2, true);
 }
 
 // Many query rows (more than 32 a KV head).  A wave still holds 32 of them, but the waves of a workgroup share the keys: R waves over
@@ -540,7 +565,7 @@ __global__ __launch_bounds__(Wide<R>::kThreads, 2) void jq_attend_wide_kernel(At
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
     const int s = seq_of_split(a, split, lane);
     const int ns = a.cu_split[s + 1] - a.cu_split[s], mine = split - a.cu_split[s];
-    const int n = live_rows(a.lens, a.n_seq, layer, s, a.cu_seq[s + 1] - a.cu_seq[s]);
+    const int cap = a.cu_seq[s + 1] - a.cu_seq[s];
     const int rw = wave % R, kw = wave / R;
     const int row0 = rg * W::kRows + 32 * rw;
 
@@ -567,7 +592,6 @@ __global__ __launch_bounds__(Wide<R>::kThreads, 2) void jq_attend_wide_kernel(At
     const_i32_ptr table = (const_i32_ptr)(a.pm.block_table ? a.pm.block_table + (int64_t)s * a.pm.max_pages : nullptr);
     const int shift = a.pm.page_shift, n_pages = a.pm.n_pages;
     const bool paged = a.pm.block_table != nullptr;
-    const int open = MASK == kSeeAll ? n : max(n - a.n_q + (MASK == kSeeCausal ? 1 : 0), 0);
 
     // This wave's requests of a stage: kRequests times four rows of K or of V, all in one tile of 32 keys.
     constexpr int kPerTile = 8 / W::kRequests;  // waves that share the requests of a tile
@@ -582,14 +606,20 @@ __global__ __launch_bounds__(Wide<R>::kThreads, 2) void jq_attend_wide_kernel(At
         const int row = my_row + 4 * i, piece = is_v ? (lane & 15) ^ 2 * (row & 7) : (lane & 15) ^ (row & 15);
         to_lds[i] = (is_v ? W::kKeys * 256 : 0) + (my_tile * 32 + row) * 256 + piece * 16;
     }
-    auto request = [&](au32x4* to, int stage) {
+    auto request = [&](au32x4* to, int stage, int rows) {  // `rows`: those that may be read
         int key = (mine + stage * ns) * W::kKeys + 32 * my_tile;
-        key = min(key, (n - 1) & ~31);  // (a stage may reach past the last tile)
-        const int last = n - 1 - key;
+        key = min(key, (rows - 1) & ~31);  // (a stage may reach past the last tile)
+        const int last = rows - 1 - key;
         const uint32_t row0 = !paged ? (uint32_t)key : ((uint32_t)clamp_page(table[key >> shift], n_pages) << shift) + (uint32_t)(key & ((1 << shift) - 1));
 #pragma unroll
         for (int i = 0; i < W::kRequests; ++i) to[i] = *(const au32x4*)(base + (row0 + (uint32_t)min(my_row + 4 * i, last)) * stride);
     };
+    // (The first stages are requested ahead of the live count: rows that are not live yet are the caller's too, and masked.)
+    au32x4 ahead[W::kAhead][W::kRequests];
+#pragma unroll
+    for (int i = 0; i < W::kAhead; ++i) request(ahead[i], i, cap);
+    const int n = live_rows(a.lens, a.n_seq, layer, s, cap);
+    const int open = MASK == kSeeAll ? n : max(n - a.n_q + (MASK == kSeeCausal ? 1 : 0), 0);
     // Addresses of a wave's reads in buffer 0: K by chunk of the dimensions (16 keys further on: + 4096), V by block of sixteen.
     int k_at[4], v_at[8];
     {
@@ -720,16 +750,13 @@ __global__ __launch_bounds__(Wide<R>::kThreads, 2) void jq_attend_wide_kernel(At
     // Stages are dealt to the sequence's workgroups in turn; those with keys that not every row sees come last.
     const int stages = (n + W::kKeys - 1) / W::kKeys, n_mine = stages > mine ? (stages - mine - 1) / ns + 1 : 0;
     if (n_mine > 0) {
-        au32x4 ahead[W::kAhead][W::kRequests];
-#pragma unroll
-        for (int i = 0; i < W::kAhead; ++i) request(ahead[i], i);
         for (int i0 = 0; i0 < n_mine; i0 += 2) {
 #pragma unroll
             for (int buf = 0; buf < 2; ++buf) {
                 const int i = i0 + buf;
                 if (i >= n_mine) break;  // (uniform)
                 deposit(ahead[buf % W::kAhead], i, buf);
-                request(ahead[buf % W::kAhead], i + W::kAhead);
+                request(ahead[buf % W::kAhead], i + W::kAhead, n);
                 lds_barrier();
                 const int key0 = (mine + i * ns) * W::kKeys + 32 * W::kTiles * kw;
                 if (key0 < n) work(key0, buf * W::kBuffer);
@@ -872,7 +899,7 @@ __global__ __launch_bounds__(kAttendThreads) void jq_attend_finish_kernel(Attend
         if (lane == 0) lse2[r] = mz.y == 0.0f ? 0.0f : mz.x + log2_of(mz.y);  // nothing seen: all its logits are -inf
     }
     __syncthreads();
-    add_weights(a, layer, s, g, lse2, b * kWeighKeys, min((b + 1) * kWeighKeys, n));
+    Weigher(a, layer, s, g, b * kWeighKeys, min((b + 1) * kWeighKeys, n)).add(lse2, false);
 }
 
 // ---- host ------------------------------------------------------------------------------------------------------------------

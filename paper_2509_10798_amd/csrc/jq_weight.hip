@@ -35,15 +35,48 @@ __device__ __forceinline__ uint32_t weight_key(float w, int pos, int keep_first,
     return pos < keep_first || pos > recent ? 0xFFFFFFFFu : sortable_key(w);
 }
 
-// One workgroup per (layer, sequence, KV head): exact radix select over the weights, four passes of eight bits, then the kept
-// rows in ascending order with their weights and positions.  Every slot written is at or before the row it comes from, and later
-// chunks read later rows only, so the weights and positions may be moved in place.
-constexpr int kWeightThreads = 1024;
+// One workgroup per (layer, sequence, KV head): exact radix select over the weights' keys, 11, 11 and 10 bits, then the kept rows
+// in ascending order with their weights and positions.  Each of the sixteen waves owns a run of rows, 256 of them (four a lane) a
+// round; up to ROUNDS rounds are held in registers, which the whole selection then works on, and longer runs are read again in every
+// pass, four rounds at a time.  A histogram has four copies, by lane, since most keys of a wave fall into a few bins of the first
+// level.  Places are counted wave by wave: the only barriers are those around a histogram and one around the waves' totals.
+// In place every slot written is at or before the row it comes from: what is held in registers has been read by then (one barrier),
+// and longer runs are moved by one wave after the other, each of its rounds read before it is written.
+constexpr int kWeightThreads = 1024, kWeightWaves = kWeightThreads / 64, kRoundRows = 256;
+constexpr int kWeightBins = 2048, kHistCopies = 4;
+typedef float any_float4 __attribute__((ext_vector_type(4), aligned(4)));
+typedef int32_t any_int4 __attribute__((ext_vector_type(4), aligned(4)));
+
+// Four rows' weights and positions.
+struct FourRows {
+    float w[4];
+    int32_t pos[4];
+    __device__ __forceinline__ void load(const float* from_w, const int32_t* from_pos, int j, int n) {
+        if (j + 4 <= n) {
+            *(any_float4*)w = *(const any_float4*)(from_w + j);
+            if (from_pos) *(any_int4*)pos = *(const any_int4*)(from_pos + j);
+        } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                w[e] = j + e < n ? from_w[j + e] : 0.0f;
+                if (from_pos) pos[e] = j + e < n ? from_pos[j + e] : 0;
+            }
+        }
+        if (!from_pos) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) pos[e] = j + e;
+        }
+    }
+};
+
+template <int ROUNDS, bool HELD>
 __global__ __launch_bounds__(kWeightThreads) void jq_weight_select_kernel(WeightArgs a) {
-    __shared__ uint32_t hist[256];
-    __shared__ uint32_t scan[kWeightThreads / 64];
+    __shared__ uint32_t hist[kWeightBins * kHistCopies];
+    __shared__ uint32_t scan[kWeightWaves];
+    __shared__ uint2 totals[kWeightWaves];
     __shared__ uint32_t picked[2];
-    const int g = blockIdx.x, s = blockIdx.y, layer = blockIdx.z, tid = threadIdx.x;
+    const int g = blockIdx.x, s = blockIdx.y, layer = blockIdx.z, tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int cap = a.tab.cu_seq[s + 1] - a.tab.cu_seq[s];
     const int n = live_of(a.lens, a.tab.n_seq, layer, s, cap);
     const uint32_t B = budget_of(a.layer_budgets, a.tab, layer, s, a.keep_first + a.keep_last);
@@ -51,68 +84,137 @@ __global__ __launch_bounds__(kWeightThreads) void jq_weight_select_kernel(Weight
     const float* w = a.weights + row0;
     const int32_t* pos = a.pos ? a.pos + row0 : nullptr;
     int32_t* idx = a.idx + ((int64_t)layer * a.h_kv + g) * a.TB + a.tab.cu_bud[s];
+    const int rounds = (n + kWeightWaves * kRoundRows - 1) / (kWeightWaves * kRoundRows);  // of a wave
+    const int first = wave * rounds * kRoundRows + 4 * lane;
 
-    uint32_t tau = 0, ties = 0xFFFFFFFFu;  // every key above tau is kept, and the first `ties` rows of key tau
-    int64_t recent = INT64_MAX;
-    if ((uint32_t)n > B) {
-        int newest = INT32_MIN;
-        if (pos) {
-            for (int j = tid; j < n; j += kWeightThreads) newest = max(newest, pos[j]);
-            uint32_t top = wave_max((uint32_t)newest ^ 0x80000000u);
-            if ((tid & 63) == 0) scan[tid >> 6] = top;
-            __syncthreads();
-            top = 0;
-            for (int i = 0; i < kWeightThreads / 64; ++i) top = max(top, scan[i]);
-            newest = (int)(top ^ 0x80000000u);
-        } else {
-            newest = n - 1;
+    FourRows held[ROUNDS];
+    auto read = [&](int i0) {
+#pragma unroll
+        for (int i = 0; i < ROUNDS; ++i)
+            if (i0 + i < rounds) held[i].load(w, pos, first + (i0 + i) * kRoundRows, n);
+    };
+    auto visit = [&](auto f) {  // f(row, four rows from it) for every round of the wave
+        for (int i0 = 0; i0 < (HELD ? 1 : rounds); i0 += ROUNDS) {
+            if (!HELD) read(i0);
+#pragma unroll
+            for (int i = 0; i < ROUNDS; ++i)
+                if (i0 + i < rounds) f(first + (i0 + i) * kRoundRows, held[i]);
         }
-        recent = (int64_t)newest - a.keep_last;
+    };
+    if (HELD) read(0);
+    uint32_t tau = 0, ties = 0xFFFFFFFFu;  // every key above tau is kept, and the first `ties` rows of key tau
+    const bool all = (uint32_t)n <= B;
+    int64_t recent = INT64_MAX;
+    if (!all && a.keep_last > 0) {
+        int newest = INT32_MIN;
+        visit([&](int j, const FourRows& r) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (j + e < n) newest = max(newest, r.pos[e]);
+        });
+        const uint32_t top = wave_max((uint32_t)newest ^ 0x80000000u);
+        if (lane == 0) scan[wave] = top;
+        __syncthreads();
+        recent = (int64_t)(int)(wave_max(scan[lane & (kWeightWaves - 1)]) ^ 0x80000000u) - a.keep_last;
+    }
+    auto key = [&](const FourRows& r, int e) { return weight_key(r.w[e], r.pos[e], a.keep_first, recent); };
+    if (!all) {
         uint32_t left = B, prefix = 0, mask = 0;  // places left among the keys that agree with prefix under mask
-        for (int shift = 24; shift >= 0; shift -= 8) {
+#pragma unroll 1
+        for (int level = 0; level < 3; ++level) {
+            const int shift = level == 0 ? 21 : level == 1 ? 10 : 0;
+            const uint32_t bins = level == 2 ? 1024 : 2048;
             __syncthreads();
-            if (tid < 256) hist[tid] = 0;
+            for (int i = tid; i < kWeightBins * kHistCopies / 4; i += kWeightThreads) ((uint4*)hist)[i] = make_uint4(0u, 0u, 0u, 0u);
             __syncthreads();
-            for (int j = tid; j < n; j += kWeightThreads) {
-                const uint32_t k = weight_key(w[j], pos ? pos[j] : j, a.keep_first, recent);
-                if ((k & mask) == prefix) atomicAdd(&hist[(k >> shift) & 255u], 1u);
+            visit([&](int j, const FourRows& r) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const uint32_t k = key(r, e);
+                    if (j + e < n && (k & mask) == prefix) atomicAdd(&hist[((k >> shift) & (bins - 1)) * kHistCopies + (lane & (kHistCopies - 1))], 1u);
+                }
+            });
+            __syncthreads();
+            // two bins a thread, from the largest down: the one in which the running count passes `left`
+            uint32_t c[2];
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const uint4 h = ((const uint4*)hist)[kWeightBins - 1 - (2 * tid + e)];
+                c[e] = h.x + h.y + h.z + h.w;
             }
-            __syncthreads();
-            // bins from the largest down: the one in which the running count passes `left`
-            const uint32_t c = tid < 256 ? hist[255 - tid] : 0u;
             uint32_t total;
-            const uint32_t upto = block_scan_incl<kWeightThreads>(c, scan, &total);
-            if (tid < 256 && upto >= left && upto - c < left) {
-                picked[0] = 255 - tid;
-                picked[1] = left - (upto - c);
+            const uint32_t upto = block_scan_incl<kWeightThreads>(c[0] + c[1], scan, &total), before = upto - c[0] - c[1];
+            if (before < left && left <= upto) {
+                const bool upper = left <= before + c[0];
+                picked[0] = kWeightBins - 1 - (2 * tid + (upper ? 0 : 1));
+                picked[1] = left - before - (upper ? 0u : c[0]);
             }
             __syncthreads();
             prefix |= picked[0] << shift;
-            mask |= 255u << shift;
+            mask |= (bins - 1) << shift;
             left = picked[1];
         }
         tau = prefix;
         ties = left;
     }
-    uint32_t kept = 0, equal = 0;  // before the present chunk
-    for (int base = 0; base < n; base += kWeightThreads) {
-        const int j = base + tid;
-        const bool live = j < n;
-        const float x = live ? w[j] : 0.0f;
-        const int p = live ? (pos ? pos[j] : j) : 0;
-        const uint32_t k = live ? weight_key(x, p, a.keep_first, recent) : 0u;
-        const bool tie = live && k == tau;
-        uint32_t n_tie, n_kept;
-        const uint32_t tie_rank = equal + block_scan_incl<kWeightThreads>(tie ? 1u : 0u, scan, &n_tie);
-        const bool keep = live && ((uint32_t)n <= B || k > tau || (tie && tie_rank <= ties));
-        const uint32_t slot = kept + block_scan_incl<kWeightThreads>(keep ? 1u : 0u, scan, &n_kept) - 1;
-        if (keep) {
-            idx[slot] = j;
-            a.weights_out[row0 + slot] = x;
-            if (a.pos_out) a.pos_out[row0 + slot] = p;
+    // What every wave keeps for certain, and its ties.
+    uint32_t sure = 0, tied = 0;
+    visit([&](int j, const FourRows& r) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const uint32_t k = key(r, e);
+            sure += j + e < n && (all || k > tau);
+            tied += j + e < n && !all && k == tau;
         }
-        kept += n_kept;
-        equal += n_tie;
+    });
+    auto add = [](uint32_t x, uint32_t y) { return x + y; };
+    sure = (uint32_t)__builtin_amdgcn_readlane((int)wave_scan(sure, 0u, add), 63);
+    tied = (uint32_t)__builtin_amdgcn_readlane((int)wave_scan(tied, 0u, add), 63);
+    if (lane == 0) totals[wave] = make_uint2(sure, tied);
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // what is held has been read, by every wave
+    __syncthreads();
+    uint32_t sure_before = 0, ties_before = 0;
+#pragma unroll
+    for (int i = 0; i < kWeightWaves; ++i) {
+        const uint2 t = totals[i];
+        sure_before += i < wave ? t.x : 0u;
+        ties_before += i < wave ? t.y : 0u;
+    }
+    auto emit = [&](int j, const FourRows& r) {
+        uint32_t is_sure = 0, is_tie = 0;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const uint32_t k = key(r, e);
+            is_sure |= (uint32_t)(j + e < n && (all || k > tau)) << e;
+            is_tie |= (uint32_t)(j + e < n && !all && k == tau) << e;
+        }
+        const uint32_t mine = (uint32_t)__popc(is_sure) | (uint32_t)__popc(is_tie) << 16, upto = wave_scan(mine, 0u, add);
+        uint32_t s0 = sure_before + ((upto - mine) & 0xFFFFu), t0 = ties_before + ((upto - mine) >> 16);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const bool surely = is_sure >> e & 1u, tie = is_tie >> e & 1u;
+            const uint32_t slot = s0 + min(t0, ties);
+            if (surely || (tie && t0 < ties)) {
+                idx[slot] = j + e;
+                a.weights_out[row0 + slot] = r.w[e];
+                if (a.pos_out) a.pos_out[row0 + slot] = r.pos[e];
+            }
+            s0 += surely;
+            t0 += tie;
+        }
+        const uint32_t round = (uint32_t)__builtin_amdgcn_readlane((int)upto, 63);
+        sure_before += round & 0xFFFFu;
+        ties_before += round >> 16;
+    };
+    if (HELD || a.weights_out != a.weights) {
+        visit(emit);
+        return;
+    }
+    for (int turn = 0; turn < kWeightWaves; ++turn) {
+        // (a visit reads its next rounds before it writes into earlier rows only)
+        if (turn == wave) visit(emit);
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        __syncthreads();
     }
 }
 
@@ -178,39 +280,65 @@ struct ReplaceArgs {
     SeqTab tab;
 };
 
-// One workgroup per (layer, sequence, KV head): the row of least key (the lowest of equals) by a reduction, then the new row.
-constexpr int kReplaceThreads = 256;
+// One workgroup per (layer, sequence, KV head): the row of least key (the lowest of equals) by a reduction, then the new row.  What
+// it has to read is 8 bytes a row, so it waits more than it reads: four rows a lane and four requests at a time, the first of them
+// ahead of the live count, which only decides whether they matter (rows up to the capacity are the caller's).
+constexpr int kReplaceThreads = 256, kReplaceAhead = 4;
 __global__ __launch_bounds__(kReplaceThreads) void jq_replace_kernel(ReplaceArgs a) {
     __shared__ uint64_t least[kReplaceThreads / 64];
     const int g = blockIdx.x, s = blockIdx.y, layer = blockIdx.z, tid = threadIdx.x;
     const int cap = a.tab.cu_seq[s + 1] - a.tab.cu_seq[s];
-    const int n = live_of(a.lens, a.tab.n_seq, layer, s, cap);
     const int64_t row0 = ((int64_t)layer * a.h_kv + g) * a.T + a.tab.cu_seq[s];
-    const int token = a.token[s];
+    const float* w = a.weights + row0;
+    const int32_t* pos = a.pos + row0;
+    FourRows rows[kReplaceAhead];
+    auto read = [&](int base) {
+#pragma unroll
+        for (int i = 0; i < kReplaceAhead; ++i) {
+            const int j = base + (i * kReplaceThreads + tid) * 4;
+            if (j < cap) rows[i].load(w, pos, j, cap);
+        }
+    };
+    read(0);
+    // the new row: sixteen lanes for K, sixteen for V
+    const int part = tid & 15;
+    wu32x4 fresh;
+    if (tid < 32) {
+        const int64_t from = (((int64_t)layer * a.tab.n_seq + s) * a.h_kv + g) * (kHeadDim * 2) + part * 16;
+        fresh = *(const wu32x4*)((tid < 16 ? a.k_new : a.v_new) + from);
+    }
+    const int token = a.token[s], n = live_of(a.lens, a.tab.n_seq, layer, s, cap);
     int slot = n;  // room left: the next row
     if (n == cap) {
         const int64_t recent = (int64_t)token - a.keep_last;  // the new token counts among the newest
         uint64_t best = UINT64_MAX;
-        for (int j = tid; j < n; j += kReplaceThreads) {
-            const uint64_t k = (uint64_t)weight_key(a.weights[row0 + j], a.pos[row0 + j], a.keep_first, recent) << 32 | (uint32_t)j;
-            best = k < best ? k : best;
+        for (int base = 0; base < n; base += 4 * kReplaceAhead * kReplaceThreads) {
+            if (base > 0) read(base);
+#pragma unroll
+            for (int i = 0; i < kReplaceAhead; ++i) {
+                const int j = base + (i * kReplaceThreads + tid) * 4;
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (j + e < n) {
+                        const uint64_t k = (uint64_t)weight_key(rows[i].w[e], rows[i].pos[e], a.keep_first, recent) << 32 | (uint32_t)(j + e);
+                        best = k < best ? k : best;
+                    }
+            }
         }
-        for (int d = 32; d; d >>= 1) {
-            const uint64_t o = __shfl_xor((unsigned long long)best, d);
-            best = o < best ? o : best;
-        }
-        if ((tid & 63) == 0) least[tid >> 6] = best;
+        // the least key of the wave, then the lowest row that has it
+        const uint32_t key = (uint32_t)(best >> 32), top = wave_min(key), row = wave_min(key == top ? (uint32_t)best : 0xFFFFFFFFu);
+        if ((tid & 63) == 0) least[tid >> 6] = (uint64_t)top << 32 | row;
         __syncthreads();
-        for (int i = 0; i < kReplaceThreads / 64; ++i) best = least[i] < best ? least[i] : best;
+        best = least[0];
+#pragma unroll
+        for (int i = 1; i < kReplaceThreads / 64; ++i) best = least[i] < best ? least[i] : best;
         slot = (int)(uint32_t)best;
     }
-    if (tid < 32) {  // sixteen lanes for the row of K, sixteen for V's
-        const int part = tid & 15;
-        const int64_t from = (((int64_t)layer * a.tab.n_seq + s) * a.h_kv + g) * (kHeadDim * 2) + part * 16;
+    if (tid < 32) {
         const int64_t to = (kv_row(a.pm, a.tab.cu_seq, a.T, layer, s, slot) * a.h_kv + g) * (kHeadDim * 2) + part * 16;
-        *(wu32x4*)((tid < 16 ? a.K : a.V) + to) = *(const wu32x4*)((tid < 16 ? a.k_new : a.v_new) + from);
+        *(wu32x4*)((tid < 16 ? a.K : a.V) + to) = fresh;
     }
-    if (tid == 0) {
+    if (tid == 32) {
         a.weights[row0 + slot] = 0.0f;
         a.pos[row0 + slot] = token;
         if (a.slot) a.slot[((int64_t)layer * a.tab.n_seq + s) * a.h_kv + g] = slot;
@@ -227,8 +355,11 @@ hipError_t launch_evict_weight(const Plan& p, const int32_t* lens, const void* K
     a.layer_budgets = p.layer_budgets;
     a.n_layers = p.n_layers; a.h_kv = p.h_kv; a.keep_first = p.keep_first; a.keep_last = p.keep_last;
     a.T = p.T; a.TB = p.TB; a.pm = p.page_map(); a.tab = p.tab;
-    hipError_t e = launch_kernel(jq_weight_select_kernel, dim3((unsigned)p.h_kv, (unsigned)p.n_seq, (unsigned)p.n_layers), dim3(kWeightThreads), 0, st,
-                                 nullptr, -1, a);
+    int32_t most = 0;
+    for (int s = 0; s < p.n_seq; ++s) most = std::max(most, p.tab.cu_seq[s + 1] - p.tab.cu_seq[s]);
+    const int rounds = (most + kWeightWaves * kRoundRows - 1) / (kWeightWaves * kRoundRows);
+    const auto select = rounds <= 1 ? jq_weight_select_kernel<1, true> : rounds <= 4 ? jq_weight_select_kernel<4, true> : jq_weight_select_kernel<4, false>;
+    hipError_t e = launch_kernel(select, dim3((unsigned)p.h_kv, (unsigned)p.n_seq, (unsigned)p.n_layers), dim3(kWeightThreads), 0, st, nullptr, -1, a);
     if (e != hipSuccess) return e;
     if (K_out == K)
         return launch_kernel(jq_weight_shift_kernel, dim3((unsigned)(8 * p.h_kv), (unsigned)p.n_seq, (unsigned)p.n_layers), dim3(kMoveThreads), 0, st, nullptr, -1, a);
