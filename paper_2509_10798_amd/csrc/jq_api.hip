@@ -781,7 +781,9 @@ int jq_evict_weight_workspace_bytes(const jq_shape* shape, size_t* bytes) {
     Plan p;
     const int rc = make_plan(shape, true, &p, false);
     if (rc != JQ_OK) return rc;
-    *bytes = align_up(idx_bytes(p));
+    WeightPlan wp;
+    plan_evict_weight(p, &wp);
+    *bytes = wp.ws_bytes;
     return JQ_OK;
 }
 
@@ -795,7 +797,9 @@ static int evict_weight_impl(const jq_shape* shape, const jq_pages* pages, bool 
     if (paged && (rc = apply_pages(pages, &p)) != JQ_OK) return rc;
     if ((uint64_t)p.n_layers * p.TB * p.h_kv * 16 > UINT32_MAX) return JQ_ERR_UNSUPPORTED;
     if (!K || !V || !weights || !K_out || !V_out || !weights_out || (pos && !pos_out) || !ws) return JQ_ERR_NULL;
-    const size_t need = align_up(idx_bytes(p));
+    WeightPlan wp;
+    plan_evict_weight(p, &wp);
+    const size_t need = wp.ws_bytes;
     if (misaligned(ws, 16) || ws_bytes < need) return JQ_ERR_WORKSPACE;
     if (misaligned(K, 16) || misaligned(V, 16) || misaligned(K_out, 16) || misaligned(V_out, 16) || misaligned(weights, 4) || misaligned(weights_out, 4) ||
         (pos && misaligned(pos, 4)) || (pos_out && misaligned(pos_out, 4)) || (idx_out && misaligned(idx_out, 4)) || (lens && misaligned(lens, 4)))
@@ -807,8 +811,8 @@ static int evict_weight_impl(const jq_shape* shape, const jq_pages* pages, bool 
                         {inplace ? nullptr : V, nkv}, {inplace ? nullptr : weights, nw}, {inplace ? nullptr : pos, nw}};
     const Buf outs[6] = {{K_out, nkv}, {V_out, nkv}, {weights_out, nw}, {pos_out, nw}, {idx_out, idx_bytes(p)}, {ws, need}};
     if (any_overlap(outs, 6, ins, 7)) return JQ_ERR_ALIAS;
-    return launch_status(launch_evict_weight(p, lens, K, V, weights, pos, K_out, V_out, weights_out, pos_out, idx_out ? idx_out : (int32_t*)ws,
-                                             (hipStream_t)stream));
+    return launch_status(launch_evict_weight(p, wp, lens, K, V, weights, pos, K_out, V_out, weights_out, pos_out, idx_out ? idx_out : (int32_t*)ws,
+                                             (char*)ws, (hipStream_t)stream));
 }
 
 int jq_evict_weight(const jq_shape* shape, const int32_t* lens, const void* K, const void* V, const float* weights, const int32_t* pos, void* K_out,

@@ -366,8 +366,15 @@ bool attend_fits(const Plan& p, const AttendPlan& ap);  // every launch stays be
 hipError_t launch_attend(const Plan& p, const AttendPlan& ap, const int32_t* lens, const uint32_t* seen, const void* Q, const void* K, const void* V,
                          void* out, float* lse, float* weights, char* ws, hipStream_t st);
 // K_out == K (then V_out == V, weights_out == weights and pos_out == pos too): within one cache.  `idx` [n_layers][h_kv][TB] takes the kept rows.
-hipError_t launch_evict_weight(const Plan& p, const int32_t* lens, const void* K, const void* V, const float* weights, const int32_t* pos,
-                               void* K_out, void* V_out, float* weights_out, int32_t* pos_out, int32_t* idx, hipStream_t st);
+// `cu_piece`, `cu_cand`: pieces of the long sequences, rows that they leave, summed up (none: sequences are selected from whole).
+struct WeightPlan {
+    int32_t cu_piece[JQ_MAX_SEQ + 1], cu_cand[JQ_MAX_SEQ + 1];
+    int32_t most_rows;  // most rows that the (last) selection reads of a sequence
+    size_t off_newest, off_cand, ws_bytes;
+};
+void plan_evict_weight(const Plan& p, WeightPlan* wp);
+hipError_t launch_evict_weight(const Plan& p, const WeightPlan& wp, const int32_t* lens, const void* K, const void* V, const float* weights, const int32_t* pos,
+                               void* K_out, void* V_out, float* weights_out, int32_t* pos_out, int32_t* idx, char* ws, hipStream_t st);
 hipError_t launch_replace(const Plan& p, const int32_t* lens, const void* k_new, const void* v_new, const int32_t* token, void* K, void* V, float* weights,
                           int32_t* pos, int32_t* slot, hipStream_t st);
 

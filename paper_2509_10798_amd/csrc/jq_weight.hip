@@ -19,6 +19,12 @@ struct WeightArgs {
     const int32_t* pos; int32_t* pos_out;      // the same; pos null: a row's number is its position; pos_out may be null
     const int32_t* lens;                       // DEVICE [n_layers][n_seq] live rows, or null: all
     int32_t* idx;                              // [n_layers][h_kv][TB]
+    // long sequences, in pieces of kPieceRows rows: each piece's largest position [n_layers][h_kv][n_pieces], and the rows that its
+    // selection kept [n_layers][h_kv][n_cand] (weight, position, number), piece after piece
+    int32_t* newest;
+    float* cand_w; int32_t* cand_pos; int32_t* cand_row;
+    int32_t n_pieces, n_cand;
+    int32_t cu_piece[JQ_MAX_SEQ + 1], cu_cand[JQ_MAX_SEQ + 1];
     const int32_t* layer_budgets;
     int32_t n_layers, h_kv, keep_first, keep_last;
     int64_t T, TB;
@@ -51,7 +57,8 @@ typedef int32_t any_int4 __attribute__((ext_vector_type(4), aligned(4)));
 struct FourRows {
     float w[4];
     int32_t pos[4];
-    __device__ __forceinline__ void load(const float* from_w, const int32_t* from_pos, int j, int n) {
+    // the rows from j on, of which there are n; without positions they are the rows' numbers, `base` for the first
+    __device__ __forceinline__ void load(const float* from_w, const int32_t* from_pos, int j, int n, int base) {
         if (j + 4 <= n) {
             *(any_float4*)w = *(const any_float4*)(from_w + j);
             if (from_pos) *(any_int4*)pos = *(const any_int4*)(from_pos + j);
@@ -64,26 +71,79 @@ struct FourRows {
         }
         if (!from_pos) {
 #pragma unroll
-            for (int e = 0; e < 4; ++e) pos[e] = j + e;
+            for (int e = 0; e < 4; ++e) pos[e] = base + j + e;
         }
     }
 };
 
-template <int ROUNDS, bool HELD>
+// STAGE: a sequence of many times as many rows as it keeps is selected from twice, so that more than one workgroup reads it:
+// kPieces, its pieces of kPieceRows rows leave a budget's worth of rows each, and kRest, the budget's rows are chosen from those.
+// Whatever the sequence keeps, its piece keeps; pieces and rows stay in order, so equal weights still go to the lower row.
+enum WeightStage { kAllRows = 0, kPieces, kRest };
+constexpr int kPieceRows = 4 * kWeightWaves * kRoundRows;  // what a workgroup holds
+
+// The largest position of every piece.
+__global__ __launch_bounds__(kWeightThreads) void jq_weight_newest_kernel(WeightArgs a) {
+    __shared__ uint32_t most[kWeightWaves];
+    const int piece = (int)blockIdx.x / a.h_kv, g = (int)blockIdx.x - piece * a.h_kv, layer = blockIdx.y, tid = threadIdx.x;
+    const int s = find_seq(a.cu_piece, a.tab.n_seq, piece), base = (piece - a.cu_piece[s]) * kPieceRows;
+    const int n = min(live_of(a.lens, a.tab.n_seq, layer, s, a.tab.cu_seq[s + 1] - a.tab.cu_seq[s]) - base, kPieceRows);
+    const int32_t* pos = a.pos + ((int64_t)layer * a.h_kv + g) * a.T + a.tab.cu_seq[s] + base;
+    int newest = INT32_MIN;
+#pragma unroll 4
+    for (int j = tid; j < n; j += kWeightThreads) newest = max(newest, pos[j]);
+    const uint32_t top = wave_max((uint32_t)newest ^ 0x80000000u);
+    if ((tid & 63) == 0) most[tid >> 6] = top;
+    __syncthreads();
+    if (tid < 64) {
+        const uint32_t x = wave_max(most[tid & (kWeightWaves - 1)]);
+        if (tid == 0) a.newest[((int64_t)layer * a.h_kv + g) * a.n_pieces + piece] = (int32_t)(x ^ 0x80000000u);
+    }
+}
+
+template <int ROUNDS, bool HELD, int STAGE>
 __global__ __launch_bounds__(kWeightThreads) void jq_weight_select_kernel(WeightArgs a) {
     __shared__ uint32_t hist[kWeightBins * kHistCopies];
     __shared__ uint32_t scan[kWeightWaves];
     __shared__ uint2 totals[kWeightWaves];
-    __shared__ uint32_t picked[2];
-    const int g = blockIdx.x, s = blockIdx.y, layer = blockIdx.z, tid = threadIdx.x, lane = tid & 63;
+    __shared__ uint32_t picked[3];
+    const int unit = (int)blockIdx.x / a.h_kv, g = (int)blockIdx.x - unit * a.h_kv, layer = blockIdx.y, tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int s = STAGE == kPieces ? find_seq(a.cu_piece, a.tab.n_seq, unit) : unit;
     const int cap = a.tab.cu_seq[s + 1] - a.tab.cu_seq[s];
-    const int n = live_of(a.lens, a.tab.n_seq, layer, s, cap);
+    const int live = live_of(a.lens, a.tab.n_seq, layer, s, cap);
     const uint32_t B = budget_of(a.layer_budgets, a.tab, layer, s, a.keep_first + a.keep_last);
-    const int64_t row0 = ((int64_t)layer * a.h_kv + g) * a.T + a.tab.cu_seq[s];
+    const int64_t head = (int64_t)layer * a.h_kv + g, row0 = head * a.T + a.tab.cu_seq[s];
+    // where the rows come from, how many they are, and where those that are kept go
     const float* w = a.weights + row0;
     const int32_t* pos = a.pos ? a.pos + row0 : nullptr;
-    int32_t* idx = a.idx + ((int64_t)layer * a.h_kv + g) * a.TB + a.tab.cu_bud[s];
+    const int32_t* number = nullptr;  // the rows' numbers; null: 0, 1, ...
+    float* w_to = a.weights_out + row0;
+    int32_t* pos_to = a.pos_out ? a.pos_out + row0 : nullptr;
+    int32_t* number_to = a.idx + head * a.TB + a.tab.cu_bud[s];
+    int n = live, base = 0;
+    const int per_piece = (int)min((uint32_t)kPieceRows, B);  // rows that a whole piece leaves
+    const bool pieced = live > kPieceRows && (uint32_t)live > B;
+    if (STAGE == kPieces) {
+        if (!pieced) return;
+        const int piece = unit - a.cu_piece[s];
+        base = piece * kPieceRows;
+        n = min(live - base, kPieceRows);
+        if (n <= 0) return;
+        const int64_t to = head * a.n_cand + a.cu_cand[s] + (int64_t)piece * per_piece;
+        w += base;
+        if (pos) pos += base;
+        w_to = a.cand_w + to;
+        pos_to = a.cand_pos + to;
+        number_to = a.cand_row + to;
+    }
+    if (STAGE == kRest && pieced) {
+        const int64_t from = head * a.n_cand + a.cu_cand[s];
+        w = a.cand_w + from;
+        pos = a.cand_pos + from;
+        number = a.cand_row + from;
+        n = live / kPieceRows * per_piece + min(live % kPieceRows, per_piece);
+    }
     const int rounds = (n + kWeightWaves * kRoundRows - 1) / (kWeightWaves * kRoundRows);  // of a wave
     const int first = wave * rounds * kRoundRows + 4 * lane;
 
@@ -91,7 +151,7 @@ __global__ __launch_bounds__(kWeightThreads) void jq_weight_select_kernel(Weight
     auto read = [&](int i0) {
 #pragma unroll
         for (int i = 0; i < ROUNDS; ++i)
-            if (i0 + i < rounds) held[i].load(w, pos, first + (i0 + i) * kRoundRows, n);
+            if (i0 + i < rounds) held[i].load(w, pos, first + (i0 + i) * kRoundRows, n, base);
     };
     auto visit = [&](auto f) {  // f(row, four rows from it) for every round of the wave
         for (int i0 = 0; i0 < (HELD ? 1 : rounds); i0 += ROUNDS) {
@@ -105,7 +165,16 @@ __global__ __launch_bounds__(kWeightThreads) void jq_weight_select_kernel(Weight
     uint32_t tau = 0, ties = 0xFFFFFFFFu;  // every key above tau is kept, and the first `ties` rows of key tau
     const bool all = (uint32_t)n <= B;
     int64_t recent = INT64_MAX;
-    if (!all && a.keep_last > 0) {
+    if (!all && a.keep_last > 0 && STAGE != kAllRows && pieced) {
+        int newest = live - 1;
+        if (a.pos) {
+            newest = INT32_MIN;
+            const int pieces = (live + kPieceRows - 1) / kPieceRows;
+            for (int i = lane; i < pieces; i += 64) newest = max(newest, a.newest[head * a.n_pieces + a.cu_piece[s] + i]);
+            newest = (int)(wave_max((uint32_t)newest ^ 0x80000000u) ^ 0x80000000u);
+        }
+        recent = (int64_t)newest - a.keep_last;
+    } else if (!all && a.keep_last > 0) {
         int newest = INT32_MIN;
         visit([&](int j, const FourRows& r) {
 #pragma unroll
@@ -148,11 +217,17 @@ __global__ __launch_bounds__(kWeightThreads) void jq_weight_select_kernel(Weight
                 const bool upper = left <= before + c[0];
                 picked[0] = kWeightBins - 1 - (2 * tid + (upper ? 0 : 1));
                 picked[1] = left - before - (upper ? 0u : c[0]);
+                picked[2] = c[upper ? 0 : 1];
             }
             __syncthreads();
             prefix |= picked[0] << shift;
             mask |= (bins - 1) << shift;
             left = picked[1];
+            if (left == picked[2] && prefix) {  // the whole bin stays, as it mostly does from the second level on: it often holds one row
+                prefix -= 1;
+                left = 0;
+                break;
+            }
         }
         tau = prefix;
         ties = left;
@@ -195,9 +270,9 @@ __global__ __launch_bounds__(kWeightThreads) void jq_weight_select_kernel(Weight
             const bool surely = is_sure >> e & 1u, tie = is_tie >> e & 1u;
             const uint32_t slot = s0 + min(t0, ties);
             if (surely || (tie && t0 < ties)) {
-                idx[slot] = j + e;
-                a.weights_out[row0 + slot] = r.w[e];
-                if (a.pos_out) a.pos_out[row0 + slot] = r.pos[e];
+                number_to[slot] = number ? number[j + e] : base + j + e;
+                w_to[slot] = r.w[e];
+                if (pos_to) pos_to[slot] = r.pos[e];
             }
             s0 += surely;
             t0 += tie;
@@ -206,7 +281,7 @@ __global__ __launch_bounds__(kWeightThreads) void jq_weight_select_kernel(Weight
         sure_before += round & 0xFFFFu;
         ties_before += round >> 16;
     };
-    if (HELD || a.weights_out != a.weights) {
+    if (HELD || w_to != w) {
         visit(emit);
         return;
     }
@@ -296,7 +371,7 @@ __global__ __launch_bounds__(kReplaceThreads) void jq_replace_kernel(ReplaceArgs
 #pragma unroll
         for (int i = 0; i < kReplaceAhead; ++i) {
             const int j = base + (i * kReplaceThreads + tid) * 4;
-            if (j < cap) rows[i].load(w, pos, j, cap);
+            if (j < cap) rows[i].load(w, pos, j, cap, 0);
         }
     };
     read(0);
@@ -347,19 +422,64 @@ __global__ __launch_bounds__(kReplaceThreads) void jq_replace_kernel(ReplaceArgs
 
 // ---- host ------------------------------------------------------------------------------------------------------------------
 
-hipError_t launch_evict_weight(const Plan& p, const int32_t* lens, const void* K, const void* V, const float* weights, const int32_t* pos,
-                               void* K_out, void* V_out, float* weights_out, int32_t* pos_out, int32_t* idx, hipStream_t st) {
+// Pieces or not: with pieces the last selection reads pieces * budget rows of every long sequence instead of all.  They are taken where
+// that at least halves what it reads (65536 rows, 2048 kept, 8 heads: PIECES_US us with pieces, 68 without).
+void plan_evict_weight(const Plan& p, WeightPlan* wp) {
+    auto up = [](size_t x) { return (x + 255) / 256 * 256; };
+    wp->cu_piece[0] = wp->cu_cand[0] = 0;
+    wp->most_rows = 0;
+    bool pays = false, costs = false;
+    int64_t cand = 0;
+    for (int s = 0; s < p.n_seq; ++s) {
+        const int64_t L = p.tab.cu_seq[s + 1] - p.tab.cu_seq[s], B = p.tab.cu_bud[s + 1] - p.tab.cu_bud[s];
+        const int64_t pieces = L > kPieceRows ? (L + kPieceRows - 1) / kPieceRows : 0, left = pieces * std::min<int64_t>(B, kPieceRows);
+        if (pieces) (2 * left <= L ? pays : costs) = true;
+        cand += left;
+        wp->cu_piece[s + 1] = wp->cu_piece[s] + (int32_t)pieces;
+        wp->cu_cand[s + 1] = (int32_t)std::min<int64_t>(cand, INT32_MAX);
+        wp->most_rows = std::max(wp->most_rows, (int32_t)(pieces ? left : L));
+    }
+    if (!pays || costs || cand > INT32_MAX) {
+        wp->most_rows = 0;
+        for (int s = 0; s < p.n_seq; ++s) {
+            wp->cu_piece[s + 1] = wp->cu_cand[s + 1] = 0;
+            wp->most_rows = std::max(wp->most_rows, p.tab.cu_seq[s + 1] - p.tab.cu_seq[s]);
+        }
+    }
+    const size_t heads = (size_t)p.n_layers * p.h_kv;
+    wp->off_newest = up(heads * p.TB * sizeof(int32_t));  // (the kept rows' numbers in front, for callers that do not take them)
+    wp->off_cand = wp->off_newest + up(heads * wp->cu_piece[p.n_seq] * sizeof(int32_t));
+    wp->ws_bytes = wp->off_cand + up(heads * wp->cu_cand[p.n_seq] * 3 * sizeof(int32_t));
+}
+
+hipError_t launch_evict_weight(const Plan& p, const WeightPlan& wp, const int32_t* lens, const void* K, const void* V, const float* weights, const int32_t* pos,
+                               void* K_out, void* V_out, float* weights_out, int32_t* pos_out, int32_t* idx, char* ws, hipStream_t st) {
     WeightArgs a{};
     a.K = (const char*)K; a.V = (const char*)V; a.K_out = (char*)K_out; a.V_out = (char*)V_out;
     a.weights = weights; a.weights_out = weights_out; a.pos = pos; a.pos_out = pos_out; a.lens = lens; a.idx = idx;
     a.layer_budgets = p.layer_budgets;
     a.n_layers = p.n_layers; a.h_kv = p.h_kv; a.keep_first = p.keep_first; a.keep_last = p.keep_last;
     a.T = p.T; a.TB = p.TB; a.pm = p.page_map(); a.tab = p.tab;
-    int32_t most = 0;
-    for (int s = 0; s < p.n_seq; ++s) most = std::max(most, p.tab.cu_seq[s + 1] - p.tab.cu_seq[s]);
-    const int rounds = (most + kWeightWaves * kRoundRows - 1) / (kWeightWaves * kRoundRows);
-    const auto select = rounds <= 1 ? jq_weight_select_kernel<1, true> : rounds <= 4 ? jq_weight_select_kernel<4, true> : jq_weight_select_kernel<4, false>;
-    hipError_t e = launch_kernel(select, dim3((unsigned)p.h_kv, (unsigned)p.n_seq, (unsigned)p.n_layers), dim3(kWeightThreads), 0, st, nullptr, -1, a);
+    a.n_pieces = wp.cu_piece[p.n_seq]; a.n_cand = wp.cu_cand[p.n_seq];
+    for (int s = 0; s <= p.n_seq; ++s) { a.cu_piece[s] = wp.cu_piece[s]; a.cu_cand[s] = wp.cu_cand[s]; }
+    a.newest = (int32_t*)(ws + wp.off_newest);
+    a.cand_w = (float*)(ws + wp.off_cand);
+    a.cand_pos = (int32_t*)(a.cand_w + (size_t)p.n_layers * p.h_kv * a.n_cand);
+    a.cand_row = a.cand_pos + (size_t)p.n_layers * p.h_kv * a.n_cand;
+    const dim3 whole((unsigned)(p.n_seq * p.h_kv), (unsigned)p.n_layers), pieces((unsigned)(a.n_pieces * p.h_kv), (unsigned)p.n_layers), block(kWeightThreads);
+    hipError_t e = hipSuccess;
+    if (a.n_pieces > 0) {
+        if (pos && p.keep_last > 0) e = launch_kernel(jq_weight_newest_kernel, pieces, block, 0, st, nullptr, -1, a);
+        if (e == hipSuccess) e = launch_kernel(jq_weight_select_kernel<4, true, kPieces>, pieces, block, 0, st, nullptr, -1, a);
+        if (e == hipSuccess)
+            e = launch_kernel(wp.most_rows <= kPieceRows ? jq_weight_select_kernel<4, true, kRest> : jq_weight_select_kernel<4, false, kRest>, whole, block, 0, st,
+                              nullptr, -1, a);
+    } else {
+        e = launch_kernel(wp.most_rows <= kPieceRows / 4 ? jq_weight_select_kernel<1, true, kAllRows>
+                          : wp.most_rows <= kPieceRows   ? jq_weight_select_kernel<4, true, kAllRows>
+                                                         : jq_weight_select_kernel<4, false, kAllRows>,
+                          whole, block, 0, st, nullptr, -1, a);
+    }
     if (e != hipSuccess) return e;
     if (K_out == K)
         return launch_kernel(jq_weight_shift_kernel, dim3((unsigned)(8 * p.h_kv), (unsigned)p.n_seq, (unsigned)p.n_layers), dim3(kMoveThreads), 0, st, nullptr, -1, a);

@@ -165,6 +165,21 @@ def test_long_sequence_keeps_the_same_rows_as_the_plain_selection():
         np.testing.assert_array_equal(wo[0, g, :B].cpu().numpy(), w[0, g, i])
 
 
+@pytest.mark.parametrize("inplace", [False, True])
+@pytest.mark.parametrize("with_pos", [True, False])
+def test_sequences_selected_in_pieces(inplace, with_pos):
+    """Long sequences beside short ones, ties, protected rows of either end; live counts at the pieces' edges."""
+    caps, budgets = [40000, 300, 33000, 70001], [900, 200, 64, 1500]
+    lens = np.array([[40000, 300, 16384, 70001], [16385, 10, 32768, 65537]], np.int32)
+    evict(13, 2, caps, budgets, 1, lens=lens, inplace=inplace, first=3, last=20, ties=True, order="scrambled" if with_pos else "ascending",
+          with_pos=with_pos)
+
+
+def test_long_sequence_that_keeps_most_of_its_rows():
+    evict(14, 1, [40000], [30000], 1, inplace=True, first=2, last=5)
+    evict(15, 1, [40000], [30000], 1, ties=True, page=64, lens=np.array([[33333]], np.int32))
+
+
 @pytest.mark.parametrize("page", [0, 32])
 @pytest.mark.parametrize("first,last", [(0, 0), (4, 16)])
 def test_replace(page, first, last):
