@@ -31,6 +31,7 @@ constexpr int kAttendThreads = 64 * kAttendWaves;
 constexpr int kTileRows = 16;   // query rows of one MFMA tile
 constexpr int kOutStride = kHeadDim + 4;  // floats a row of partial output takes in LDS: rows of 128 would meet in the same banks
 constexpr int kMostHeld = 65536;  // bytes of logits that a workgroup holds in LDS
+constexpr float kLargeSum = 16777216.0f;
 constexpr float kSlack = 8.0f;  // a row's running maximum may lag this far (in powers of two) behind before its sums are rescaled
 
 // Which cache rows a query row sees, apart from the live ones' end.
@@ -308,6 +309,24 @@ __global__ __launch_bounds__(kAttendThreads, RT == 1 ? 3 : 2) void jq_attend_ker
     const int ns = a.cu_split[s + 1] - a.cu_split[s], mine = split - a.cu_split[s];
     const int row0 = rg * RT * kTileRows;
 
+    // Tiles of 32 keys, dealt to the sequence's waves in turn, so that all of them sweep one moving window of the cache.
+    const uint32_t stride = (uint32_t)a.h_kv * (kHeadDim * 2);
+    const int64_t first_row = a.pm.block_table ? ((int64_t)layer * a.pm.n_pages) << a.pm.page_shift : (int64_t)layer * a.T + a.cu_seq[s];
+    const char* K = a.K + first_row * stride + g * (kHeadDim * 2);
+    const char* V = a.V + first_row * stride + g * (kHeadDim * 2);
+    const_i32_ptr table = (const_i32_ptr)(a.pm.block_table ? a.pm.block_table + (int64_t)s * a.pm.max_pages : nullptr);
+    const int shift = a.pm.page_shift, n_pages = a.pm.n_pages;
+    const bool paged = a.pm.block_table != nullptr;
+    auto tile_row = [&](int key) {  // a page holds whole tiles: page sizes are powers of two from 32 on
+        if (!paged) return (uint32_t)key;
+        return ((uint32_t)clamp_page(table[key >> shift], n_pages) << shift) + (uint32_t)(key & ((1 << shift) - 1));
+    };
+    // The first tile is requested before anything else is looked at, the live count too, which only decides whether it matters: rows
+    // that are not live yet are the caller's as well, and masked.
+    const int step = 32 * kAttendWaves * ns, cap = a.cu_seq[s + 1] - a.cu_seq[s];
+    int key = 32 * (kAttendWaves * mine + wave);
+    KvTile t;
+    if (key < cap) load_tile(t, K, V, tile_row(key), cap - 1 - key, stride, lane);
     RowState<RT> st;
     int row_limit[RT];
     const uint32_t* row_seen[RT];
@@ -326,24 +345,6 @@ __global__ __launch_bounds__(kAttendThreads, RT == 1 ? 3 : 2) void jq_attend_ker
         row_seen[r] = MASK == kSeeTree ? a.seen + ((int64_t)s * a.n_q + i) * a.words : nullptr;
     }
 
-    // Tiles of 32 keys, dealt to the sequence's waves in turn, so that all of them sweep one moving window of the cache.
-    const uint32_t stride = (uint32_t)a.h_kv * (kHeadDim * 2);
-    const int64_t first_row = a.pm.block_table ? ((int64_t)layer * a.pm.n_pages) << a.pm.page_shift : (int64_t)layer * a.T + a.cu_seq[s];
-    const char* K = a.K + first_row * stride + g * (kHeadDim * 2);
-    const char* V = a.V + first_row * stride + g * (kHeadDim * 2);
-    const_i32_ptr table = (const_i32_ptr)(a.pm.block_table ? a.pm.block_table + (int64_t)s * a.pm.max_pages : nullptr);
-    const int shift = a.pm.page_shift, n_pages = a.pm.n_pages;
-    const bool paged = a.pm.block_table != nullptr;
-    auto tile_row = [&](int key) {  // a page holds whole tiles: page sizes are powers of two from 32 on
-        if (!paged) return (uint32_t)key;
-        return ((uint32_t)clamp_page(table[key >> shift], n_pages) << shift) + (uint32_t)(key & ((1 << shift) - 1));
-    };
-    // The first tile is requested ahead of the live count, which only decides whether it matters: rows that are not live yet are
-    // the caller's too, and masked.
-    const int step = 32 * kAttendWaves * ns, cap = a.cu_seq[s + 1] - a.cu_seq[s];
-    int key = 32 * (kAttendWaves * mine + wave);
-    KvTile t;
-    if (key < cap) load_tile(t, K, V, tile_row(key), cap - 1 - key, stride, lane);
     const int n = live_rows(a.lens, a.n_seq, layer, s, cap);
     // keys from `open` on are not seen by every row
     const int open = MASK == kSeeAll ? n : max(n - a.n_q + (MASK == kSeeCausal ? 1 : 0), 0);
@@ -540,10 +541,11 @@ template <int R>
 struct Wide {
     static constexpr int kWaves = 8, kThreads = 64 * kWaves, kRows = 32 * R;
     static constexpr int KW = kWaves / R;                      // waves over the same rows, each with keys of its own
-    static constexpr int kKeys = KW == 1 ? 64 : 128;           // of a stage
+    static constexpr int kKeys = KW == 4 ? 128 : 64;           // of a stage
     static constexpr int kTiles = kKeys / 32 / KW;             // of 32 keys, a wave and stage
-    static constexpr int kAhead = KW == 1 ? 2 : 1;             // stages requested ahead: 64 KB
+    static constexpr int kAhead = KW == 4 ? 1 : 2;             // stages requested ahead: 64 KB
     static constexpr bool kExact = R == 2;                     // probabilities in two bf16 parts
+    static constexpr int kEarly = 2;                           // blocks of V requested ahead of their use
     static constexpr int kRequests = kKeys / 2 / kWaves;       // of 1 KB, a wave and stage
     static constexpr int kBuffer = 2 * kKeys * 256;            // K, then V
     static constexpr int kMerge = (kWaves - R) * 32 * (kOutStride * 4 + 8);
@@ -568,24 +570,6 @@ __global__ __launch_bounds__(Wide<R>::kThreads, 2) void jq_attend_wide_kernel(At
     const int cap = a.cu_seq[s + 1] - a.cu_seq[s];
     const int rw = wave % R, kw = wave / R;
     const int row0 = rg * W::kRows + 32 * rw;
-
-    bf16x8 q[2][4];
-    f32x4 o[2][8];  // d = 16 r + 4 (l / 16) + e of query row l % 16 in o[i][r][e]
-    float m[2], z[2];
-    int token[2];   // the query rows' tokens
-#pragma unroll
-    for (int r = 0; r < 2; ++r) {
-        const int row = min(row0 + r * kTileRows + (lane & 15), a.rows - 1);
-        const int i = row / a.group, h = g * a.group + row - i * a.group;
-        const char* from = a.Q + ((((int64_t)layer * a.n_seq + s) * a.n_q + i) * a.h_q + h) * (kHeadDim * 2);
-#pragma unroll
-        for (int c = 0; c < 4; ++c) q[r][c] = __builtin_bit_cast(bf16x8, *(const au32x4*)(from + 64 * c + 16 * (lane >> 4)));
-#pragma unroll
-        for (int d = 0; d < 8; ++d) o[r][d] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-        m[r] = -__builtin_inff();
-        z[r] = 0.0f;
-        token[r] = i;
-    }
 
     const uint32_t stride = (uint32_t)a.h_kv * (kHeadDim * 2);
     const int64_t first_row = a.pm.block_table ? ((int64_t)layer * a.pm.n_pages) << a.pm.page_shift : (int64_t)layer * a.T + a.cu_seq[s];
@@ -614,12 +598,31 @@ __global__ __launch_bounds__(Wide<R>::kThreads, 2) void jq_attend_wide_kernel(At
 #pragma unroll
         for (int i = 0; i < W::kRequests; ++i) to[i] = *(const au32x4*)(base + (row0 + (uint32_t)min(my_row + 4 * i, last)) * stride);
     };
-    // (The first stages are requested ahead of the live count: rows that are not live yet are the caller's too, and masked.)
+    // The first stages are requested before anything else is looked at, the live count too: rows that are not live yet are the
+    // caller's as well, and masked.  (What follows, mostly instructions that the cache does not hold yet, takes some 3 us.)
     au32x4 ahead[W::kAhead][W::kRequests];
 #pragma unroll
     for (int i = 0; i < W::kAhead; ++i) request(ahead[i], i, cap);
     const int n = live_rows(a.lens, a.n_seq, layer, s, cap);
     const int open = MASK == kSeeAll ? n : max(n - a.n_q + (MASK == kSeeCausal ? 1 : 0), 0);
+    bf16x8 q[2][4];
+    f32x4 o[2][8];  // d = 16 r + 4 (l / 16) + e of query row l % 16 in o[i][r][e]
+    float m[2], z[2];
+    int token[2];   // the query rows' tokens
+#pragma unroll
+    for (int r = 0; r < 2; ++r) {
+        const int row = min(row0 + r * kTileRows + (lane & 15), a.rows - 1);
+        const int i = row / a.group, h = g * a.group + row - i * a.group;
+        const char* from = a.Q + ((((int64_t)layer * a.n_seq + s) * a.n_q + i) * a.h_q + h) * (kHeadDim * 2);
+#pragma unroll
+        for (int c = 0; c < 4; ++c) q[r][c] = __builtin_bit_cast(bf16x8, *(const au32x4*)(from + 64 * c + 16 * (lane >> 4)));
+#pragma unroll
+        for (int d = 0; d < 8; ++d) o[r][d] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+        m[r] = -__builtin_inff();
+        z[r] = 0.0f;
+        token[r] = i;
+    }
+
     // Addresses of a wave's reads in buffer 0: K by chunk of the dimensions (16 keys further on: + 4096), V by block of sixteen.
     int k_at[4], v_at[8];
     {
@@ -647,66 +650,87 @@ __global__ __launch_bounds__(Wide<R>::kThreads, 2) void jq_attend_wide_kernel(At
 #pragma unroll
         for (int k = 0; k < W::kRequests; ++k) *(au32x4*)(wide_lds + buf * W::kBuffer + to_lds[k]) = from[k];
     };
-    auto work = [&](int key0, int at) {  // the wave's keys of a stage, from key0; `at`: the buffer's place in LDS
-        constexpr int T = W::kTiles;
-        f32x4 x[T][2][2];  // by tile, row tile, half tile
+    auto work = [&](int key0, int at) {  // the 32 keys from key0; `at`: their place in LDS behind the wave's first ones
+        // LDS answers late: all of K's rows are requested together, and half of V's ahead of the terms.
+        bf16x8 k[4][2];
 #pragma unroll
-        for (int t = 0; t < T; ++t)
+        for (int c = 0; c < 4; ++c)
 #pragma unroll
-            for (int c = 0; c < 4; ++c)
+            for (int i = 0; i < 2; ++i) k[c][i] = *(const bf16x8*)(wide_lds + k_at[c] + at + i * 4096);
+        __builtin_amdgcn_sched_barrier(0);
+        f32x4 x[2][2];  // by row tile, half tile
 #pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    const bf16x8 k = *(const bf16x8*)(wide_lds + k_at[c] + at + t * 8192 + i * 4096);
+        for (int c = 0; c < 4; ++c)
 #pragma unroll
-                    for (int r = 0; r < 2; ++r)
-                        x[t][r][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, q[r][c], c ? x[t][r][i] : f32x4{0.0f, 0.0f, 0.0f, 0.0f}, 0, 0, 0);
-                }
-        if (key0 + 32 * T > open) {
+            for (int i = 0; i < 2; ++i)
 #pragma unroll
-            for (int t = 0; t < T; ++t)
+                for (int r = 0; r < 2; ++r)
+                    x[r][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k[c][i], q[r][c], c ? x[r][i] : f32x4{0.0f, 0.0f, 0.0f, 0.0f}, 0, 0, 0);
+        s16x4 v[8][2];
+        auto read_v = [&](int d) {
 #pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    const uint32_t bad = *(const uint32_t*)(bad_keys + at / W::kBuffer * W::kKeys + 32 * (T * kw + t) + 16 * i + 4 * (lane >> 4));
+            for (int i = 0; i < 2; ++i) v[d][i] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)(wide_lds + v_at[d] + at + i * 4096));
+        };
 #pragma unroll
-                    for (int r = 0; r < 2; ++r)
+        for (int d = 0; d < W::kEarly; ++d) read_v(d);
+        __builtin_amdgcn_sched_barrier(0);
+        if (key0 + 32 > open) {
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            const int key = key0 + 32 * t + 16 * i + 4 * (lane >> 4) + e;
-                            bool see = key < n;
-                            if (MASK == kSeeCausal) see = key <= n - a.n_q + token[r];
-                            if (MASK == kSeeTree) {
-                                const int j = key - (n - a.n_q);
-                                if (see && j >= 0) see = (a.seen[((int64_t)s * a.n_q + token[r]) * a.words + (j >> 5)] >> (j & 31)) & 1u;
-                            }
-                            x[t][r][i][e] = see ? ((bad >> (8 * e)) & 1u ? __builtin_nanf("") : x[t][r][i][e]) : -__builtin_inff();
+            for (int i = 0; i < 2; ++i) {
+                const uint32_t bad = *(const uint32_t*)(bad_keys + at / W::kBuffer * W::kKeys + at % W::kBuffer / 256 + 32 * W::kTiles * kw + 16 * i + 4 * (lane >> 4));
+#pragma unroll
+                for (int r = 0; r < 2; ++r)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const int key = key0 + 16 * i + 4 * (lane >> 4) + e;
+                        bool see = key < n;
+                        if (MASK == kSeeCausal) see = key <= n - a.n_q + token[r];
+                        if (MASK == kSeeTree) {
+                            const int j = key - (n - a.n_q);
+                            if (see && j >= 0) see = (a.seen[((int64_t)s * a.n_q + token[r]) * a.words + (j >> 5)] >> (j & 31)) & 1u;
                         }
-                }
+                        x[r][i][e] = see ? ((bad >> (8 * e)) & 1u ? __builtin_nanf("") : x[r][i][e]) : -__builtin_inff();
+                    }
+            }
         }
         if (KEEP) {
 #pragma unroll
             for (int r = 0; r < 2; ++r) {
                 const int row = row0 + r * kTileRows + (lane & 15);
                 float* to = a.logits + (((int64_t)layer * a.h_kv + g) * a.rows + row) * a.logit_T + logit_at(a.cu_seq, s) + key0 + 4 * (lane >> 4);
-#pragma unroll
-                for (int t = 0; t < T; ++t)
-                    if (row < a.rows && key0 + 32 * t < n) {
-                        *(f32x4*)(to + 32 * t) = x[t][r][0] * a.scale2;
-                        *(f32x4*)(to + 32 * t + 16) = x[t][r][1] * a.scale2;
-                    }
+                if (row < a.rows) {
+                    *(f32x4*)to = x[r][0] * a.scale2;
+                    *(f32x4*)(to + 16) = x[r][1] * a.scale2;
+                }
             }
         }
-        float top[2];
-#pragma unroll
-        for (int r = 0; r < 2; ++r) {
-            top[r] = fmaxf(max4(x[0][r][0]), max4(x[0][r][1]));
-#pragma unroll
-            for (int t = 1; t < T; ++t) top[r] = fmaxf(top[r], fmaxf(max4(x[t][r][0]), max4(x[t][r][1])));
-            top[r] *= a.scale2;
-        }
-        if (__any(top[0] > m[0] + kSlack || top[1] > m[1] + kSlack)) {
+        // The running maximum only has to keep the terms in range, so it is set by the first keys and looked at again when a row's sum
+        // has grown past 2^24 (it cannot by its number of keys alone) or is not a number: then the tile's terms are formed anew.
+        // (Finding the maximum of every tile took a sixth of the instructions.)
+        bf16x8 p[2], rest[2];
+        float sum[2];
+        auto terms = [&]() {
 #pragma unroll
             for (int r = 0; r < 2; ++r) {
-                float to = fmaxf(top[r], __shfl_xor(top[r], 16));
+                const float mm = m[r] == -__builtin_inff() ? 0.0f : m[r];
+                sum[r] = z[r];
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const float y = __builtin_amdgcn_exp2f(__builtin_fmaf(x[r][i][e], a.scale2, -mm));
+                        sum[r] += y;
+                        p[r][4 * i + e] = (__bf16)y;
+                        if (W::kExact) rest[r][4 * i + e] = (__bf16)(y - (float)p[r][4 * i + e]);
+                    }
+            }
+        };
+        terms();
+        if (__any(!(fmaxf(sum[0], sum[1]) <= kLargeSum) || fminf(m[0], m[1]) == -__builtin_inff())) {
+#pragma unroll
+            for (int r = 0; r < 2; ++r) {
+                float to = fmaxf(max4(x[r][0]), max4(x[r][1])) * a.scale2;
+                to = fmaxf(to, __shfl_xor(to, 16));
                 to = fmaxf(m[r], fmaxf(to, __shfl_xor(to, 32)));
                 const float f = m[r] == to ? 1.0f : __builtin_amdgcn_exp2f(m[r] - to);
                 m[r] = to;
@@ -714,36 +738,20 @@ __global__ __launch_bounds__(Wide<R>::kThreads, 2) void jq_attend_wide_kernel(At
 #pragma unroll
                 for (int d = 0; d < 8; ++d) o[r][d] *= f;
             }
+            terms();
         }
-        float mm[2];
 #pragma unroll
-        for (int r = 0; r < 2; ++r) mm[r] = m[r] == -__builtin_inff() ? 0.0f : m[r];
+        for (int r = 0; r < 2; ++r) z[r] = sum[r];
 #pragma unroll
-        for (int t = 0; t < T; ++t) {
-            bf16x8 p[2], rest[2];
+        for (int d = 0; d < 8; ++d) {
+            if (d + W::kEarly < 8) read_v(d + W::kEarly);
+            __builtin_amdgcn_sched_barrier(0);
+            const bf16x8 vt = __builtin_bit_cast(bf16x8, __builtin_shufflevector(v[d][0], v[d][1], 0, 1, 2, 3, 4, 5, 6, 7));
 #pragma unroll
-            for (int r = 0; r < 2; ++r)
+            for (int r = 0; r < 2; ++r) o[r][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vt, p[r], o[r][d], 0, 0, 0);
+            if (W::kExact) {
 #pragma unroll
-                for (int i = 0; i < 2; ++i)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const float y = __builtin_amdgcn_exp2f(__builtin_fmaf(x[t][r][i][e], a.scale2, -mm[r]));
-                        z[r] += y;
-                        p[r][4 * i + e] = (__bf16)y;
-                        if (W::kExact) rest[r][4 * i + e] = (__bf16)(y - (float)p[r][4 * i + e]);
-                    }
-#pragma unroll
-            for (int d = 0; d < 8; ++d) {
-                s16x4 v[2];
-#pragma unroll
-                for (int i = 0; i < 2; ++i) v[i] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)(wide_lds + v_at[d] + at + t * 8192 + i * 4096));
-                const bf16x8 vt = __builtin_bit_cast(bf16x8, __builtin_shufflevector(v[0], v[1], 0, 1, 2, 3, 4, 5, 6, 7));
-#pragma unroll
-                for (int r = 0; r < 2; ++r) o[r][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vt, p[r], o[r][d], 0, 0, 0);
-                if (W::kExact) {
-#pragma unroll
-                    for (int r = 0; r < 2; ++r) o[r][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vt, rest[r], o[r][d], 0, 0, 0);
-                }
+                for (int r = 0; r < 2; ++r) o[r][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vt, rest[r], o[r][d], 0, 0, 0);
             }
         }
     };
@@ -756,10 +764,13 @@ __global__ __launch_bounds__(Wide<R>::kThreads, 2) void jq_attend_wide_kernel(At
                 const int i = i0 + buf;
                 if (i >= n_mine) break;  // (uniform)
                 deposit(ahead[buf % W::kAhead], i, buf);
-                request(ahead[buf % W::kAhead], i + W::kAhead, n);
+                request(ahead[buf % W::kAhead], i + W::kAhead, n);  // (past the last stage: its last tile again, which costs less than a branch)
                 lds_barrier();
-                const int key0 = (mine + i * ns) * W::kKeys + 32 * W::kTiles * kw;
-                if (key0 < n) work(key0, buf * W::kBuffer);
+#pragma unroll
+                for (int t = 0; t < W::kTiles; ++t) {
+                    const int key0 = (mine + i * ns) * W::kKeys + 32 * (W::kTiles * kw + t);
+                    if (key0 < n) work(key0, buf * W::kBuffer + t * 8192);
+                }
             }
         }
     }
@@ -917,30 +928,40 @@ static void plan_splits(const Plan& p, bool weights, AttendPlan* ap) {
     const int row_tiles = (p.rows + kTileRows - 1) / kTileRows;
     ap->row_tiles = row_tiles <= 1 ? 1 : row_tiles <= 2 ? 2 : row_tiles <= 4 ? 4 : row_tiles <= 8 ? 8 : 16;
     ap->row_groups = (row_tiles + ap->row_tiles - 1) / ap->row_tiles;
-    // The smallest share (in rows of the cache, whole tiles for every wave) that makes no more workgroups than there are CUs.
-    const int64_t heads = (int64_t)p.n_layers * p.h_kv * ap->row_groups, unit = 128;
+    // Shares of a sequence are counted in what its workgroups take at a time.  First the smallest share that makes no more workgroups
+    // than there are CUs, then those left over to the sequences with the largest.
+    const int64_t heads = (int64_t)p.n_layers * p.h_kv * ap->row_groups, unit = ap->row_tiles > 4 ? 64 : 128;
+    auto units = [&](int s) { return (p.tab.cu_seq[s + 1] - p.tab.cu_seq[s] + unit - 1) / unit; };
     auto workgroups = [&](int64_t share) {
         int64_t n = 0;
-        for (int s = 0; s < p.n_seq; ++s) n += (p.tab.cu_seq[s + 1] - p.tab.cu_seq[s] + share - 1) / share;
-        return n * heads;
+        for (int s = 0; s < p.n_seq; ++s) n += (units(s) + share - 1) / share;
+        return n;
     };
     int64_t lo = 1, hi = (p.T + unit - 1) / unit;
     if (weights && row_tiles <= 2) hi = std::min(hi, (int64_t)kMostHeld / (p.rows * 4) / unit);  // its logits have to fit the LDS that is theirs
     while (lo < hi) {
         const int64_t mid = (lo + hi) / 2;
-        if (workgroups(mid * unit) <= kChip) hi = mid; else lo = mid + 1;
+        if (workgroups(mid) * heads <= kChip) hi = mid; else lo = mid + 1;
     }
-    const int64_t share = lo * unit;
+    int32_t ns[JQ_MAX_SEQ];
+    for (int s = 0; s < p.n_seq; ++s) ns[s] = (int32_t)((units(s) + lo - 1) / lo);
+    if (p.n_seq > 1)
+        for (int64_t left = kChip / heads - workgroups(lo); left > 0; --left) {
+            int at = 0;
+            for (int s = 1; s < p.n_seq; ++s)
+                if (units(s) * ns[at] > units(at) * ns[s]) at = s;
+            if (units(at) <= ns[at]) break;
+            ++ns[at];
+        }
     ap->cu_split[0] = 0;
     int64_t most_L = 0, tiles = 0;
     int32_t most_ns = 0;
     for (int s = 0; s < p.n_seq; ++s) {
         const int64_t L = p.tab.cu_seq[s + 1] - p.tab.cu_seq[s];
-        const int32_t ns = (int32_t)((L + share - 1) / share);
-        ap->cu_split[s + 1] = ap->cu_split[s] + ns;
+        ap->cu_split[s + 1] = ap->cu_split[s] + ns[s];
         most_L = std::max(most_L, L);
-        most_ns = std::max(most_ns, ns);
-        tiles = std::max(tiles, ((L + 31) / 32 + 4 * ns - 1) / (4 * ns));  // of 32 keys, a wave
+        most_ns = std::max(most_ns, ns[s]);
+        tiles = std::max(tiles, ((L + 31) / 32 + 4 * ns[s] - 1) / (4 * ns[s]));  // of 32 keys, a wave
     }
     ap->hold_keys = weights && row_tiles <= 2 ? (int32_t)(tiles * 32 * kAttendWaves) : 0;
     ap->one_launch = row_tiles <= 2 && most_ns <= kMostJoined && most_ns * p.rows <= kMostSums && (!weights || most_ns == 1 || most_L * p.rows <= kMostWeighed);
