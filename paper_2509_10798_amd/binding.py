@@ -7,6 +7,7 @@ if the library cannot be loaded the import of a function fails loudly.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import os
 from dataclasses import dataclass, field
@@ -525,10 +526,18 @@ def _call(name, shape: Shape, pages, device, stream, *args):
     _check(rc, name)
 
 
-def _workspace(ws, need, device):
+def _empty(size, dtype, device, stream):
+    """A new tensor on GPU number `device`, of the memory that belongs to the stream the call goes to: it is not handed to others
+    before that stream is done with it."""
+    import torch
+    with contextlib.nullcontext() if stream is None else torch.cuda.stream(stream):
+        return torch.empty(size, dtype=dtype, device=torch.device("cuda", device))
+
+
+def _workspace(ws, need, device, stream):
     import torch
     if ws is None:
-        ws = torch.empty(need(), dtype=torch.uint8, device=torch.device("cuda", device))
+        ws = _empty(need(), torch.uint8, device, stream)
     return _tensor("ws", ws, torch.uint8, (ws.numel(),), device), ws.numel(), ws
 
 
@@ -549,9 +558,9 @@ def _attend(name, shape: Shape, pages, seen, Q, K, V, lens, out, lse, want_lse, 
     rows = (shape.n_layers, shape.n_seq, shape.n_q, shape.h_q)
     q, kv = rows + (shape.d,), _cache_size(shape, pages, K)
     if out is None:
-        out = torch.empty_like(Q)
+        out = _empty(q, bf, dev, stream)
     if lse is None and want_lse:
-        lse = torch.empty(rows, dtype=f32, device=K.device)
+        lse = _empty(rows, f32, dev, stream)
     ins = (_tensor("Q", Q, bf, q, dev), _tensor("K", K, bf, kv, dev), _tensor("V", V, bf, kv, dev), _tensor("out", out, bf, q, dev),
            _tensor("lse", lse, f32, rows, dev))
     front = (_tensor("lens", lens, i32, rows[:2], dev),)
@@ -559,7 +568,7 @@ def _attend(name, shape: Shape, pages, seen, Q, K, V, lens, out, lse, want_lse, 
         front += (_tensor("seen", seen, i32, (shape.n_seq, shape.n_q, -(-shape.n_q // 32)), dev),)
     else:
         ins += (_tensor("weights", weights, f32, (shape.n_layers, shape.h_kv, shape.T), dev),)
-    sp, n, ws = _workspace(ws, lambda: attend_workspace_bytes(shape, weights is not None), dev)
+    sp, n, ws = _workspace(ws, lambda: attend_workspace_bytes(shape, weights is not None), dev, stream)
     _call(name, shape, pages, dev, stream, *front, *ins, sp, n)
     return out, lse
 
@@ -612,13 +621,13 @@ def _evict_weight(name, shape: Shape, pages, K, V, weights, pos, lens, K_out, V_
     if K_out is None and V_out is None and weights_out is None and pos_out is None:  # within the cache
         K_out, V_out, weights_out, pos_out = K, V, weights, pos
     if idx_out is None:
-        idx_out = torch.empty(kept, dtype=i32, device=K.device)
+        idx_out = _empty(kept, i32, dev, stream)
     args = (_tensor("lens", lens, i32, (shape.n_layers, shape.n_seq), dev), _tensor("K", K, bf, kv, dev), _tensor("V", V, bf, kv, dev),
             _tensor("weights", weights, f32, per_row, dev), _tensor("pos", pos, i32, per_row, dev), _tensor("K_out", K_out, bf, kv, dev),
             _tensor("V_out", V_out, bf, kv, dev), _tensor("weights_out", weights_out, f32, per_row, dev),
             _tensor("pos_out", pos_out, i32, per_row, dev), _tensor("idx_out", idx_out, i32, kept, dev))
     _tensor("layer_budgets", shape.layer_budgets, i32, (shape.n_layers, shape.n_seq), dev)
-    sp, n, ws = _workspace(ws, lambda: evict_weight_workspace_bytes(shape), dev)
+    sp, n, ws = _workspace(ws, lambda: evict_weight_workspace_bytes(shape), dev, stream)
     _call(name, shape, pages, dev, stream, *args, sp, n)
     return K_out, V_out, weights_out, pos_out, idx_out
 
@@ -644,7 +653,7 @@ def _replace(name, shape: Shape, pages, k_new, v_new, token, K, V, weights, pos,
     dev, bf, f32, i32 = _device_of(K), torch.bfloat16, torch.float32, torch.int32
     kv, per_row, heads = _cache_size(shape, pages, K), (shape.n_layers, shape.h_kv, shape.T), (shape.n_layers, shape.n_seq, shape.h_kv)
     if slot_out is None:
-        slot_out = torch.empty(heads, dtype=i32, device=K.device)
+        slot_out = _empty(heads, i32, dev, stream)
     _call(name, shape, pages, dev, stream, _tensor("lens", lens, i32, heads[:2], dev), _tensor("k_new", k_new, bf, heads + (shape.d,), dev),
           _tensor("v_new", v_new, bf, heads + (shape.d,), dev), _tensor("token", token, i32, (shape.n_seq,), dev), _tensor("K", K, bf, kv, dev),
           _tensor("V", V, bf, kv, dev), _tensor("weights", weights, f32, per_row, dev), _tensor("pos", pos, i32, per_row, dev),

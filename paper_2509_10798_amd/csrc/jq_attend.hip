@@ -915,12 +915,17 @@ __global__ __launch_bounds__(kAttendThreads) void jq_attend_finish_kernel(Attend
 
 // ---- host ------------------------------------------------------------------------------------------------------------------
 
-// How many workgroups share each sequence: as many as make one per CU over the whole call, none with fewer than 128 rows of the
-// cache to itself.  More of them ask for no more bytes a second and leave more sums to join (us a call, workgroups 256 / 512 / 768):
-// one token over 131072 rows 100 / 109 / 106, 32 tokens behind four prompts of 52296 rows together 61 / 72 / 83, a tree of 64 over
-// 32832 rows 60 / 77 / 96.  Rounded up sequence by sequence, 256 workgroups' worth of rows became 288 for eight ragged sequences,
-// which two rounds of the chip took 63 us for; found by bisection, 47.
-constexpr int kChip = 256;
+// How many workgroups share each sequence.  Asked for more than one workgroup per CU, memory answers no faster, and there are more
+// sums to join (us a call, workgroups 256 / 512 / 768): one token over 131072 rows 100 / 109 / 106, 32 tokens behind four prompts of
+// 52296 rows together 61 / 72 / 83, a tree of 64 over 32832 rows 60 / 77 / 96.  So the smallest share is looked for that makes
+// no more workgroups than there are CUs -- not a share of the rows rounded up for every sequence, which made 288 for eight ragged
+// ones (63 us, 47 now).  Where sequences and heads alone are more than that, whole sequences leave CUs idle behind the longest, and
+// smaller shares in two to four rounds of the chip may be ahead; a round costs its share and a start, which is dearer where sums of
+// many query rows have to be joined afterwards.  In rows of the cache, fitted to (whole sequences / as chosen) one token, 40 x 4099 rows
+// 158 / 133 us, 36 x 2000 78 / 65, 64 ragged sequences of 80 to 7000 203 / 128; trees of 20 over those 257 / 161, 12 x 40 x 4099 189 /
+// 177, and as they are 25 x 40 x 2099 103 (125 in smaller shares), 64 x 40 x 1099 96 (133).
+constexpr int kChip = 256, kRounds = 4;
+constexpr int kStart = 320, kWideStart = 1500;
 constexpr int kMostSums = 160;       // sums of 128 dimensions that it adds up
 constexpr int kMostJoined = 64;      // shares of a sequence that its last workgroup joins: a lane each
 constexpr int64_t kMostWeighed = 16384;  // logits of a (sequence, head) that it weighs
@@ -928,29 +933,36 @@ static void plan_splits(const Plan& p, bool weights, AttendPlan* ap) {
     const int row_tiles = (p.rows + kTileRows - 1) / kTileRows;
     ap->row_tiles = row_tiles <= 1 ? 1 : row_tiles <= 2 ? 2 : row_tiles <= 4 ? 4 : row_tiles <= 8 ? 8 : 16;
     ap->row_groups = (row_tiles + ap->row_tiles - 1) / ap->row_tiles;
-    // Shares of a sequence are counted in what its workgroups take at a time.  First the smallest share that makes no more workgroups
-    // than there are CUs, then those left over to the sequences with the largest.
+    // Shares are counted in what a workgroup takes at a time; workgroups left over go to the sequences with the largest.
     const int64_t heads = (int64_t)p.n_layers * p.h_kv * ap->row_groups, unit = ap->row_tiles > 4 ? 64 : 128;
-    auto units = [&](int s) { return (p.tab.cu_seq[s + 1] - p.tab.cu_seq[s] + unit - 1) / unit; };
+    int32_t units[JQ_MAX_SEQ];
+    for (int s = 0; s < p.n_seq; ++s) units[s] = (int32_t)(((int64_t)p.tab.cu_seq[s + 1] - p.tab.cu_seq[s] + unit - 1) / unit);
     auto workgroups = [&](int64_t share) {
         int64_t n = 0;
-        for (int s = 0; s < p.n_seq; ++s) n += (units(s) + share - 1) / share;
+        for (int s = 0; s < p.n_seq; ++s) n += ((uint32_t)units[s] + (uint32_t)share - 1) / (uint32_t)share;
         return n;
     };
-    int64_t lo = 1, hi = (p.T + unit - 1) / unit;
-    if (weights && row_tiles <= 2) hi = std::min(hi, (int64_t)kMostHeld / (p.rows * 4) / unit);  // its logits have to fit the LDS that is theirs
-    while (lo < hi) {
-        const int64_t mid = (lo + hi) / 2;
-        if (workgroups(mid) * heads <= kChip) hi = mid; else lo = mid + 1;
+    int64_t most = (p.T + unit - 1) / unit;
+    if (weights && row_tiles <= 2) most = std::min(most, (int64_t)kMostHeld / (p.rows * 4) / unit);  // its logits have to fit the LDS that is theirs
+    int64_t share = most, best = INT64_MAX, slots = 0;
+    const int64_t start = ap->row_tiles > 2 ? kWideStart : kStart;
+    for (int rounds = 1; rounds <= (p.n_seq * heads > kChip ? kRounds : 1); ++rounds) {
+        int64_t lo = 1, hi = most;
+        while (lo < hi) {
+            const int64_t mid = (lo + hi) / 2;
+            if (workgroups(mid) * heads <= rounds * kChip) hi = mid; else lo = mid + 1;
+        }
+        const int64_t n = workgroups(lo) * heads, cost = (n + kChip - 1) / kChip * (lo * unit + start);
+        if (cost < best) { best = cost; share = lo; slots = rounds * kChip / heads; }
     }
     int32_t ns[JQ_MAX_SEQ];
-    for (int s = 0; s < p.n_seq; ++s) ns[s] = (int32_t)((units(s) + lo - 1) / lo);
+    for (int s = 0; s < p.n_seq; ++s) ns[s] = (int32_t)((units[s] + share - 1) / share);
     if (p.n_seq > 1)
-        for (int64_t left = kChip / heads - workgroups(lo); left > 0; --left) {
+        for (int64_t left = slots - workgroups(share); left > 0; --left) {
             int at = 0;
             for (int s = 1; s < p.n_seq; ++s)
-                if (units(s) * ns[at] > units(at) * ns[s]) at = s;
-            if (units(at) <= ns[at]) break;
+                if ((int64_t)units[s] * ns[at] > (int64_t)units[at] * ns[s]) at = s;
+            if (units[at] <= ns[at]) break;
             ++ns[at];
         }
     ap->cu_split[0] = 0;

@@ -423,7 +423,7 @@ __global__ __launch_bounds__(kReplaceThreads) void jq_replace_kernel(ReplaceArgs
 // ---- host ------------------------------------------------------------------------------------------------------------------
 
 // Pieces or not: with pieces the last selection reads pieces * budget rows of every long sequence instead of all.  They are taken where
-// that at least halves what it reads (65536 rows, 2048 kept, 8 heads: PIECES_US us with pieces, 68 without).
+// that at least halves what it reads (65536 rows, 2048 kept, 8 heads: 40 us a call with pieces, 73 without).
 void plan_evict_weight(const Plan& p, WeightPlan* wp) {
     auto up = [](size_t x) { return (x + 255) / 256 * 256; };
     wp->cu_piece[0] = wp->cu_cand[0] = 0;

@@ -209,6 +209,25 @@ def test_many_layers_sequences_and_heads():
     run(18, 3, list(range(20, 20 + 40)), 32, 8, 1, weigh=True)
 
 
+def test_as_many_sequences_as_a_call_takes():
+    lens = np.array([[(37 * i) % 70 for i in range(128)]], np.int32)
+    run(22, 1, [70 - (i % 3) for i in range(128)], 4, 2, 1, lens=lens, page=32, weigh=True)
+    run(23, 1, [70 - (i % 3) for i in range(128)], 4, 2, 9, mode="tree")
+
+
+def test_more_sequences_than_the_chip_takes_at_a_time():
+    """300 (sequence, head) pairs of very different lengths, cut into shares of several rounds, with and without weights to hold."""
+    caps = [5, 2000, 37, 700, 1, 333] * 25
+    run(24, 1, caps[:100], 3, 3, 1, weigh=True)
+    run(25, 1, [c + 20 for c in caps[:100]], 12, 3, 20, mode="causal", lens=np.array([[c + i % 23 for i, c in enumerate(caps[:100])]], np.int32))
+    run(26, 1, [c + 20 for c in caps[:100]], 12, 3, 20, mode="tree")
+
+
+def test_more_query_rows_than_a_workgroup_takes():
+    run(27, 1, [700, 400], 8, 2, 300, mode="causal")
+    run(28, 1, [333], 40, 2, 40, mode="tree", page=32)
+
+
 def test_the_same_call_twice_gives_the_same_bits():
     import torch
     rng, Q, K, V, cu, live = make(19, 1, [9000, 511], 32, 8, 1, None)
@@ -272,6 +291,24 @@ def test_calls_on_two_streams():
         got.append((o, e))
     for i, (o, e) in enumerate(got):
         jq.attend(sh, q, k, v, out=o, lse=e, ws=wss[i % 2], stream=streams[i % 2])
+    torch.cuda.synchronize()
+    for o, e in got:
+        assert torch.equal(o, ref[0]) and torch.equal(e, ref[1])
+
+
+def test_temporaries_belong_to_the_stream_of_the_call():
+    """Calls on a side stream whose workspace and outputs are allocated inside, while the current stream allocates and overwrites
+    memory of the same sizes."""
+    import torch
+    rng, Q, K, V, cu, live = make(29, 1, [3000], 16, 4, 1, None)
+    sh = jq.Shape(n_layers=1, seq_lens=[3000], n_q=1, h_q=16, h_kv=4)
+    q, k, v = to_dev_bf16(Q), to_dev_bf16(K), to_dev_bf16(V)
+    ref = jq.attend(sh, q, k, v)
+    torch.cuda.synchronize()
+    side, got = torch.cuda.Stream(), []
+    for _ in range(20):
+        got.append(jq.attend(sh, q, k, v, stream=side))
+        torch.empty(jq.attend_workspace_bytes(sh), dtype=torch.uint8, device="cuda").fill_(0xFF)
     torch.cuda.synchronize()
     for o, e in got:
         assert torch.equal(o, ref[0]) and torch.equal(e, ref[1])
