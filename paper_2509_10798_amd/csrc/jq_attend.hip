@@ -6,7 +6,11 @@
 //   weights[j] += sum_r p[r,j]        (where the caller accumulates the attention every cached row receives)
 //
 // K and V are read once, 512 bytes a (row, KV head); the few query rows stay in registers.  One pass with a running maximum m
-// and sum z per query row; workgroups that share a sequence leave (m, z, unnormalised out) which a second launch joins.
+// and sum z per query row; workgroups that share a sequence leave (m, z, unnormalised out), which the last of them joins, or a
+// second launch where that is much.  All sums and statistics are fp32.  Measured on one MI355X, whole calls, 8 KV heads of 4 query
+// heads: one token over 131072 rows 101 us (5.3 TB/s; a copy of 2 GiB reaches 4.9), 32 sequences of 2048 rows with weights 55
+// (bound by memory), one token over 1000 rows of 2 heads 11 (bound by the round trips of a join), 25 drafted tokens over eight
+// paged caches of 29909 rows together 42, 64 over 32832 rows 55 (matrix and vector instructions, which take turns).
 //
 // Layout.  Both products are v_mfma_f32_16x16x32_bf16, of which lane l holds row (or column) l % 16 and the eight products'
 // terms 8 * (l / 16) .. + 7 of either operand, and of the result column l % 16 and rows 4 * (l / 16) .. + 3.  Scores are
@@ -31,8 +35,8 @@ constexpr int kAttendThreads = 64 * kAttendWaves;
 constexpr int kTileRows = 16;   // query rows of one MFMA tile
 constexpr int kOutStride = kHeadDim + 4;  // floats a row of partial output takes in LDS: rows of 128 would meet in the same banks
 constexpr int kMostHeld = 65536;  // bytes of logits that a workgroup holds in LDS
-constexpr float kLargeSum = 16777216.0f;
 constexpr float kSlack = 8.0f;  // a row's running maximum may lag this far (in powers of two) behind before its sums are rescaled
+constexpr float kLargeSum = 16777216.0f;  // or, with many query rows, until a lane's share of the sum is this large
 
 // Which cache rows a query row sees, apart from the live ones' end.
 enum AttendMask { kSeeAll = 0, kSeeCausal, kSeeTree };
@@ -171,10 +175,10 @@ __device__ __forceinline__ void tile_step(RowState<RT>& st, KvTile& t, const Att
                     s[r][i][e] = see ? (bad[i][e] ? __builtin_nanf("") : s[r][i][e]) : -__builtin_inff();
                 }
     }
-    if (KEEP) {  // `hold`: the lane's place in the tile's part of the held logits, null for the lanes past the last query row
+    if (KEEP) {  // `hold`: the lane's place in the tile's part of the held logits
 #pragma unroll
         for (int r = 0; r < RT; ++r)
-            if (hold && r * kTileRows + (lane & 15) < a.rows) {
+            if (r * kTileRows + (lane & 15) < a.rows) {
 #pragma unroll
                 for (int i = 0; i < 2; ++i) *(f32x4*)(hold + r * kTileRows * a.hold_keys + 16 * i) = s[r][i];
             }
@@ -194,8 +198,9 @@ __device__ __forceinline__ void tile_step(RowState<RT>& st, KvTile& t, const Att
             for (int d = 0; d < 8; ++d) st.o[r][d] *= f;
         }
     }
-    // Probabilities in two bf16 parts, the rounded value and the rest (2^-17 of it): out is then as exact as its own rounding
-    // leaves it.  The second product doubles, which a call of few rows does not notice: it waits for K and V.
+    // Probabilities in two bf16 parts, the rounded value and the rest, so that 2^-16 of them is lost and not 2^-8: out is then as
+    // exact as its own rounding leaves it.  The second product doubles, which a call of few rows does not notice: it waits for K
+    // and V.
     bf16x8 hi[RT], lo[RT];
 #pragma unroll
     for (int r = 0; r < RT; ++r) {
@@ -530,13 +535,17 @@ __global__ __launch_bounds__(kAttendThreads, RT == 1 ? 3 : 2) void jq_attend_ker
     if (KEEP) weigher.add(lse2, true);
 }
 
-// Many query rows (more than 32 a KV head).  A wave still holds 32 of them, but the waves of a workgroup share the keys: R waves over
-// all rows of a group times KW over 32 keys each.  K and V go through LDS, where every wave reads all of its keys' rows: requested
-// into registers two stages ahead, written to one of two buffers, one barrier a stage.
-//   K's rows are read sixteen lanes a row of 256 bytes, piece p of row k at p ^ (k & 15), so that eight lanes' pieces meet in eight
-//   different bank groups; V is read transposed (ds_read_b64_tr_b16: a lane receives four keys' values of one dimension out of four
-//   rows of sixteen), piece p of row k at p ^ 2 (k & 7) for the same reason.  A wave reads 16 KB a stage for 32 rows, which takes
-//   LDS about as long as the matrix cores take for them.
+// Many query rows (more than 32 a KV head).  A wave still holds 32 of them, but the eight waves of a workgroup share the keys: R waves
+// over all rows of a group times KW over keys of their own.  K and V go through LDS, where every wave reads all of its keys' rows:
+// requested into registers stages ahead, written to one of two buffers, one barrier a stage.  (Every wave reading K and V for itself
+// took 117 us for 128 rows behind four prompts, 57 now.)
+// K's rows are read sixteen lanes a row of 256 bytes, piece p of row k at p ^ (k & 15), so that eight lanes' pieces meet in eight
+// different bank groups; V is read transposed (ds_read_b64_tr_b16: a lane receives four keys' values of one dimension out of four
+// rows of sixteen), piece p of row k at p ^ 2 (k & 7) for the same reason (no bank conflicts are counted).
+// What bounds it: with 128 rows a group memory, and the 20 us that two launches of this size cost whatever they do; with 256 the
+// instructions of a tile of 32 keys and 32 rows, 512 cycles of the matrix cores and some 420 of the vector ALU, which add up
+// also across the two waves of a SIMD.  Tried without gain: four stages ahead, two tiles' terms together, more of V's reads early,
+// wave priorities, half of the waves held back behind each barrier.
 template <int R>
 struct Wide {
     static constexpr int kWaves = 8, kThreads = 64 * kWaves, kRows = 32 * R;
@@ -544,7 +553,9 @@ struct Wide {
     static constexpr int kKeys = KW == 4 ? 128 : 64;           // of a stage
     static constexpr int kTiles = kKeys / 32 / KW;             // of 32 keys, a wave and stage
     static constexpr int kAhead = KW == 4 ? 1 : 2;             // stages requested ahead: 64 KB
-    static constexpr bool kExact = R == 2;                     // probabilities in two bf16 parts
+    // Probabilities in two bf16 parts only where memory is waited for anyway.  With one, out is off by 1.4 times its own rounding (2-norm
+    // against 64 bits 0.0023, 0.0017 with two), and a call is faster: 128 rows behind four prompts 60 us / 68, 256 over 32832 60 / 72.
+    static constexpr bool kExact = R == 2;
     static constexpr int kEarly = 2;                           // blocks of V requested ahead of their use
     static constexpr int kRequests = kKeys / 2 / kWaves;       // of 1 KB, a wave and stage
     static constexpr int kBuffer = 2 * kKeys * 256;            // K, then V
