@@ -190,7 +190,7 @@ __device__ __forceinline__ void tile_step(RowState<RT>& st, KvTile& t, const Att
         if (__any(top > st.m[r] + kSlack)) {
             top = fmaxf(top, __shfl_xor(top, 16));
             top = fmaxf(top, __shfl_xor(top, 32));
-            const float to = fmaxf(st.m[r], top);
+            const float to = top > st.m[r] + kSlack ? top : st.m[r];  // (a row's bits do not depend on the others of its wave)
             const float f = st.m[r] == to ? 1.0f : __builtin_amdgcn_exp2f(st.m[r] - to);  // (-inf stays -inf: no 0 * inf)
             st.m[r] = to;
             st.z[r] *= f;
@@ -743,6 +743,10 @@ __global__ __launch_bounds__(Wide<R>::kThreads, 2) void jq_attend_wide_kernel(At
                 float to = fmaxf(max4(x[r][0]), max4(x[r][1])) * a.scale2;
                 to = fmaxf(to, __shfl_xor(to, 16));
                 to = fmaxf(m[r], fmaxf(to, __shfl_xor(to, 32)));
+                int late = !(sum[r] <= kLargeSum) || m[r] == -__builtin_inff();
+                late |= __shfl_xor(late, 16);
+                late |= __shfl_xor(late, 32);
+                if (!late) to = m[r];  // a row's bits do not depend on the others of its wave
                 const float f = m[r] == to ? 1.0f : __builtin_amdgcn_exp2f(m[r] - to);
                 m[r] = to;
                 z[r] *= f;

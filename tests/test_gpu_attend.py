@@ -205,6 +205,83 @@ def test_rising_scores():
     check(Q, K, V, cu, live, out, lse)
 
 
+@pytest.mark.parametrize("n_q", [4, 16, 32, 64])  # each way of sharing query rows and keys out
+@pytest.mark.parametrize("where", ["k", "v"])
+@pytest.mark.parametrize("value", [0x7FC0, 0xFF80])
+def test_rows_unseen_by_any_number_of_tokens_may_hold_anything(n_q, where, value):
+    import torch
+    base, h_q, h_kv = 200, 8, 2
+    rng, Q, K, V, cu, live = make(30 + n_q, 1, [base + n_q], h_q, h_kv, n_q, None)
+    seen = np.zeros((1, n_q, -(-n_q // 32)), np.uint32)
+    for i in range(n_q):
+        seen[0, i, i // 32] |= np.uint32(1 << (i % 32))
+        seen[0, i, 0] |= np.uint32(1)
+    clean = K.copy(), V.copy()
+    dirty = [j for j in (1, n_q // 2, n_q - 1)]
+    for j in dirty:
+        (K if where == "k" else V)[0, base + j, :, j % 128] = value
+    sh = jq.Shape(n_layers=1, seq_lens=[base + n_q], n_q=n_q, h_q=h_q, h_kv=h_kv)
+    mask = dev_i32(seen.view(np.int32))
+    out, lse = jq.attend_tree(sh, mask, to_dev_bf16(Q), to_dev_bf16(K), to_dev_bf16(V))
+    ref, rlse = jq.attend_tree(sh, mask, to_dev_bf16(Q), to_dev_bf16(clean[0]), to_dev_bf16(clean[1]))
+    torch.cuda.synchronize()
+    others = [i for i in range(n_q) if i not in dirty]
+    assert torch.equal(out[:, :, others], ref[:, :, others]) and torch.equal(lse[:, :, others], rlse[:, :, others])
+    check(Q, *clean, cu, live, ref, rlse, "tree", seen)
+    # the same of causal queries: those before the first dirty row do not see it
+    causal = jq.Shape(n_layers=1, seq_lens=[base + n_q], n_q=n_q, h_q=h_q, h_kv=h_kv, window=True)
+    out, lse = jq.attend(causal, to_dev_bf16(Q), to_dev_bf16(K), to_dev_bf16(V))
+    ref, rlse = jq.attend(causal, to_dev_bf16(Q), to_dev_bf16(clean[0]), to_dev_bf16(clean[1]))
+    torch.cuda.synchronize()
+    assert torch.equal(out[:, :, :1], ref[:, :, :1]) and torch.equal(lse[:, :, :1], rlse[:, :, :1])
+
+
+@pytest.mark.parametrize("n_q", [2, 16, 32, 64])
+@pytest.mark.parametrize("way", ["rising", "falling", "sawtooth", "one_late"])
+def test_scores_hundreds_of_octaves_apart(n_q, way):
+    """The running maximum has to follow, sums must neither overflow nor vanish: scores between -600 and 600."""
+    import torch
+    from workloads import f32_to_bf16_bits
+    n = 3000
+    rng, Q, K, V, cu, live = make(40, 1, [n], 8, 2, n_q, None)
+    x = np.linspace(-1, 1, n)
+    ramp = {"rising": x, "falling": -x, "sawtooth": np.where(np.arange(n) % 97 < 50, x, -x), "one_late": np.where(np.arange(n) == n - 70, 1.0, -1.0)}[way]
+    K = f32_to_bf16_bits((0.05 * f64(K[0]) + ramp[:, None, None]).astype(np.float32))[None]
+    Q = f32_to_bf16_bits((np.ones(Q.shape) * 53 + 0.2 * f64(Q)).astype(np.float32))
+    sh = jq.Shape(n_layers=1, seq_lens=[n], n_q=n_q, h_q=8, h_kv=2)
+    out, lse = jq.attend(sh, to_dev_bf16(Q), to_dev_bf16(K), to_dev_bf16(V))
+    torch.cuda.synchronize()
+    check(Q, K, V, cu, live, out, lse)
+
+
+@pytest.mark.parametrize("n_q", [1, 9, 20, 40])
+def test_nothing_live_anywhere(n_q):
+    run(41, 2, [50, 64], 8, 2, n_q, lens=np.zeros((2, 2), np.int32), weigh=n_q < 20)
+    run(42, 1, [n_q, n_q], 8, 2, n_q, mode="causal", weigh=n_q < 20)
+
+
+def test_calls_of_several_host_threads():
+    import threading
+    import torch
+    rng, Q, K, V, cu, live = make(43, 1, [5000, 77], 16, 4, 1, None)
+    sh = [jq.Shape(n_layers=1, seq_lens=[5000, 77], n_q=1, h_q=16, h_kv=4) for _ in range(4)]
+    q, k, v = to_dev_bf16(Q), to_dev_bf16(K), to_dev_bf16(V)
+    ref = jq.attend(sh[0], q, k, v)
+    torch.cuda.synchronize()
+    got = [[] for _ in sh]
+
+    def work(i):
+        side = torch.cuda.Stream()
+        for _ in range(10):
+            got[i].append(jq.attend(sh[i], q, k, v, stream=side))
+        side.synchronize()
+    threads = [threading.Thread(target=work, args=(i,)) for i in range(len(sh))]
+    [t.start() for t in threads]
+    [t.join() for t in threads]
+    torch.cuda.synchronize()
+    assert all(torch.equal(o, ref[0]) and torch.equal(e, ref[1]) for g in got for o, e in g) and all(len(g) == 10 for g in got)
+
+
 def test_many_layers_sequences_and_heads():
     run(18, 3, list(range(20, 20 + 40)), 32, 8, 1, weigh=True)
 

@@ -292,3 +292,68 @@ def test_a_decoding_loop(page):
         np.testing.assert_array_equal(rows(kc)[:40, g], kh[kept, g])
         np.testing.assert_array_equal(pos[0, g, :40].cpu().numpy(), ph[0, g, kept])
         assert set(range(L + 8, L + 12)) <= set(pos[0, g, :40].tolist())
+
+
+@pytest.mark.parametrize("page", [0, 64])
+def test_a_captured_decoding_step_replayed(page):
+    """Replacement, attention of the token and of a drafted tree, then eviction, as two captured graphs that share their workspaces:
+    every replay leaves the bits that the same calls leave eagerly on a copy of the state."""
+    import torch
+    h_q, h_kv, cap, n_draft = 8, 2, 300, 6
+    rng = np.random.default_rng(50)
+    K, V = bf16(rng, 1, cap, h_kv, 128), bf16(rng, 1, cap, h_kv, 128)
+    pages = ()
+    if page:
+        K, table = to_pages(np.random.default_rng(3), K, [cap], page, fill=0)
+        V, _ = to_pages(np.random.default_rng(3), V, [cap], page, fill=0)
+        pages = (jq.Pages(page, K.shape[1], dev_i32(table)),)
+    step = jq.Shape(n_layers=1, seq_lens=[cap], n_q=1, h_q=h_q, h_kv=h_kv, keep_first=2, keep_last=8)
+    tree = jq.Shape(n_layers=1, seq_lens=[cap], n_q=n_draft, h_q=h_q, h_kv=h_kv)
+    few = jq.Shape(n_layers=1, seq_lens=[cap], n_q=1, h_q=h_q, h_kv=h_kv, budgets=[200], keep_first=2, keep_last=8)
+    kn, vn, q = (to_dev_bf16(bf16(rng, 1, 1, h, 128)) for h in (h_kv, h_kv, h_q))
+    qt = to_dev_bf16(bf16(rng, 1, 1, n_draft, h_q, 128))
+    from decode_ref import random_tree
+    seen = dev_i32(random_tree(rng, n_draft)[None].view(np.int32))
+    ws = jq.alloc_attend_workspace(step, weights=True), jq.alloc_attend_workspace(tree), jq.alloc_evict_weight_workspace(few)
+    rep, att, atree, ev = ((jq.replace_lightest_paged, jq.attend_paged, jq.attend_tree_paged, jq.evict_weight_paged) if page else
+                           (jq.replace_lightest, jq.attend, jq.attend_tree, jq.evict_weight))
+
+    def state():
+        s = {"K": to_dev_bf16(K), "V": to_dev_bf16(V), "w": torch.linspace(0.1, 3, h_kv * cap, device="cuda").view(1, h_kv, cap).flip(-1).contiguous(),
+             "pos": torch.arange(cap, dtype=torch.int32, device="cuda").expand(1, h_kv, cap).contiguous(), "lens": dev_i32([[cap - 3]]),
+             "token": dev_i32([cap]), "slot": torch.zeros((1, 1, h_kv), dtype=torch.int32, device="cuda"), "out": torch.zeros_like(q.view(1, 1, 1, h_q, 128)),
+             "lse": torch.zeros((1, 1, 1, h_q), device="cuda"), "tout": torch.zeros_like(qt), "tlse": torch.zeros((1, 1, n_draft, h_q), device="cuda"),
+             "idx": torch.zeros((1, h_kv, 200), dtype=torch.int32, device="cuda")}
+        return s
+
+    def decode(s):
+        rep(step, *pages, kn, vn, s["token"], s["K"], s["V"], s["w"], s["pos"], lens=s["lens"], slot_out=s["slot"])
+        s["lens"].add_(1).clamp_(max=cap)
+        att(step, *pages, q.view(1, 1, 1, h_q, 128), s["K"], s["V"], lens=s["lens"], weights=s["w"], out=s["out"], lse=s["lse"], ws=ws[0])
+        atree(tree, *pages, seen, qt, s["K"], s["V"], lens=s["lens"], out=s["tout"], lse=s["tlse"], ws=ws[1])
+        s["token"].add_(1)
+
+    def prune(s):
+        ev(few, *pages, s["K"], s["V"], s["w"], s["pos"], lens=s["lens"], idx_out=s["idx"], ws=ws[2])
+        s["lens"].clamp_(max=200)
+    side = torch.cuda.Stream()
+    warm = state()
+    with torch.cuda.stream(side):
+        decode(warm), prune(warm)
+    side.synchronize()
+    a, b = state(), state()
+    graphs = []
+    for f in (decode, prune):
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, stream=side):
+            f(a)
+        graphs.append(g)
+    torch.cuda.synchronize()
+    for i, which in enumerate((0, 0, 0, 0, 0, 0, 1, 0, 0, 1, 0)):
+        graphs[which].replay()
+        torch.cuda.synchronize()
+        (decode, prune)[which](b)
+        torch.cuda.synchronize()
+        for name in a:
+            x, y = a[name], b[name]
+            assert torch.equal(x.view(torch.int16) if x.dtype == torch.bfloat16 else x, y.view(torch.int16) if y.dtype == torch.bfloat16 else y), (i, name)
