@@ -73,12 +73,15 @@ typedef enum jq_status {
     JQ_OK = 0,
     JQ_ERR_NULL = -1,        /* a required pointer is NULL                               */
     JQ_ERR_SHAPE = -2,       /* a dimension, pool_k, scale or cu_seqlens is malformed    */
-    JQ_ERR_BUDGET = -3,      /* some budget is outside 1..L_s, or below keep_first+keep_last */
+    JQ_ERR_BUDGET = -3,      /* some budget is outside 1..L_s, or below keep_first+keep_last; */
+                             /* jq_replace_lightest: nothing would be left to replace      */
     JQ_ERR_UNSUPPORTED = -4, /* valid but not implemented: d != 128, more than JQ_MAX_SEQ  */
                              /* sequences, more than 65535 layers or 256 KV heads, more    */
                              /* than 2^20 query rows per KV head, a sequence (or a layer's */
                              /* page pool) with 4 GiB or more of keys, 2^31 or more kept   */
-                             /* rows or workgroups in one call, a misaligned tensor        */
+                             /* rows or workgroups in one call, weights for more than 128  */
+                             /* query rows per KV head, more than JQ_MAX_DRAFT drafted     */
+                             /* tokens, a misaligned tensor                                */
     JQ_ERR_WORKSPACE = -5,   /* workspace missing, misaligned (16 B) or too small        */
     JQ_ERR_ALIAS = -6,       /* an output overlaps an input or another output            */
     JQ_ERR_LAUNCH = -7       /* the HIP runtime refused a launch                         */

@@ -875,11 +875,12 @@ const char* jq_status_string(int status) {
         case JQ_OK: return "ok";
         case JQ_ERR_NULL: return "a required pointer is NULL";
         case JQ_ERR_SHAPE: return "malformed shape (dimension, pool_k, scale or cu_seqlens)";
-        case JQ_ERR_BUDGET: return "a budget is outside 1..L or below keep_first + keep_last";
+        case JQ_ERR_BUDGET: return "a budget is outside 1..L or below keep_first + keep_last, or no row is left to replace";
         case JQ_ERR_UNSUPPORTED:
             return "valid but unsupported (d != 128, more than JQ_MAX_SEQ sequences, more than 65535 layers or 256 KV heads, "
                    "a sequence or a layer's page pool with 4 GiB or more of keys, more than 2^31 - 1 kept rows or "
-                   "workgroups in one call, or a misaligned tensor)";
+                   "workgroups in one call, weights for more than 128 query rows per KV head, more than JQ_MAX_DRAFT drafted tokens, "
+                   "or a misaligned tensor)";
         case JQ_ERR_WORKSPACE: return "workspace missing, misaligned or too small";
         case JQ_ERR_ALIAS: return "an output overlaps an input or another output";
         case JQ_ERR_LAUNCH: return "the HIP runtime refused a launch";

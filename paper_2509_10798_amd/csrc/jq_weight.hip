@@ -6,6 +6,8 @@
 //   jq_replace_lightest    one token: its row takes the slot of the lightest one
 //
 // Rows of the first keep_first positions and of the newest keep_last are never taken, whatever they weigh.
+#include <type_traits>
+
 #include "jq_common.h"
 
 namespace jq {
@@ -24,6 +26,7 @@ struct WeightArgs {
     int32_t* newest;
     float* cand_w; int32_t* cand_pos; int32_t* cand_row;
     int32_t n_pieces, n_cand;
+    int32_t own_newest;                        // every piece looks through all of its sequence's positions: no launch for `newest`
     int32_t cu_piece[JQ_MAX_SEQ + 1], cu_cand[JQ_MAX_SEQ + 1];
     const int32_t* layer_budgets;
     int32_t n_layers, h_kv, keep_first, keep_last;
@@ -43,20 +46,24 @@ __device__ __forceinline__ uint32_t weight_key(float w, int pos, int keep_first,
 
 // One workgroup per (layer, sequence, KV head): exact radix select over the weights' keys, 11, 11 and 10 bits, then the kept rows
 // in ascending order with their weights and positions.  Each of the sixteen waves owns a run of rows, 256 of them (four a lane) a
-// round; up to ROUNDS rounds are held in registers, which the whole selection then works on, and longer runs are read again in every
-// pass, four rounds at a time.  A histogram has four copies, by lane, since most keys of a wave fall into a few bins of the first
-// level.  Places are counted wave by wave: the only barriers are those around a histogram and one around the waves' totals.
+// round; up to ROUNDS rounds are held in registers with their keys, which the whole selection then works on, and longer runs are read
+// again in every pass, four rounds at a time.  It is one chain of waits and of instructions that four waves of a SIMD take turns
+// with (7 ns each): every level has a histogram of its own, cleared while the first rows are on their way, and three barriers; a row
+// costs some thirty instructions, places being counted by ballots, wave by wave, with one barrier around the waves' totals.
 // In place every slot written is at or before the row it comes from: what is held in registers has been read by then (one barrier),
 // and longer runs are moved by one wave after the other, each of its rounds read before it is written.
 constexpr int kWeightThreads = 1024, kWeightWaves = kWeightThreads / 64, kRoundRows = 256;
-constexpr int kWeightBins = 2048, kHistCopies = 4;
+constexpr int kWeightBins = 2048;
+constexpr int kFirstCopies = 4, kRestCopies = 2;  // of histograms, by lane: adds to one address take turns
+constexpr int kHistWords = kWeightBins * (kFirstCopies + 2 * kRestCopies);
 typedef float any_float4 __attribute__((ext_vector_type(4), aligned(4)));
 typedef int32_t any_int4 __attribute__((ext_vector_type(4), aligned(4)));
 
-// Four rows' weights and positions.
+// Four rows' weights and positions, and their keys where they are ranked.
 struct FourRows {
     float w[4];
     int32_t pos[4];
+    uint32_t key[4];
     // the rows from j on, of which there are n; without positions they are the rows' numbers, `base` for the first
     __device__ __forceinline__ void load(const float* from_w, const int32_t* from_pos, int j, int n, int base) {
         if (j + 4 <= n) {
@@ -72,6 +79,16 @@ struct FourRows {
         if (!from_pos) {
 #pragma unroll
             for (int e = 0; e < 4; ++e) pos[e] = base + j + e;
+        }
+    }
+    // Keys: above every weight's those of rows from position keep_first + inner on, and, as the difference wraps, below keep_first; 0
+    // behind the last row.  A row may have that key too; it comes before those, and never are more rows asked for than there are.
+    __device__ __forceinline__ void rank(int j, int n, int keep_first, uint32_t inner) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) key[e] = (uint32_t)pos[e] - (uint32_t)keep_first >= inner ? 0xFFFFFFFFu : sortable_key(w[e]);
+        if (j + 4 > n) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) key[e] = j + e < n ? key[e] : 0u;
         }
     }
 };
@@ -103,36 +120,55 @@ __global__ __launch_bounds__(kWeightThreads) void jq_weight_newest_kernel(Weight
 
 template <int ROUNDS, bool HELD, int STAGE>
 __global__ __launch_bounds__(kWeightThreads) void jq_weight_select_kernel(WeightArgs a) {
-    __shared__ uint32_t hist[kWeightBins * kHistCopies];
-    __shared__ uint32_t scan[kWeightWaves];
+    extern __shared__ __align__(16) uint32_t hist[];
+    __shared__ uint32_t scan[3][kWeightWaves];
     __shared__ uint2 totals[kWeightWaves];
-    __shared__ uint32_t picked[3];
+    __shared__ uint32_t picked[3][3];
     const int unit = (int)blockIdx.x / a.h_kv, g = (int)blockIdx.x - unit * a.h_kv, layer = blockIdx.y, tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int s = STAGE == kPieces ? find_seq(a.cu_piece, a.tab.n_seq, unit) : unit;
     const int cap = a.tab.cu_seq[s + 1] - a.tab.cu_seq[s];
-    const int live = live_of(a.lens, a.tab.n_seq, layer, s, cap);
-    const uint32_t B = budget_of(a.layer_budgets, a.tab, layer, s, a.keep_first + a.keep_last);
     const int64_t head = (int64_t)layer * a.h_kv + g, row0 = head * a.T + a.tab.cu_seq[s];
-    // where the rows come from, how many they are, and where those that are kept go
+    // Where the rows come from.  What is held is requested before the live count and the budget are known: rows up to the capacity are
+    // the caller's.
     const float* w = a.weights + row0;
     const int32_t* pos = a.pos ? a.pos + row0 : nullptr;
+    const int piece = STAGE == kPieces ? unit - a.cu_piece[s] : 0, base = piece * kPieceRows;
+    int room = STAGE == kPieces ? min(cap - base, kPieceRows) : cap;
+    if (STAGE == kPieces) {
+        w += base;
+        if (pos) pos += base;
+    }
+    FourRows held[ROUNDS];
+    int rounds, first;  // of a wave
+    auto read = [&](int i0) {
+#pragma unroll
+        for (int i = 0; i < ROUNDS; ++i)
+            if (i0 + i < rounds) held[i].load(w, pos, first + (i0 + i) * kRoundRows, room, base);
+    };
+    auto divide = [&]() {
+        rounds = (room + kWeightWaves * kRoundRows - 1) / (kWeightWaves * kRoundRows);
+        first = wave * rounds * kRoundRows + 4 * lane;
+    };
+    if (HELD && STAGE != kRest) {
+        divide();
+        read(0);
+    }
+    const int live = live_of(a.lens, a.tab.n_seq, layer, s, cap);
+    const uint32_t B = budget_of(a.layer_budgets, a.tab, layer, s, a.keep_first + a.keep_last);
+    // how many there are, and where those that are kept go
     const int32_t* number = nullptr;  // the rows' numbers; null: 0, 1, ...
     float* w_to = a.weights_out + row0;
     int32_t* pos_to = a.pos_out ? a.pos_out + row0 : nullptr;
     int32_t* number_to = a.idx + head * a.TB + a.tab.cu_bud[s];
-    int n = live, base = 0;
+    int n = live;
     const int per_piece = (int)min((uint32_t)kPieceRows, B);  // rows that a whole piece leaves
     const bool pieced = live > kPieceRows && (uint32_t)live > B;
     if (STAGE == kPieces) {
         if (!pieced) return;
-        const int piece = unit - a.cu_piece[s];
-        base = piece * kPieceRows;
         n = min(live - base, kPieceRows);
         if (n <= 0) return;
         const int64_t to = head * a.n_cand + a.cu_cand[s] + (int64_t)piece * per_piece;
-        w += base;
-        if (pos) pos += base;
         w_to = a.cand_w + to;
         pos_to = a.cand_pos + to;
         number_to = a.cand_row + to;
@@ -144,107 +180,121 @@ __global__ __launch_bounds__(kWeightThreads) void jq_weight_select_kernel(Weight
         number = a.cand_row + from;
         n = live / kPieceRows * per_piece + min(live % kPieceRows, per_piece);
     }
-    const int rounds = (n + kWeightWaves * kRoundRows - 1) / (kWeightWaves * kRoundRows);  // of a wave
-    const int first = wave * rounds * kRoundRows + 4 * lane;
-
-    FourRows held[ROUNDS];
-    auto read = [&](int i0) {
+    if (!HELD || STAGE == kRest) {
+        room = n;
+        divide();
+        if (HELD) read(0);
+    }
+    const bool all = (uint32_t)n <= B;
+    uint32_t inner = 0;  // positions between those that stay
+    auto rank = [&](int i0) {
 #pragma unroll
         for (int i = 0; i < ROUNDS; ++i)
-            if (i0 + i < rounds) held[i].load(w, pos, first + (i0 + i) * kRoundRows, n, base);
+            if (i0 + i < rounds) held[i].rank(first + (i0 + i) * kRoundRows, n, a.keep_first, inner);
     };
-    auto visit = [&](auto f) {  // f(row, four rows from it) for every round of the wave
+    auto visit = [&](bool ranked, auto f) {  // f(row, four rows from it) for every round of the wave
         for (int i0 = 0; i0 < (HELD ? 1 : rounds); i0 += ROUNDS) {
             if (!HELD) read(i0);
+            if (!HELD && ranked) rank(i0);
 #pragma unroll
             for (int i = 0; i < ROUNDS; ++i)
                 if (i0 + i < rounds) f(first + (i0 + i) * kRoundRows, held[i]);
         }
     };
-    if (HELD) read(0);
-    uint32_t tau = 0, ties = 0xFFFFFFFFu;  // every key above tau is kept, and the first `ties` rows of key tau
-    const bool all = (uint32_t)n <= B;
-    int64_t recent = INT64_MAX;
-    if (!all && a.keep_last > 0 && STAGE != kAllRows && pieced) {
-        int newest = live - 1;
-        if (a.pos) {
-            newest = INT32_MIN;
-            const int pieces = (live + kPieceRows - 1) / kPieceRows;
-            for (int i = lane; i < pieces; i += 64) newest = max(newest, a.newest[head * a.n_pieces + a.cu_piece[s] + i]);
-            newest = (int)(wave_max((uint32_t)newest ^ 0x80000000u) ^ 0x80000000u);
+    if (!all || STAGE == kPieces) {  // (a piece that leaves all its rows still tells the newest)
+        for (int i = tid; i < kHistWords / 4; i += kWeightThreads) ((uint4*)hist)[i] = make_uint4(0u, 0u, 0u, 0u);
+        int newest = live - 1;  // without positions
+        if (a.keep_last > 0 && a.pos) {
+            int top = INT32_MIN;
+            if (STAGE != kAllRows && pieced && !(STAGE == kPieces && a.own_newest)) {
+                const int pieces = (live + kPieceRows - 1) / kPieceRows;
+                for (int i = lane; i < pieces; i += 64) top = max(top, a.newest[head * a.n_pieces + a.cu_piece[s] + i]);
+            } else {
+                auto raise = [&](int j, const FourRows& r) {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) top = j + e < n ? max(top, r.pos[e]) : top;
+                };
+                visit(false, raise);
+                if (STAGE == kPieces) {  // the other pieces' positions
+                    const int32_t* from = pos - base;
+#pragma unroll 4
+                    for (int j = 4 * tid; j + 4 <= live; j += 4 * kWeightThreads) {
+                        const any_int4 x = *(const any_int4*)(from + j);
+                        top = max(max(max(top, x[0]), max(x[1], x[2])), x[3]);
+                    }
+                    if (tid < live % 4) top = max(top, from[live - 1 - tid]);
+                }
+                const uint32_t in_wave = wave_max((uint32_t)top ^ 0x80000000u);
+                if (lane == 0) scan[2][wave] = in_wave;
+                lds_barrier();
+                top = (int)(scan[2][lane & (kWeightWaves - 1)] ^ 0x80000000u);
+            }
+            newest = (int)(wave_max((uint32_t)top ^ 0x80000000u) ^ 0x80000000u);
+            if (STAGE == kPieces && a.own_newest && tid == 0) a.newest[head * a.n_pieces + unit] = newest;
         }
-        recent = (int64_t)newest - a.keep_last;
-    } else if (!all && a.keep_last > 0) {
-        int newest = INT32_MIN;
-        visit([&](int j, const FourRows& r) {
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-                if (j + e < n) newest = max(newest, r.pos[e]);
-        });
-        const uint32_t top = wave_max((uint32_t)newest ^ 0x80000000u);
-        if (lane == 0) scan[wave] = top;
-        __syncthreads();
-        recent = (int64_t)(int)(wave_max(scan[lane & (kWeightWaves - 1)]) ^ 0x80000000u) - a.keep_last;
+        // (all rows' positions are at most `newest` where any stay for being new, so none is keep_first + inner by wrapping)
+        const int64_t between = (int64_t)newest - a.keep_last - a.keep_first + 1;
+        inner = all ? 0u : a.keep_last == 0 ? 0x80000000u - (uint32_t)a.keep_first : (uint32_t)max(between, (int64_t)0);
     }
-    auto key = [&](const FourRows& r, int e) { return weight_key(r.w[e], r.pos[e], a.keep_first, recent); };
+    if (HELD) rank(0);
+    uint32_t tau = 0, ties = 0;  // every key above tau is kept, and the first `ties` rows of key tau
     if (!all) {
-        uint32_t left = B, prefix = 0, mask = 0;  // places left among the keys that agree with prefix under mask
-#pragma unroll 1
-        for (int level = 0; level < 3; ++level) {
-            const int shift = level == 0 ? 21 : level == 1 ? 10 : 0;
-            const uint32_t bins = level == 2 ? 1024 : 2048;
-            __syncthreads();
-            for (int i = tid; i < kWeightBins * kHistCopies / 4; i += kWeightThreads) ((uint4*)hist)[i] = make_uint4(0u, 0u, 0u, 0u);
-            __syncthreads();
-            visit([&](int j, const FourRows& r) {
+        uint32_t left = B;  // places left among the keys that agree with tau under the levels' bits so far
+        lds_barrier();      // histograms are clear
+        auto level = [&](auto which) {  // true: no row of the bin that is found goes
+            constexpr int L = decltype(which)::value, shift = L == 0 ? 21 : L == 1 ? 10 : 0, copies = L == 0 ? kFirstCopies : kRestCopies;
+            constexpr uint32_t bins = L == 2 ? 1024 : 2048, mask = L == 0 ? 0u : L == 1 ? 0xFFE00000u : 0xFFFFFC00u;
+            uint32_t* h = hist + (L == 0 ? 0 : kWeightBins * (kFirstCopies + (L - 1) * kRestCopies)), *mine = h + (lane & (copies - 1));
+            visit(true, [&](int j, const FourRows& r) {
+                if (j < n) {
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const uint32_t k = key(r, e);
-                    if (j + e < n && (k & mask) == prefix) atomicAdd(&hist[((k >> shift) & (bins - 1)) * kHistCopies + (lane & (kHistCopies - 1))], 1u);
+                    for (int e = 0; e < 4; ++e)
+                        if (L == 0 || (r.key[e] & mask) == tau) atomicAdd(mine + ((r.key[e] >> shift) & (bins - 1)) * copies, 1u);
                 }
             });
-            __syncthreads();
+            lds_barrier();
             // two bins a thread, from the largest down: the one in which the running count passes `left`
-            uint32_t c[2];
+            uint32_t c[2] = {0, 0};
 #pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                const uint4 h = ((const uint4*)hist)[kWeightBins - 1 - (2 * tid + e)];
-                c[e] = h.x + h.y + h.z + h.w;
+            for (int i = 0; i < copies; ++i) {
+                const uint32_t* two = h + (kWeightBins - 2 - 2 * tid) * copies;
+                c[0] += two[copies + i];
+                c[1] += two[i];
             }
-            uint32_t total;
-            const uint32_t upto = block_scan_incl<kWeightThreads>(c[0] + c[1], scan, &total), before = upto - c[0] - c[1];
+            auto add = [](uint32_t x, uint32_t y) { return x + y; };
+            const uint32_t in_wave = wave_scan(c[0] + c[1], 0u, add);
+            if (lane == 63) scan[L & 1][wave] = in_wave;
+            lds_barrier();
+            const uint32_t waves = row_scan(lane < kWeightWaves ? scan[L & 1][lane] : 0u, 0u, add);
+            const uint32_t upto = in_wave + (wave > 0 ? (uint32_t)__builtin_amdgcn_readlane((int)waves, wave > 0 ? wave - 1 : 0) : 0u), before = upto - c[0] - c[1];
             if (before < left && left <= upto) {
                 const bool upper = left <= before + c[0];
-                picked[0] = kWeightBins - 1 - (2 * tid + (upper ? 0 : 1));
-                picked[1] = left - before - (upper ? 0u : c[0]);
-                picked[2] = c[upper ? 0 : 1];
+                picked[L][0] = kWeightBins - 1 - (2 * tid + (upper ? 0 : 1));
+                picked[L][1] = left - before - (upper ? 0u : c[0]);
+                picked[L][2] = c[upper ? 0 : 1];
             }
-            __syncthreads();
-            prefix |= picked[0] << shift;
-            mask |= (bins - 1) << shift;
-            left = picked[1];
-            if (left == picked[2] && prefix) {  // the whole bin stays, as it mostly does from the second level on: it often holds one row
-                prefix -= 1;
-                left = 0;
-                break;
-            }
+            lds_barrier();
+            tau |= picked[L][0] << shift;
+            left = picked[L][1];
+            return left == picked[L][2] && tau;
+        };
+        // The whole bin stays, as it mostly does from the second level on: it often holds one row.
+        if (level(std::integral_constant<int, 0>()) || level(std::integral_constant<int, 1>()) || level(std::integral_constant<int, 2>())) {
+            tau -= 1;
+            left = 0;
         }
-        tau = prefix;
         ties = left;
     }
     // What every wave keeps for certain, and its ties.
     uint32_t sure = 0, tied = 0;
-    visit([&](int j, const FourRows& r) {
+    visit(true, [&](int, const FourRows& r) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const uint32_t k = key(r, e);
-            sure += j + e < n && (all || k > tau);
-            tied += j + e < n && !all && k == tau;
+        for (int e = 0; e < 4; ++e) sure += (uint32_t)__popcll(__ballot(r.key[e] > tau));
+        if (ties > 0) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) tied += (uint32_t)__popcll(__ballot(r.key[e] == tau));
         }
     });
-    auto add = [](uint32_t x, uint32_t y) { return x + y; };
-    sure = (uint32_t)__builtin_amdgcn_readlane((int)wave_scan(sure, 0u, add), 63);
-    tied = (uint32_t)__builtin_amdgcn_readlane((int)wave_scan(tied, 0u, add), 63);
     if (lane == 0) totals[wave] = make_uint2(sure, tied);
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // what is held has been read, by every wave
     __syncthreads();
@@ -255,39 +305,45 @@ __global__ __launch_bounds__(kWeightThreads) void jq_weight_select_kernel(Weight
         sure_before += i < wave ? t.x : 0u;
         ties_before += i < wave ? t.y : 0u;
     }
+    auto lower = [](uint64_t votes, uint32_t from) {  // `from` and the votes of lower lanes
+        return __builtin_amdgcn_mbcnt_hi((uint32_t)(votes >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)votes, from));
+    };
     auto emit = [&](int j, const FourRows& r) {
-        uint32_t is_sure = 0, is_tie = 0;
+        uint32_t s0 = sure_before, t0 = ties_before;
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            const uint32_t k = key(r, e);
-            is_sure |= (uint32_t)(j + e < n && (all || k > tau)) << e;
-            is_tie |= (uint32_t)(j + e < n && !all && k == tau) << e;
+            const uint64_t votes = __ballot(r.key[e] > tau);
+            s0 = lower(votes, s0);
+            sure_before += (uint32_t)__popcll(votes);
         }
-        const uint32_t mine = (uint32_t)__popc(is_sure) | (uint32_t)__popc(is_tie) << 16, upto = wave_scan(mine, 0u, add);
-        uint32_t s0 = sure_before + ((upto - mine) & 0xFFFFu), t0 = ties_before + ((upto - mine) >> 16);
+        if (ties > 0) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const uint64_t votes = __ballot(r.key[e] == tau);
+                t0 = lower(votes, t0);
+                ties_before += (uint32_t)__popcll(votes);
+            }
+        }
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            const bool surely = is_sure >> e & 1u, tie = is_tie >> e & 1u;
-            const uint32_t slot = s0 + min(t0, ties);
+            const bool surely = r.key[e] > tau, tie = r.key[e] == tau;
+            const uint32_t to = 4 * (s0 + min(t0, ties));  // (32 bits: fewer than 2^30 rows fit 4 GiB of keys)
             if (surely || (tie && t0 < ties)) {
-                number_to[slot] = number ? number[j + e] : base + j + e;
-                w_to[slot] = r.w[e];
-                if (pos_to) pos_to[slot] = r.pos[e];
+                *(int32_t*)((char*)number_to + to) = number ? number[j + e] : base + j + e;
+                *(float*)((char*)w_to + to) = r.w[e];
+                if (pos_to) *(int32_t*)((char*)pos_to + to) = r.pos[e];
             }
             s0 += surely;
             t0 += tie;
         }
-        const uint32_t round = (uint32_t)__builtin_amdgcn_readlane((int)upto, 63);
-        sure_before += round & 0xFFFFu;
-        ties_before += round >> 16;
     };
     if (HELD || w_to != w) {
-        visit(emit);
+        visit(true, emit);
         return;
     }
     for (int turn = 0; turn < kWeightWaves; ++turn) {
         // (a visit reads its next rounds before it writes into earlier rows only)
-        if (turn == wave) visit(emit);
+        if (turn == wave) visit(true, emit);
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         __syncthreads();
     }
@@ -423,7 +479,7 @@ __global__ __launch_bounds__(kReplaceThreads) void jq_replace_kernel(ReplaceArgs
 // ---- host ------------------------------------------------------------------------------------------------------------------
 
 // Pieces or not: with pieces the last selection reads pieces * budget rows of every long sequence instead of all.  They are taken where
-// that at least halves what it reads (65536 rows, 2048 kept, 8 heads: 40 us a call with pieces, 73 without).
+// that at least halves what it reads (65536 rows, 2048 kept, 8 heads: 31 us a call with pieces, 64 without).
 void plan_evict_weight(const Plan& p, WeightPlan* wp) {
     auto up = [](size_t x) { return (x + 255) / 256 * 256; };
     wp->cu_piece[0] = wp->cu_cand[0] = 0;
@@ -452,6 +508,19 @@ void plan_evict_weight(const Plan& p, WeightPlan* wp) {
     wp->ws_bytes = wp->off_cand + up(heads * wp->cu_cand[p.n_seq] * 3 * sizeof(int32_t));
 }
 
+// Up to this many pieces each of them reads the others' positions too: with four 2 us longer, where the launch that finds the pieces'
+// largest takes 4.5 and a gap.  (What they read together grows with the square of the pieces.)
+constexpr int kOwnNewest = 8;
+
+template <int ROUNDS, bool HELD, int STAGE>
+static hipError_t launch_select(const WeightArgs& a, dim3 grid, hipStream_t st) {
+    constexpr int lds = kHistWords * 4;
+    static std::atomic<uint64_t> done{0};
+    const hipError_t e = allow_dynamic_lds((const void*)jq_weight_select_kernel<ROUNDS, HELD, STAGE>, lds, done);
+    if (e != hipSuccess) return e;
+    return launch_kernel(jq_weight_select_kernel<ROUNDS, HELD, STAGE>, grid, dim3(kWeightThreads), lds, st, nullptr, -1, a);
+}
+
 hipError_t launch_evict_weight(const Plan& p, const WeightPlan& wp, const int32_t* lens, const void* K, const void* V, const float* weights, const int32_t* pos,
                                void* K_out, void* V_out, float* weights_out, int32_t* pos_out, int32_t* idx, char* ws, hipStream_t st) {
     WeightArgs a{};
@@ -469,16 +538,16 @@ hipError_t launch_evict_weight(const Plan& p, const WeightPlan& wp, const int32_
     const dim3 whole((unsigned)(p.n_seq * p.h_kv), (unsigned)p.n_layers), pieces((unsigned)(a.n_pieces * p.h_kv), (unsigned)p.n_layers), block(kWeightThreads);
     hipError_t e = hipSuccess;
     if (a.n_pieces > 0) {
-        if (pos && p.keep_last > 0) e = launch_kernel(jq_weight_newest_kernel, pieces, block, 0, st, nullptr, -1, a);
-        if (e == hipSuccess) e = launch_kernel(jq_weight_select_kernel<4, true, kPieces>, pieces, block, 0, st, nullptr, -1, a);
-        if (e == hipSuccess)
-            e = launch_kernel(wp.most_rows <= kPieceRows ? jq_weight_select_kernel<4, true, kRest> : jq_weight_select_kernel<4, false, kRest>, whole, block, 0, st,
-                              nullptr, -1, a);
+        int32_t most = 0;
+        for (int s = 0; s < p.n_seq; ++s) most = std::max(most, wp.cu_piece[s + 1] - wp.cu_piece[s]);
+        a.own_newest = most <= kOwnNewest;
+        if (pos && p.keep_last > 0 && !a.own_newest) e = launch_kernel(jq_weight_newest_kernel, pieces, block, 0, st, nullptr, -1, a);
+        if (e == hipSuccess) e = launch_select<4, true, kPieces>(a, pieces, st);
+        if (e == hipSuccess) e = wp.most_rows <= kPieceRows ? launch_select<4, true, kRest>(a, whole, st) : launch_select<4, false, kRest>(a, whole, st);
     } else {
-        e = launch_kernel(wp.most_rows <= kPieceRows / 4 ? jq_weight_select_kernel<1, true, kAllRows>
-                          : wp.most_rows <= kPieceRows   ? jq_weight_select_kernel<4, true, kAllRows>
-                                                         : jq_weight_select_kernel<4, false, kAllRows>,
-                          whole, block, 0, st, nullptr, -1, a);
+        e = wp.most_rows <= kPieceRows / 4 ? launch_select<1, true, kAllRows>(a, whole, st)
+            : wp.most_rows <= kPieceRows   ? launch_select<4, true, kAllRows>(a, whole, st)
+                                           : launch_select<4, false, kAllRows>(a, whole, st);
     }
     if (e != hipSuccess) return e;
     if (K_out == K)

@@ -175,6 +175,27 @@ def test_sequences_selected_in_pieces(inplace, with_pos):
           with_pos=with_pos)
 
 
+def test_a_sequence_of_many_pieces():
+    evict(16, 1, [150_001, 16_385], [700, 90], 1, inplace=True, first=3, last=70, order="scrambled")
+
+
+@pytest.mark.parametrize("first,last", [(0, 0), (3, 0), (0, 5), (3, 5)])
+@pytest.mark.parametrize("L", [700, 40_000])
+def test_positions_at_the_ends_of_their_type(L, first, last):
+    import torch
+    rng, K, V, w, pos = cache(17, 1, [L], 1, order="scrambled")
+    at = rng.permutation(L)
+    pos[0, 0, at[:6]] = np.array([2 ** 31 - 1, 2 ** 31 - 2, -1, -2 ** 31, -2 ** 31 + 1, 2 ** 31 - 7], np.int64).astype(np.int32)
+    for p in (pos, np.minimum(pos, 9), np.where(pos < 0, pos, -2 ** 31).astype(np.int32)):  # of the last, more are protected than stay
+        sh = jq.Shape(n_layers=1, seq_lens=[L], n_q=1, h_q=1, h_kv=1, budgets=[100], keep_first=first, keep_last=last)
+        *_, idx = jq.evict_weight(sh, to_dev_bf16(K), to_dev_bf16(V), dev_f32(w), dev_i32(p))
+        torch.cuda.synchronize()
+        q = p[0, 0].astype(np.int64)
+        stay = np.flatnonzero((q < first) | (q > q.max() - last))
+        want = stay[:100] if stay.size > 100 else evict_order(w[0, 0], q, L, 100, first, last)
+        np.testing.assert_array_equal(idx[0, 0].cpu().numpy(), want)
+
+
 def test_long_sequence_that_keeps_most_of_its_rows():
     evict(14, 1, [40000], [30000], 1, inplace=True, first=2, last=5)
     evict(15, 1, [40000], [30000], 1, ties=True, page=64, lens=np.array([[33333]], np.int32))
