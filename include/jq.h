@@ -422,8 +422,9 @@ int jq_attend_tree_paged(const jq_shape* shape, const jq_pages* pages, const int
  * them may be the inputs themselves -- the eviction then needs no second cache -- or none may overlap any input.
  * A sequence of no more live rows than its budget keeps them all.  Rows and slots behind the kept ones are left as
  * they were; the caller sets lens to min(lens, budget).  idx_out may be NULL.  Paged: the outputs are pools of the
- * inputs' shape behind the same block table, and no page may belong to two sequences.  shape->window must be 0; pool_k, n_q, h_q and scale (beyond their checks) do not matter.
- * `ws` must hold jq_evict_weight_workspace_bytes. */
+ * inputs' shape behind the same block table, and no page may belong to two sequences.  Where positions repeat, so that
+ * more rows are protected than the budget, the lowest of them stay.  shape->window must be 0; pool_k, n_q, h_q and scale
+ * (beyond their checks) do not matter.  `ws` must hold jq_evict_weight_workspace_bytes. */
 int jq_evict_weight_workspace_bytes(const jq_shape* shape, size_t* bytes);
 int jq_evict_weight(const jq_shape* shape, const int32_t* lens, const void* K, const void* V, const float* weights,
                     const int32_t* pos, void* K_out, void* V_out, float* weights_out, int32_t* pos_out,
@@ -437,8 +438,9 @@ int jq_evict_weight_paged(const jq_shape* shape, const jq_pages* pages, const in
  * appended; then it takes the place of the head's lightest row (ties: the lowest), never one of a position below
  * keep_first or above token[s] - keep_last: keep_first + max(keep_last, 1) <= L_s, otherwise JQ_ERR_BUDGET.  The row's
  * weight starts at 0 and its position is token[s].  slot_out (DEVICE int32 [n_layers, n_seq, h_kv], may be NULL) takes
- * the row's number.  shape->window must be 0; no page may belong to two sequences.  The caller sets lens to min(lens + 1, L_s) before the next call.  Rows are no longer in the order of
- * their positions then: pos says which they are, to jq_evict_weight too. */
+ * the row's number.  shape->window must be 0; no page may belong to two sequences.  The caller sets lens to
+ * min(lens + 1, L_s) before the next call.  Rows are no longer in the order of their positions then: pos says which they
+ * are, to jq_evict_weight too. */
 int jq_replace_lightest(const jq_shape* shape, const int32_t* lens, const void* k_new, const void* v_new,
                         const int32_t* token, void* K, void* V, float* weights, int32_t* pos, int32_t* slot_out,
                         void* stream);

@@ -479,7 +479,7 @@ __global__ __launch_bounds__(kReplaceThreads) void jq_replace_kernel(ReplaceArgs
 // ---- host ------------------------------------------------------------------------------------------------------------------
 
 // Pieces or not: with pieces the last selection reads pieces * budget rows of every long sequence instead of all.  They are taken where
-// that at least halves what it reads (65536 rows, 2048 kept, 8 heads: 31 us a call with pieces, 64 without).
+// that at least halves what it reads (65536 rows, 2048 kept, 8 heads: 30 us a call with pieces, 66 without).
 void plan_evict_weight(const Plan& p, WeightPlan* wp) {
     auto up = [](size_t x) { return (x + 255) / 256 * 256; };
     wp->cu_piece[0] = wp->cu_cand[0] = 0;
@@ -508,9 +508,9 @@ void plan_evict_weight(const Plan& p, WeightPlan* wp) {
     wp->ws_bytes = wp->off_cand + up(heads * wp->cu_cand[p.n_seq] * 3 * sizeof(int32_t));
 }
 
-// Up to this many pieces each of them reads the others' positions too: with four 2 us longer, where the launch that finds the pieces'
-// largest takes 4.5 and a gap.  (What they read together grows with the square of the pieces.)
-constexpr int kOwnNewest = 8;
+// Up to this many pieces each of them reads the others' positions too, instead of a launch that finds every piece's largest (us a call,
+// 8 heads: four pieces 30.1, with the launch 32.0; eight 37.2 / 37.4, of four layers 51.9 / 51.6).
+constexpr int kOwnNewest = 4;
 
 template <int ROUNDS, bool HELD, int STAGE>
 static hipError_t launch_select(const WeightArgs& a, dim3 grid, hipStream_t st) {
