@@ -378,3 +378,45 @@ def test_a_captured_decoding_step_replayed(page):
         for name in a:
             x, y = a[name], b[name]
             assert torch.equal(x.view(torch.int16) if x.dtype == torch.bfloat16 else x, y.view(torch.int16) if y.dtype == torch.bfloat16 else y), (i, name)
+
+
+def test_offsets_past_32_bits():
+    """Two sequences of more than 2 GiB of keys each: their last rows are attended to by many query rows, appended and kept."""
+    import torch
+    caps, h_kv, h_q, n_q, B = [1_200_003, 1_100_001], 8, 32, 10, 8
+    T = sum(caps)
+    K = torch.zeros((1, T, h_kv, 128), dtype=torch.bfloat16, device="cuda")
+    V = torch.zeros_like(K)
+    w, pos = torch.zeros((1, h_kv, T), device="cuda"), torch.arange(T, dtype=torch.int32, device="cuda").expand(1, h_kv, T).contiguous()
+    gen = torch.Generator(device="cuda").manual_seed(18)
+    new = [torch.randn((1, 2, h_kv, 128), generator=gen, device="cuda").to(torch.bfloat16) for _ in range(2)]
+    new[0].fill_(4.0)
+    cu = [0, caps[0], T]
+    lens = torch.tensor([[c - 1 for c in caps]], dtype=torch.int32, device="cuda")
+    token = torch.tensor([2 ** 30, 2 ** 30 + 1], dtype=torch.int32, device="cuda")
+    sh = jq.Shape(n_layers=1, seq_lens=caps, n_q=n_q, h_q=h_q, h_kv=h_kv, budgets=[B, B])
+    slot = jq.replace_lightest(sh, *new, token, K, V, w, pos, lens=lens)
+    # scores: 45 for the new row, 0 for the others, which together weigh 4e-14 of it
+    Q = torch.ones((1, 2, n_q, h_q, 128), dtype=torch.bfloat16, device="cuda")
+    out, lse = jq.attend(sh, Q, K, V, weights=w)
+    torch.cuda.synchronize()
+    for s in range(2):
+        assert (slot[0, s] == caps[s] - 1).all()
+        assert torch.equal(K[0, cu[s + 1] - 1], new[0][0, s]) and torch.equal(V[0, cu[s + 1] - 1], new[1][0, s])
+        assert (pos[0, :, cu[s + 1] - 1] == 2 ** 30 + s).all()
+        want = new[1][0, s].repeat_interleave(h_q // h_kv, 0).expand(n_q, h_q, 128)
+        assert torch.equal(out[0, s], want)
+        assert (lse[0, s] - 4 * 128 / 128 ** 0.5).abs().max() < 1e-4
+        assert (w[0, :, cu[s + 1] - 1] - n_q * h_q // h_kv).abs().max() < 1e-3
+    last = torch.arange(B, device="cuda")
+    for s in range(2):  # the last rows stand out, and stay
+        K[0, cu[s + 1] - B:cu[s + 1]] = (1 + last + 100 * s).to(torch.bfloat16)[:, None, None]
+        V[0, cu[s + 1] - B:cu[s + 1]] = -(1 + last + 100 * s).to(torch.bfloat16)[:, None, None]
+        w[0, :, cu[s + 1] - B:cu[s + 1]] = 50.0 + last
+    *_, idx = jq.evict_weight(sh, K, V, w, pos)
+    torch.cuda.synchronize()
+    for s in range(2):
+        assert torch.equal(idx[0, :, s * B:(s + 1) * B], (caps[s] - B + last).to(torch.int32).expand(h_kv, B))
+        rows = (1 + last + 100 * s).to(torch.bfloat16)[:, None, None].expand(B, h_kv, 128)
+        assert torch.equal(K[0, cu[s]:cu[s] + B], rows) and torch.equal(V[0, cu[s]:cu[s] + B], -rows)
+        assert not K[0, cu[s] + B:cu[s + 1] - B].any()
