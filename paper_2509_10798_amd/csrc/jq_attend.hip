@@ -91,8 +91,94 @@ constexpr float kLn2 = 0.69314718055994531f;
 
 __device__ __forceinline__ float max4(f32x4 x) { return fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])); }
 
+// What sums are multiplied by when their row's maximum moves.  Never 0, so that an infinity among them stays one: 2^-126 of sums that
+// this happens to is nothing beside the new ones.
+__device__ __forceinline__ float rescale(float from, float to) { return from == to ? 1.0f : __builtin_amdgcn_exp2f(fmaxf(from - to, -126.0f)); }
+
+// Values of V that are not finite.  They make the outputs of their own dimension, of the rows that see their key, infinite or NaN, and
+// reach nothing else: log-sum-exps and weights are functions of Q and K.  In the products they would reach rows that do not see
+// them (0 * inf), so tiles that some row does not see whole are cleared of them; in the others they spoil their own dimension, but a
+// second part of a probability that is 0 or negative makes a NaN of an infinity.  So a wave that has cleared any, or ends with a
+// sum that is not finite though its row's terms are, reads its V once more and marks those outputs by the definition alone
+// (mark_kinds).  Other calls pay for the look at their sums.
 __device__ __forceinline__ bool finite_pair(uint32_t x) {  // neither bf16 of the pair is infinite or NaN
     return (x & 0x7F80u) != 0x7F80u && (x & 0x7F800000u) != 0x7F800000u;
+}
+__device__ __forceinline__ bool finite_piece(au32x4 x) { return finite_pair(x[0]) && finite_pair(x[1]) && finite_pair(x[2]) && finite_pair(x[3]); }
+__device__ __forceinline__ au32x4 cleared(au32x4 x) {  // zeros for what is not finite
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+        const uint32_t low = (x[w] & 0x7F80u) == 0x7F80u ? 0u : x[w] & 0xFFFFu, high = (x[w] & 0x7F800000u) == 0x7F800000u ? 0u : x[w] & 0xFFFF0000u;
+        x[w] = low | high;
+    }
+    return x;
+}
+template <int N>
+__device__ __forceinline__ bool all_finite(const f32x4 (&o)[N]) {
+    float x = 0.0f;
+#pragma unroll
+    for (int d = 0; d < N; ++d)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x = __builtin_fmaf(o[d][e], 0.0f, x);
+    return x == 0.0f;
+}
+__device__ __forceinline__ float sum_of_row(float z) {  // over the four lanes of a query row
+    z += __shfl_xor(z, 16);
+    return z + __shfl_xor(z, 32);
+}
+
+// The marks of a wave's row tiles, in the layout of their sums: 0, or what stands in for the sum.  Kinds are counted by a product
+// over 32 keys: 1 for a NaN, 64 for +inf, 4096 for -inf times 1 where a row sees the key, so that its sums are exact whole numbers.
+// tile(i): first key of the wave's tile i, -1 behind the last; row(key): its row of V; sees(r, key): of the lane's query row in
+// row tile r; dim(d): the lane's dimension of the left operand in block d.
+template <int RT, class Tile, class Row, class Sees, class Dim>
+__device__ __forceinline__ void mark_kinds(f32x4 (&marks)[RT][8], const char* V, uint32_t stride, int n, int lane, Tile tile, Row row, Sees sees, Dim dim) {
+#pragma unroll
+    for (int r = 0; r < RT; ++r)
+#pragma unroll
+        for (int d = 0; d < 8; ++d) marks[r][d] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    for (int i = 0, key0 = tile(0); key0 >= 0; key0 = tile(++i)) {
+        const uint32_t row0 = row(key0);
+        uint32_t at[8];  // the rows of the lane's eight keys; those behind the last are nobody's to see
+        bool ok = true;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            at[k] = (row0 + (uint32_t)min(16 * (k >> 2) + 4 * (lane >> 4) + (k & 3), n - 1 - key0)) * stride;
+            ok = ok && finite_piece(*(const au32x4*)(V + (at[k] + (uint32_t)(lane & 15) * 16u)));
+        }
+        if (!__any(!ok)) continue;
+        au32x4 seen[RT];
+#pragma unroll
+        for (int r = 0; r < RT; ++r)
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                const int key = key0 + 16 * (k >> 2) + 4 * (lane >> 4) + (k & 3);
+                const uint32_t one = sees(r, key) ? 0x3F80u : 0u;
+                seen[r][k >> 1] = k & 1 ? seen[r][k >> 1] | one << 16 : one;
+            }
+#pragma unroll
+        for (int d = 0; d < 8; ++d) {
+            au32x4 kinds;
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                const uint32_t x = *(const uint16_t*)(V + (at[k] + (uint32_t)dim(d) * 2u));
+                const uint32_t kind = (x & 0x7F80u) != 0x7F80u ? 0u : x & 0x7Fu ? 0x3F80u : x & 0x8000u ? 0x4580u : 0x4280u;
+                kinds[k >> 1] = k & 1 ? kinds[k >> 1] | kind << 16 : kind;
+            }
+#pragma unroll
+            for (int r = 0; r < RT; ++r) {
+                const f32x4 count = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kinds), __builtin_bit_cast(bf16x8, seen[r]),
+                                                                            f32x4{0.0f, 0.0f, 0.0f, 0.0f}, 0, 0, 0);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const int c = (int)count[e];
+                    const float nan = c & 63 ? __builtin_nanf("") : 0.0f, up = c & 0xFC0 ? __builtin_inff() : 0.0f, down = c >> 12 ? __builtin_inff() : 0.0f;
+                    marks[r][d][e] += nan + up - down;
+                }
+            }
+            __builtin_amdgcn_sched_barrier(0);  // (all blocks' comparisons together do not fit the scalar registers)
+        }
+    }
 }
 
 // 32 keys of K and V in registers: k[t][c] is chunk c (32 of the 128 dimensions) of key 16 t + l % 16, v[t][e] 8 dimensions of key
@@ -127,26 +213,34 @@ struct RowState {
     float m[RT], z[RT];  // running maximum (the same in the four lanes of a row) and the lane's own share of the sum
 };
 
+// Whether a query row sees a key.  Without branches, and what depends on it is selected: of branches around stores to elements of a
+// vector the compiler (ROCm 7.2) has lost the store.
+template <int MASK>
+__device__ __forceinline__ bool row_sees(const AttendArgs& a, int key, int n, int row_limit, const uint32_t* row_seen) {
+    if (MASK == kSeeAll) return key < n;
+    if (MASK == kSeeCausal) return key < min(n, row_limit);
+    const int j = key - (n - a.n_q);
+    const uint32_t bit = row_seen[min(max(j, 0), a.n_q - 1) >> 5] >> (j & 31) & 1u;
+    return (key < n) & ((j < 0) | (bit != 0));
+}
+
 // One tile of 32 keys.  MASKED: some row may not see some key of it, or the tile reaches past the live rows.
 template <int RT, bool MASKED, int MASK, bool KEEP>
 __device__ __forceinline__ void tile_step(RowState<RT>& st, KvTile& t, const AttendArgs& a, int lane, int key0, int n, const int* row_limit,
-                                          const uint32_t* const* row_seen, float* hold) {
-    uint32_t bad[2][4];  // keys whose V is not finite, by the lanes that hold their 16 pieces
+                                          const uint32_t* const* row_seen, float* hold, bool* was_cleared) {
     if (MASKED) {
-        // What a query row does not see must not reach it, not even times zero: such values count as zeros, and every row
-        // that does see the key gets a NaN for its score instead.
+        bool ok = true;
 #pragma unroll
         for (int i = 0; i < 2; ++i)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                bool ok = true;
+            for (int e = 0; e < 4; ++e) ok = ok && finite_piece(t.v[i][e]);
+        if (__any(!ok)) {
+            *was_cleared = true;
 #pragma unroll
-                for (int w = 0; w < 4; ++w) ok = ok && finite_pair(t.v[i][e][w]);
-                const uint64_t votes = __ballot(!ok);
-                bad[i][e] = (uint32_t)(votes >> (16 * (lane >> 4))) & 0xFFFFu;
-                if (bad[i][e])
-                    t.v[i][e] = au32x4{0u, 0u, 0u, 0u};
-            }
+            for (int i = 0; i < 2; ++i)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) t.v[i][e] = cleared(t.v[i][e]);
+        }
     }
     f32x4 s[RT][2];
 #pragma unroll
@@ -166,13 +260,7 @@ __device__ __forceinline__ void tile_step(RowState<RT>& st, KvTile& t, const Att
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     const int key = key0 + 16 * i + 4 * (lane >> 4) + e;
-                    bool see = key < n;
-                    if (MASK == kSeeCausal) see = key < row_limit[r];
-                    if (MASK == kSeeTree) {
-                        const int j = key - (n - a.n_q);
-                        if (see && j >= 0) see = (row_seen[r][j >> 5] >> (j & 31)) & 1u;
-                    }
-                    s[r][i][e] = see ? (bad[i][e] ? __builtin_nanf("") : s[r][i][e]) : -__builtin_inff();
+                    s[r][i][e] = row_sees<MASK>(a, key, n, row_limit[r], row_seen[r]) ? s[r][i][e] : -__builtin_inff();
                 }
     }
     if (KEEP) {  // `hold`: the lane's place in the tile's part of the held logits
@@ -191,7 +279,7 @@ __device__ __forceinline__ void tile_step(RowState<RT>& st, KvTile& t, const Att
             top = fmaxf(top, __shfl_xor(top, 16));
             top = fmaxf(top, __shfl_xor(top, 32));
             const float to = top > st.m[r] + kSlack ? top : st.m[r];  // (a row's bits do not depend on the others of its wave)
-            const float f = st.m[r] == to ? 1.0f : __builtin_amdgcn_exp2f(st.m[r] - to);  // (-inf stays -inf: no 0 * inf)
+            const float f = rescale(st.m[r], to);
             st.m[r] = to;
             st.z[r] *= f;
 #pragma unroll
@@ -365,24 +453,42 @@ __global__ __launch_bounds__(kAttendThreads, RT == 1 ? 3 : 2) void jq_attend_ker
     // out as they are formed they kept reads from being under way: 32 sequences of 2048 rows 71.7 us a call, without weights 58.3.)
     float* held = (float*)(lds_stats + kAttendWaves * RT * kTileRows);
     float* hold = KEEP ? held + (lane & 15) * a.hold_keys + 32 * wave + 4 * (lane >> 4) : nullptr;
+    bool was_cleared = false;
     while (key + 32 <= open) {
-        tile_step<RT, false, MASK, KEEP>(st, t, a, lane, key, n, row_limit, row_seen, hold);
+        tile_step<RT, false, MASK, KEEP>(st, t, a, lane, key, n, row_limit, row_seen, hold, &was_cleared);
         if (KEEP) hold += 32 * kAttendWaves;
         key += step;
         if (key < n) load_tile(t, K, V, tile_row(key), n - 1 - key, stride, lane);
     }
     while (key < n) {
-        tile_step<RT, true, MASK, KEEP>(st, t, a, lane, key, n, row_limit, row_seen, hold);
+        tile_step<RT, true, MASK, KEEP>(st, t, a, lane, key, n, row_limit, row_seen, hold, &was_cleared);
         if (KEEP) hold += 32 * kAttendWaves;
         key += step;
         if (key < n) load_tile(t, K, V, tile_row(key), n - 1 - key, stride, lane);
     }
 
+    bool marked = was_cleared;
+#pragma unroll
+    for (int r = 0; r < RT; ++r) {
+        st.z[r] = sum_of_row(st.z[r]);
+        marked |= st.z[r] < __builtin_inff() && !all_finite(st.o[r]);
+    }
+    if (__any(marked)) {
+        f32x4 marks[RT][8];
+        auto tile = [&](int i) { const int k = 32 * (kAttendWaves * mine + wave) + i * step; return k < n ? k : -1; };
+        auto sees = [&](int r, int k) { return row_sees<MASK>(a, k, n, row_limit[r], row_seen[r]); };
+        mark_kinds<RT>(marks, V, stride, n, lane, tile, tile_row, sees, [&](int d) { return 8 * (lane & 15) + d; });
+#pragma unroll
+        for (int r = 0; r < RT; ++r)
+#pragma unroll
+            for (int d = 0; d < 8; ++d)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) st.o[r][d][e] = marks[r][d][e] == 0.0f ? st.o[r][d][e] : marks[r][d][e];
+    }
+
     // The four waves' sums, in wave order.
 #pragma unroll
     for (int r = 0; r < RT; ++r) {
-        st.z[r] += __shfl_xor(st.z[r], 16);
-        st.z[r] += __shfl_xor(st.z[r], 32);
         if (lane < 16) lds_stats[(wave * RT + r) * kTileRows + lane] = make_float2(st.m[r], st.z[r]);
     }
     __syncthreads();
@@ -391,7 +497,7 @@ __global__ __launch_bounds__(kAttendThreads, RT == 1 ? 3 : 2) void jq_attend_ker
         float m = -__builtin_inff();
 #pragma unroll
         for (int w = 0; w < kAttendWaves; ++w) m = fmaxf(m, lds_stats[(w * RT + r) * kTileRows + (lane & 15)].x);
-        const float f = st.m[r] == m ? 1.0f : __builtin_amdgcn_exp2f(st.m[r] - m);
+        const float f = rescale(st.m[r], m);
         float* to = lds + ((wave * RT + r) * kTileRows + (lane & 15)) * kOutStride + 32 * (lane >> 4);
 #pragma unroll
         for (int e = 0; e < 4; ++e)
@@ -500,7 +606,7 @@ __global__ __launch_bounds__(kAttendThreads, RT == 1 ? 3 : 2) void jq_attend_ker
         float m = mz.x;
 #pragma unroll
         for (int d = 32; d; d >>= 1) m = fmaxf(m, __shfl_xor(m, d));
-        const float f = mz.x == m ? 1.0f : __builtin_amdgcn_exp2f(mz.x - m);
+        const float f = rescale(mz.x, m);
         float z = mz.y * f;
 #pragma unroll
         for (int d = 32; d; d >>= 1) z += __shfl_xor(z, d);
@@ -519,8 +625,9 @@ __global__ __launch_bounds__(kAttendThreads, RT == 1 ? 3 : 2) void jq_attend_ker
                 if (t0 > 0 || i > part) request(t, i);
 #pragma unroll
                 for (int k = 0; k < kBatch; ++k) {
-                    const float f = i + k * parts < ns ? factor[r * ns + i + k * parts] : 0.0f;
-                    o += f32x4{lo[k].x, lo[k].y, hi[k].x, hi[k].y} * f;
+                    const bool there = i + k * parts < ns;  // (nothing times 0: a sum may be infinite)
+                    const float f = factor[there ? r * ns + i + k * parts : 0];
+                    o += f32x4{there ? lo[k].x : 0.0f, there ? lo[k].y : 0.0f, there ? hi[k].x : 0.0f, there ? hi[k].y : 0.0f} * f;
                 }
             }
         }
@@ -560,7 +667,8 @@ struct Wide {
     static constexpr int kRequests = kKeys / 2 / kWaves;       // of 1 KB, a wave and stage
     static constexpr int kBuffer = 2 * kKeys * 256;            // K, then V
     static constexpr int kMerge = (kWaves - R) * 32 * (kOutStride * 4 + 8);
-    static constexpr int kLds = 2 * kBuffer + 2 * kKeys > kMerge ? 2 * kBuffer + 2 * kKeys : kMerge;  // (behind the buffers a flag a key)
+    static constexpr int kFlags = 2 * kBuffer > kMerge ? 2 * kBuffer : kMerge;  // behind the buffers a byte a wave
+    static constexpr int kLds = kFlags + 16;
 };
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) s16x4* lds_s16x4;
@@ -570,7 +678,8 @@ __global__ __launch_bounds__(Wide<R>::kThreads, 2) void jq_attend_wide_kernel(At
     using W = Wide<R>;
     constexpr int KW = W::KW;
     extern __shared__ __align__(16) char wide_lds[];
-    uint8_t* bad_keys = (uint8_t*)wide_lds + 2 * W::kBuffer;  // [2][kKeys]
+    uint8_t* marked = (uint8_t*)wide_lds + W::kFlags;  // [kWaves]: the wave has cleared values of V, or has sums that are not finite
+    bool was_cleared = false;
     const int per = 8 * a.row_groups;
     const int u = (int)blockIdx.x / per * 8 + ((int)blockIdx.x & 7), rg = ((int)blockIdx.x % per) >> 3;
     if (u >= a.units) return;
@@ -601,11 +710,14 @@ __global__ __launch_bounds__(Wide<R>::kThreads, 2) void jq_attend_wide_kernel(At
         const int row = my_row + 4 * i, piece = is_v ? (lane & 15) ^ 2 * (row & 7) : (lane & 15) ^ (row & 15);
         to_lds[i] = (is_v ? W::kKeys * 256 : 0) + (my_tile * 32 + row) * 256 + piece * 16;
     }
+    auto tile_row = [&](int key) {
+        return !paged ? (uint32_t)key : ((uint32_t)clamp_page(table[key >> shift], n_pages) << shift) + (uint32_t)(key & ((1 << shift) - 1));
+    };
     auto request = [&](au32x4* to, int stage, int rows) {  // `rows`: those that may be read
         int key = (mine + stage * ns) * W::kKeys + 32 * my_tile;
         key = min(key, (rows - 1) & ~31);  // (a stage may reach past the last tile)
         const int last = rows - 1 - key;
-        const uint32_t row0 = !paged ? (uint32_t)key : ((uint32_t)clamp_page(table[key >> shift], n_pages) << shift) + (uint32_t)(key & ((1 << shift) - 1));
+        const uint32_t row0 = tile_row(key);
 #pragma unroll
         for (int i = 0; i < W::kRequests; ++i) to[i] = *(const au32x4*)(base + (row0 + (uint32_t)min(my_row + 4 * i, last)) * stride);
     };
@@ -645,21 +757,21 @@ __global__ __launch_bounds__(Wide<R>::kThreads, 2) void jq_attend_wide_kernel(At
             v_at[d] = W::kKeys * 256 + kw * W::kTiles * 8192 + vrow * 256 + ((2 * d + ((lane & 3) >> 1)) ^ 2 * (vrow & 7)) * 16 + (lane & 1) * 8;
     }
     auto deposit = [&](au32x4* from, int stage, int buf) {
-        // Where some row does not see some key, values of V that are not finite count as zeros, and the rows that do see the key
-        // are told.
         if (is_v && (mine + stage * ns) * W::kKeys + W::kKeys > open) {
+            bool ok = true;
 #pragma unroll
-            for (int k = 0; k < W::kRequests; ++k) {
-                bool ok = true;
+            for (int k = 0; k < W::kRequests; ++k) ok = ok && finite_piece(from[k]);
+            if (__any(!ok)) {
+                was_cleared = true;
 #pragma unroll
-                for (int w = 0; w < 4; ++w) ok = ok && finite_pair(from[k][w]);
-                const bool bad = ((uint32_t)(__ballot(!ok) >> (16 * (lane >> 4))) & 0xFFFFu) != 0;
-                if (bad) from[k] = au32x4{0u, 0u, 0u, 0u};
-                if ((lane & 15) == 0) bad_keys[buf * W::kKeys + my_tile * 32 + my_row + 4 * k] = bad;
+                for (int k = 0; k < W::kRequests; ++k) from[k] = cleared(from[k]);
             }
         }
 #pragma unroll
         for (int k = 0; k < W::kRequests; ++k) *(au32x4*)(wide_lds + buf * W::kBuffer + to_lds[k]) = from[k];
+    };
+    auto sees = [&](int r, int key) {
+        return row_sees<MASK>(a, key, n, n - a.n_q + token[r] + 1, MASK == kSeeTree ? a.seen + ((int64_t)s * a.n_q + token[r]) * a.words : nullptr);
     };
     auto work = [&](int key0, int at) {  // the 32 keys from key0; `at`: their place in LDS behind the wave's first ones
         // LDS answers late: all of K's rows are requested together, and half of V's ahead of the terms.
@@ -688,19 +800,12 @@ __global__ __launch_bounds__(Wide<R>::kThreads, 2) void jq_attend_wide_kernel(At
         if (key0 + 32 > open) {
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
-                const uint32_t bad = *(const uint32_t*)(bad_keys + at / W::kBuffer * W::kKeys + at % W::kBuffer / 256 + 32 * W::kTiles * kw + 16 * i + 4 * (lane >> 4));
 #pragma unroll
                 for (int r = 0; r < 2; ++r)
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
                         const int key = key0 + 16 * i + 4 * (lane >> 4) + e;
-                        bool see = key < n;
-                        if (MASK == kSeeCausal) see = key <= n - a.n_q + token[r];
-                        if (MASK == kSeeTree) {
-                            const int j = key - (n - a.n_q);
-                            if (see && j >= 0) see = (a.seen[((int64_t)s * a.n_q + token[r]) * a.words + (j >> 5)] >> (j & 31)) & 1u;
-                        }
-                        x[r][i][e] = see ? ((bad >> (8 * e)) & 1u ? __builtin_nanf("") : x[r][i][e]) : -__builtin_inff();
+                        x[r][i][e] = sees(r, key) ? x[r][i][e] : -__builtin_inff();
                     }
             }
         }
@@ -747,7 +852,7 @@ __global__ __launch_bounds__(Wide<R>::kThreads, 2) void jq_attend_wide_kernel(At
                 late |= __shfl_xor(late, 16);
                 late |= __shfl_xor(late, 32);
                 if (!late) to = m[r];  // a row's bits do not depend on the others of its wave
-                const float f = m[r] == to ? 1.0f : __builtin_amdgcn_exp2f(m[r] - to);
+                const float f = rescale(m[r], to);
                 m[r] = to;
                 z[r] *= f;
 #pragma unroll
@@ -792,8 +897,25 @@ __global__ __launch_bounds__(Wide<R>::kThreads, 2) void jq_attend_wide_kernel(At
 
 #pragma unroll
     for (int r = 0; r < 2; ++r) {
-        z[r] += __shfl_xor(z[r], 16);
-        z[r] += __shfl_xor(z[r], 32);
+        z[r] = sum_of_row(z[r]);
+        was_cleared |= z[r] < __builtin_inff() && !all_finite(o[r]);
+    }
+    if (lane == 0) marked[wave] = 0;
+    if (was_cleared) marked[wave] = 1;
+    lds_barrier();
+    if (__any(marked[lane % W::kWaves])) {
+        f32x4 marks[2][8];
+        auto tile = [&](int i) {
+            const int key = (mine + i / W::kTiles * ns) * W::kKeys + 32 * (W::kTiles * kw + i % W::kTiles);
+            return key < n ? key : -1;
+        };
+        mark_kinds<2>(marks, a.V + first_row * stride + g * (kHeadDim * 2), stride, n, lane, tile, tile_row, sees, [&](int d) { return 16 * d + (lane & 15); });
+#pragma unroll
+        for (int r = 0; r < 2; ++r)
+#pragma unroll
+            for (int d = 0; d < 8; ++d)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) o[r][d][e] = marks[r][d][e] == 0.0f ? o[r][d][e] : marks[r][d][e];
     }
     const int64_t part_row = (((int64_t)layer * a.n_splits + split) * a.h_kv + g) * a.rows;
     if (KW > 1) {  // the waves over other keys of the same rows
@@ -816,7 +938,7 @@ __global__ __launch_bounds__(Wide<R>::kThreads, 2) void jq_attend_wide_kernel(At
             const float mine_m = m[r];
 #pragma unroll
             for (int w = 0; w < KW - 1; ++w) m[r] = fmaxf(m[r], stats[(w * R + rw) * 32 + r * kTileRows + (lane & 15)].x);
-            float f = mine_m == m[r] ? 1.0f : __builtin_amdgcn_exp2f(mine_m - m[r]);
+            float f = rescale(mine_m, m[r]);
             z[r] *= f;
 #pragma unroll
             for (int d = 0; d < 8; ++d) o[r][d] *= f;
@@ -824,7 +946,7 @@ __global__ __launch_bounds__(Wide<R>::kThreads, 2) void jq_attend_wide_kernel(At
             for (int w = 0; w < KW - 1; ++w) {
                 const int at = (w * R + rw) * 32 + r * kTileRows + (lane & 15);
                 const float2 mz = stats[at];
-                f = mz.x == m[r] ? 1.0f : __builtin_amdgcn_exp2f(mz.x - m[r]);
+                f = rescale(mz.x, m[r]);
                 z[r] += mz.y * f;
 #pragma unroll
                 for (int d = 0; d < 8; ++d) o[r][d] += *(const f32x4*)(sums + at * kOutStride + 16 * d + 4 * (lane >> 4)) * f;
@@ -853,7 +975,7 @@ __device__ __forceinline__ float2 merge_stats(const float2* from, int64_t step, 
     for (int i = lane + 64; i < ns; i += 64) m = fmaxf(m, from[i * step].x);
 #pragma unroll
     for (int d = 32; d; d >>= 1) m = fmaxf(m, __shfl_xor(m, d));
-    *factor = own.x == m ? 1.0f : __builtin_amdgcn_exp2f(own.x - m);
+    *factor = rescale(own.x, m);
     float z = own.y * *factor;
     for (int i = lane + 64; i < ns; i += 64) {
         const float2 mz = from[i * step];
@@ -891,7 +1013,9 @@ __global__ __launch_bounds__(kAttendThreads) void jq_attend_finish_kernel(Attend
 #pragma unroll
         for (int k = 0; k < kFirst; ++k) {
             const float f = __shfl(factor, half + 2 * k);
-            if (half + 2 * k < ns) o += x[k] * f;
+            const bool there = half + 2 * k < ns;  // (nothing times 0: a sum may be infinite)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[e] += there ? x[k][e] * f : 0.0f;
         }
         for (int i0 = 2 * kFirst; i0 < ns; i0 += 2 * kFirst) {
 #pragma unroll
@@ -902,9 +1026,10 @@ __global__ __launch_bounds__(kAttendThreads) void jq_attend_finish_kernel(Attend
                 float f = __shfl(factor, i & 63);
                 if (i >= 64) {
                     const float mi = a.stats[at + min(i, ns - 1) * step].x;
-                    f = mi == mz.x ? 1.0f : __builtin_amdgcn_exp2f(mi - mz.x);
+                    f = rescale(mi, mz.x);
                 }
-                if (i < ns) o += x[k] * f;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) o[e] += i < ns ? x[k][e] * f : 0.0f;
             }
         }
 #pragma unroll
