@@ -442,8 +442,8 @@ int jq_evict_weight_paged(const jq_shape* shape, const jq_pages* pages, const in
  * keep_first or above token[s] - keep_last: keep_first + max(keep_last, 1) <= L_s, otherwise JQ_ERR_BUDGET.  The row's
  * weight starts at 0 and its position is token[s].  slot_out (DEVICE int32 [n_layers, n_seq, h_kv], may be NULL) takes
  * the row's number.  shape->window must be 0; no page may belong to two sequences.  The caller sets lens to
- * min(lens + 1, L_s) before the next call.  Rows are no longer in the order of their positions then: pos says which they
- * are, to jq_evict_weight too. */
+ * min(lens + 1, L_s) before the next call.  Where positions repeat or lie beyond token[s], so that no row may go, the
+ * lowest does.  Rows are no longer in the order of their positions then: pos says which they are, to jq_evict_weight too. */
 int jq_replace_lightest(const jq_shape* shape, const int32_t* lens, const void* k_new, const void* v_new,
                         const int32_t* token, void* K, void* V, float* weights, int32_t* pos, int32_t* slot_out,
                         void* stream);

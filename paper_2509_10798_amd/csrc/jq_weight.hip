@@ -39,9 +39,11 @@ __device__ __forceinline__ int live_of(const int32_t* lens, int n_seq, int layer
     return lens ? min(max(lens[(int64_t)layer * n_seq + s], 0), cap) : cap;
 }
 
-// What a row is ranked by: its weight, and above every weight the rows that stay.
+// What a row is ranked by: its weight, and above every weight, a NaN of all ones too, the rows that stay.
+constexpr uint32_t kStays = 0xFFFFFFFFu;
+__device__ __forceinline__ uint32_t free_key(float w) { return min(sortable_key(w), kStays - 1u); }
 __device__ __forceinline__ uint32_t weight_key(float w, int pos, int keep_first, int64_t recent) {
-    return pos < keep_first || pos > recent ? 0xFFFFFFFFu : sortable_key(w);
+    return pos < keep_first || pos > recent ? kStays : free_key(w);
 }
 
 // One workgroup per (layer, sequence, KV head): exact radix select over the weights' keys, 11, 11 and 10 bits, then the kept rows
@@ -85,7 +87,7 @@ struct FourRows {
     // behind the last row.  A row may have that key too; it comes before those, and never are more rows asked for than there are.
     __device__ __forceinline__ void rank(int j, int n, int keep_first, uint32_t inner) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) key[e] = (uint32_t)pos[e] - (uint32_t)keep_first >= inner ? 0xFFFFFFFFu : sortable_key(w[e]);
+        for (int e = 0; e < 4; ++e) key[e] = (uint32_t)pos[e] - (uint32_t)keep_first >= inner ? kStays : free_key(w[e]);
         if (j + 4 > n) {
 #pragma unroll
             for (int e = 0; e < 4; ++e) key[e] = j + e < n ? key[e] : 0u;
