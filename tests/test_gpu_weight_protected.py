@@ -71,3 +71,14 @@ def test_where_every_row_is_protected_the_lowest_goes():
     slot = jq.replace_lightest(sh, kn, vn, dev_i32([60]), k, v, w, pos)
     torch.cuda.synchronize()
     assert int(slot) == 0 and torch.equal(k[0, 0], kn[0, 0]) and torch.equal(v[0, 0], vn[0, 0]) and int(pos[0, 0, 0]) == 60
+
+
+@pytest.mark.parametrize("inplace", [False, True])
+@pytest.mark.parametrize("with_pos", [True, False])
+def test_kept_rows_beyond_what_a_workgroup_holds(inplace, with_pos):
+    """Pieces that leave more than 16384 rows to choose from, beside a short and a long sequence that are not cut; live counts at the
+    edges of pieces, protected rows at both ends, ties."""
+    from test_gpu_weight_eviction import evict
+    caps, budgets = [150_001, 300, 16_384], [1800, 120, 9000]
+    lens = np.array([[150_001, 300, 16_384], [131_073, 17, 16_383], [16_384, 0, 9001]], np.int32)
+    evict(31, 3, caps, budgets, 1, lens=lens, inplace=inplace, first=3, last=40, ties=True, order="scrambled" if with_pos else "ascending", with_pos=with_pos)
