@@ -717,7 +717,7 @@ int attend_plan(const jq_shape* shape, bool weights, Plan* p, AttendPlan* ap) {
     if (rc != JQ_OK) return rc;
     if (weights && p->rows > kMaxWeighRows) return JQ_ERR_UNSUPPORTED;
     plan_attend(*p, weights, ap);
-    return attend_fits(*p, *ap) ? JQ_OK : JQ_ERR_UNSUPPORTED;
+    return attend_fits(*p, *ap, weights) ? JQ_OK : JQ_ERR_UNSUPPORTED;
 }
 }  // namespace
 

@@ -1139,15 +1139,27 @@ void plan_attend(const Plan& p, bool weights, AttendPlan* ap) {
     ap->ws_bytes = ap->off_logits + (weights ? up((size_t)p.n_layers * p.h_kv * p.rows * ap->logit_T * sizeof(float)) : 0);
 }
 
-bool attend_fits(const Plan& p, const AttendPlan& ap) {
-    const int64_t most = UINT32_MAX;
-    const int64_t sweep = ((int64_t)ap.cu_split[p.n_seq] * p.h_kv + 8) * ap.row_groups * (ap.row_tiles > 2 ? 512 : 256);
-    const int64_t finish = ((int64_t)p.n_seq * p.h_kv * p.rows / kAttendWaves + 1 + (p.T / kWeighKeys + p.n_seq) * (int64_t)p.n_seq * p.h_kv) * kAttendThreads;
-    return sweep <= most && finish <= most;
+// Workgroups of a layer's sweep, and of the launch behind it: those that join, blocks of weights a (sequence, head).
+static int64_t sweep_groups(const Plan& p, const AttendPlan& ap) { return ((int64_t)ap.cu_split[p.n_seq] * p.h_kv + 7) / 8 * 8 * ap.row_groups; }
+struct Finish {
+    int64_t joins, blocks, groups;
+};
+static Finish finish_groups(const Plan& p, const AttendPlan& ap, bool weights) {
+    int32_t most = 0;
+    for (int s = 0; s < p.n_seq; ++s) most = std::max(most, p.tab.cu_seq[s + 1] - p.tab.cu_seq[s]);
+    const int64_t heads = (int64_t)p.n_seq * p.h_kv;
+    Finish f;
+    f.joins = ap.cu_split[p.n_seq] > p.n_seq ? (heads * p.rows + kAttendWaves - 1) / kAttendWaves : 0;
+    f.blocks = (most + kWeighKeys - 1) / kWeighKeys;
+    f.groups = ap.one_launch ? 0 : f.joins + (weights ? f.blocks * heads : 0);
+    return f;
+}
+bool attend_fits(const Plan& p, const AttendPlan& ap, bool weights) {
+    return sweep_groups(p, ap) * (ap.row_tiles > 2 ? 512 : kAttendThreads) <= UINT32_MAX && finish_groups(p, ap, weights).groups * kAttendThreads <= UINT32_MAX;
 }
 
 template <int RT, int MASK, bool KEEP>
-static hipError_t launch_sweep(const AttendArgs& a, hipStream_t st) {
+static hipError_t launch_sweep(const AttendArgs& a, dim3 grid, hipStream_t st) {
     constexpr int most = kAttendWaves * RT * kTileRows * (kOutStride * 4 + 8) + (KEEP ? kMostHeld : 0);
     const int lds = kAttendWaves * RT * kTileRows * (kOutStride * 4 + 8) + (KEEP ? a.rows * a.hold_keys * 4 : 0);
     if (most > 65536) {
@@ -1155,30 +1167,28 @@ static hipError_t launch_sweep(const AttendArgs& a, hipStream_t st) {
         const hipError_t e = allow_dynamic_lds((const void*)jq_attend_kernel<RT, MASK, KEEP>, most, done);
         if (e != hipSuccess) return e;
     }
-    const dim3 grid((unsigned)((a.units + 7) / 8 * 8 * a.row_groups), (unsigned)a.n_layers);
     return launch_kernel(jq_attend_kernel<RT, MASK, KEEP>, grid, dim3(kAttendThreads), lds, st, nullptr, -1, a);
 }
 
 template <int R, int MASK, bool KEEP>
-static hipError_t launch_wide(const AttendArgs& a, hipStream_t st) {
+static hipError_t launch_wide(const AttendArgs& a, dim3 grid, hipStream_t st) {
     constexpr int lds = Wide<R>::kLds;
     if (lds > 65536) {
         static std::atomic<uint64_t> done{0};
         const hipError_t e = allow_dynamic_lds((const void*)jq_attend_wide_kernel<R, MASK, KEEP>, lds, done);
         if (e != hipSuccess) return e;
     }
-    const dim3 grid((unsigned)((a.units + 7) / 8 * 8 * a.row_groups), (unsigned)a.n_layers);
     return launch_kernel(jq_attend_wide_kernel<R, MASK, KEEP>, grid, dim3(Wide<R>::kThreads), lds, st, nullptr, -1, a);
 }
 
 template <int MASK, bool KEEP>
-static hipError_t launch_rows(const AttendArgs& a, int row_tiles, hipStream_t st) {
+static hipError_t launch_rows(const AttendArgs& a, int row_tiles, dim3 grid, hipStream_t st) {
     switch (row_tiles) {
-        case 1: return launch_sweep<1, MASK, KEEP>(a, st);
-        case 2: return launch_sweep<2, MASK, KEEP>(a, st);
-        case 4: return launch_wide<2, MASK, KEEP>(a, st);
-        case 8: return launch_wide<4, MASK, KEEP>(a, st);
-        default: return launch_wide<8, MASK, KEEP>(a, st);
+        case 1: return launch_sweep<1, MASK, KEEP>(a, grid, st);
+        case 2: return launch_sweep<2, MASK, KEEP>(a, grid, st);
+        case 4: return launch_wide<2, MASK, KEEP>(a, grid, st);
+        case 8: return launch_wide<4, MASK, KEEP>(a, grid, st);
+        default: return launch_wide<8, MASK, KEEP>(a, grid, st);
     }
 }
 
@@ -1203,17 +1213,16 @@ hipError_t launch_attend(const Plan& p, const AttendPlan& ap, const int32_t* len
     a.pm = p.page_map();
     for (int s = 0; s <= p.n_seq; ++s) { a.cu_seq[s] = p.tab.cu_seq[s]; a.cu_split[s] = ap.cu_split[s]; }
     // one new token sees every live row, its own among them: no mask either way
+    const dim3 grid((unsigned)sweep_groups(p, ap), (unsigned)p.n_layers);
     hipError_t e;
-    if (seen) e = launch_rows<kSeeTree, false>(a, ap.row_tiles, st);
-    else if (p.window && p.n_q > 1) e = weights ? launch_rows<kSeeCausal, true>(a, ap.row_tiles, st) : launch_rows<kSeeCausal, false>(a, ap.row_tiles, st);
-    else e = weights ? launch_rows<kSeeAll, true>(a, ap.row_tiles, st) : launch_rows<kSeeAll, false>(a, ap.row_tiles, st);
+    if (seen) e = launch_rows<kSeeTree, false>(a, ap.row_tiles, grid, st);
+    else if (p.window && p.n_q > 1) e = weights ? launch_rows<kSeeCausal, true>(a, ap.row_tiles, grid, st) : launch_rows<kSeeCausal, false>(a, ap.row_tiles, grid, st);
+    else e = weights ? launch_rows<kSeeAll, true>(a, ap.row_tiles, grid, st) : launch_rows<kSeeAll, false>(a, ap.row_tiles, grid, st);
     if (e != hipSuccess) return e;
-    if (a.tag || (a.n_splits == p.n_seq && !weights)) return e;
-    int32_t most = 0;
-    for (int s = 0; s < p.n_seq; ++s) most = std::max(most, p.tab.cu_seq[s + 1] - p.tab.cu_seq[s]);
-    const int joins = a.n_splits > p.n_seq ? (p.n_seq * p.h_kv * p.rows + kAttendWaves - 1) / kAttendWaves : 0, blocks = (most + kWeighKeys - 1) / kWeighKeys;
-    const dim3 grid((unsigned)(joins + (weights ? blocks * p.n_seq * p.h_kv : 0)), (unsigned)p.n_layers);
-    return launch_kernel(jq_attend_finish_kernel, grid, dim3(kAttendThreads), 0, st, nullptr, -1, a, joins, blocks);
+    const Finish f = finish_groups(p, ap, weights != nullptr);
+    if (f.groups == 0) return e;
+    return launch_kernel(jq_attend_finish_kernel, dim3((unsigned)f.groups, (unsigned)p.n_layers), dim3(kAttendThreads), 0, st, nullptr, -1, a, (int)f.joins,
+                         (int)f.blocks);
 }
 
 }  // namespace jq

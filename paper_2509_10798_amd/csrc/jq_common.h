@@ -361,7 +361,7 @@ struct AttendPlan {
     size_t off_arrived, off_stats, off_part, off_logits, ws_bytes;
 };
 void plan_attend(const Plan& p, bool weights, AttendPlan* ap);
-bool attend_fits(const Plan& p, const AttendPlan& ap);  // every launch stays below 2^32 threads
+bool attend_fits(const Plan& p, const AttendPlan& ap, bool weights);  // every launch stays below 2^32 threads
 // `lens`, `seen`, `lse`, `weights` may be null; with `seen` the queries are drafted tokens, otherwise p.window says whether they are causal.
 hipError_t launch_attend(const Plan& p, const AttendPlan& ap, const int32_t* lens, const uint32_t* seen, const void* Q, const void* K, const void* V,
                          void* out, float* lse, float* weights, char* ws, hipStream_t st);
