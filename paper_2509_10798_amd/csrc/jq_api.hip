@@ -795,7 +795,6 @@ static int evict_weight_impl(const jq_shape* shape, const jq_pages* pages, bool 
     if (rc != JQ_OK) return rc;
     if (p.window) return JQ_ERR_SHAPE;  // no queries here
     if (paged && (rc = apply_pages(pages, &p)) != JQ_OK) return rc;
-    if ((uint64_t)p.n_layers * p.TB * p.h_kv * 16 > UINT32_MAX) return JQ_ERR_UNSUPPORTED;
     if (!K || !V || !weights || !K_out || !V_out || !weights_out || (pos && !pos_out) || !ws) return JQ_ERR_NULL;
     WeightPlan wp;
     plan_evict_weight(p, &wp);

@@ -26,6 +26,7 @@ struct WeightArgs {
     int32_t* newest;
     float* cand_w; int32_t* cand_pos; int32_t* cand_row;
     int32_t n_pieces, n_cand;
+    int64_t first_item;                        // of a launch of the copy: (layer, kept row, head)
     int32_t own_newest;                        // every piece looks through all of its sequence's positions: no launch for `newest`
     int32_t cu_piece[JQ_MAX_SEQ + 1], cu_cand[JQ_MAX_SEQ + 1];
     const int32_t* layer_budgets;
@@ -354,7 +355,7 @@ __global__ __launch_bounds__(kWeightThreads) void jq_weight_select_kernel(Weight
 // The kept rows of K and V, out of one cache into another: sixteen bytes a lane, sixteen lanes a row.
 constexpr int kMoveThreads = 256;
 __global__ __launch_bounds__(kMoveThreads) void jq_weight_copy_kernel(WeightArgs a) {
-    const int64_t item = ((int64_t)blockIdx.x * kMoveThreads + threadIdx.x) / 16;  // (layer, kept row, head), heads fastest
+    const int64_t item = a.first_item + ((int64_t)blockIdx.x * kMoveThreads + threadIdx.x) / 16;  // (layer, kept row, head), heads fastest
     if (item >= (int64_t)a.n_layers * a.TB * a.h_kv) return;
     const int g = (int)(item % a.h_kv), part = threadIdx.x & 15;
     const int64_t tb = item / a.h_kv % a.TB;
@@ -554,8 +555,14 @@ hipError_t launch_evict_weight(const Plan& p, const WeightPlan& wp, const int32_
     if (e != hipSuccess) return e;
     if (K_out == K)
         return launch_kernel(jq_weight_shift_kernel, dim3((unsigned)(8 * p.h_kv), (unsigned)p.n_seq, (unsigned)p.n_layers), dim3(kMoveThreads), 0, st, nullptr, -1, a);
-    const int64_t threads = (int64_t)p.n_layers * p.TB * p.h_kv * 16;
-    return launch_kernel(jq_weight_copy_kernel, dim3((unsigned)((threads + kMoveThreads - 1) / kMoveThreads)), dim3(kMoveThreads), 0, st, nullptr, -1, a);
+    constexpr int64_t group = kMoveThreads / 16, most = (int64_t)(UINT32_MAX / kMoveThreads) * group;  // rows of a workgroup, of a launch
+    const int64_t items = (int64_t)p.n_layers * p.TB * p.h_kv;
+    for (; a.first_item < items; a.first_item += most) {
+        const unsigned groups = (unsigned)((std::min(items - a.first_item, most) + group - 1) / group);
+        e = launch_kernel(jq_weight_copy_kernel, dim3(groups), dim3(kMoveThreads), 0, st, nullptr, -1, a);
+        if (e != hipSuccess) break;
+    }
+    return e;
 }
 
 hipError_t launch_replace(const Plan& p, const int32_t* lens, const void* k_new, const void* v_new, const int32_t* token, void* K, void* V, float* weights,

@@ -2,6 +2,7 @@
 import pytest
 
 import paper_2509_10798_amd as jq
+from test_decode_refusals import NULL, evict, pages
 
 
 def bytes_of(weights=False, **kw):
@@ -20,6 +21,15 @@ def test_query_rows_that_no_launch_holds():
     with pytest.raises(jq.JQError):
         bytes_of(seq_lens=[64] * 128, n_q=1 << 18, h_q=1024, h_kv=256)
     assert bytes_of(seq_lens=[4096], n_q=1 << 15) > 0
+
+
+@pytest.mark.parametrize("layers", [65, 70, 1000])
+def test_kept_rows_have_no_limit_of_their_own(layers):
+    """2^28 kept (layer, row, head) rows and more, 128 GiB of K and V: the shape passes, the missing tensor is what is refused."""
+    sh = jq.Shape(n_layers=layers, seq_lens=[4096] * 128, n_q=1, h_q=8, h_kv=8, pool_k=1, budgets=[4096] * 128)
+    assert evict(sh, v=None) == NULL
+    assert evict(sh, pg=pages(size=32, n=1 << 14, per=128), v=None) == NULL
+    assert jq.evict_weight_workspace_bytes(sh) >= layers * 8 * 4096 * 128 * 4
 
 
 @pytest.mark.gpu
