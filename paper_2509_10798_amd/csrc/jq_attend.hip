@@ -598,7 +598,7 @@ __global__ __launch_bounds__(kAttendThreads, RT == 1 ? 3 : 2) void jq_attend_ker
     if (KEEP) weigher.request(0);
     // Factors of all shares' sums, [rows_here][ns], and the rows' (m, z).
     float* factor = lds;
-    float* sums = factor + rows_here * ns;  // [parts][items] outputs of four
+    float* sums = factor + (rows_here * ns + 3) / 4 * 4;  // [parts][items] outputs of four, at multiples of sixteen bytes
     float* lse2 = (float*)(lds_stats + rows_here);
     __syncthreads();
     for (int r = wave; r < rows_here; r += kAttendWaves) {  // a wave a row, a lane a share (there are 64 at most)
