@@ -1188,7 +1188,9 @@ static hipError_t launch_rows(const AttendArgs& a, int row_tiles, dim3 grid, hip
         case 2: return launch_sweep<2, MASK, KEEP>(a, grid, st);
         case 4: return launch_wide<2, MASK, KEEP>(a, grid, st);
         case 8: return launch_wide<4, MASK, KEEP>(a, grid, st);
-        default: return launch_wide<8, MASK, KEEP>(a, grid, st);
+        default:  // more than 128 query rows: without weights
+            if constexpr (KEEP) return hipErrorInvalidValue;
+            else return launch_wide<8, MASK, KEEP>(a, grid, st);
     }
 }
 
