@@ -109,6 +109,7 @@ def _budgets(c):
     return [min(c["budget"], L) for L in _caps(c)]
 
 
+_MOST_WEIGHED = 128      # query rows of a KV head that a call takes whose weights are accumulated: of more tokens some at a time
 _SINKS, _RECENT = 4, 32  # rows that eviction never takes: the first tokens and the newest
 
 
@@ -221,13 +222,22 @@ def _kept(case, st, rows):
 
     first, newest = st["keep"]
     kind = st["kind"]
-    sh = jq.Shape(n_layers=case["layers"], seq_lens=_caps(case), n_q=case["n_q"], h_q=case["h_q"], h_kv=case["h_kv"], pool_k=1,
-                  budgets=_budgets(case) if kind == "evict" else None, keep_first=first if kind in ("evict", "replace") else 0,
-                  keep_last=newest if kind in ("evict", "replace") else 0, window=case["causal"])
+
+    def shape(n_q):
+        return jq.Shape(n_layers=case["layers"], seq_lens=_caps(case), n_q=n_q, h_q=case["h_q"], h_kv=case["h_kv"], pool_k=1,
+                        budgets=_budgets(case) if kind == "evict" else None, keep_first=first if kind in ("evict", "replace") else 0,
+                        keep_last=newest if kind in ("evict", "replace") else 0, window=case["causal"])
+
+    sh = shape(case["n_q"])
     kept = {"jq": jq, "sh": sh}
     if case["page"]:
         kept["pages"] = jq.Pages(case["page"], rows // case["page"], st["table"])
-    if kind in ("attend", "tree"):
+    most = _MOST_WEIGHED // st["G"]  # tokens of a call that accumulates weights
+    if case["weigh"] and case["n_q"] > most:
+        kept["portions"] = [(i, min(i + most, case["n_q"])) for i in range(0, case["n_q"], most)]
+        kept["shapes"] = [shape(b - a) for a, b in kept["portions"]]
+        kept["ws"] = max((jq.alloc_attend_workspace(x, weights=True) for x in kept["shapes"]), key=len)
+    elif kind in ("attend", "tree"):
         kept["ws"] = jq.alloc_attend_workspace(sh, weights=case["weigh"])
     if kind == "evict":
         kept["ws"] = jq.alloc_evict_weight_workspace(sh)
@@ -249,7 +259,12 @@ def run(state):
 def _own(s):
     jq, sh, pages, kind = s["jq"], s["sh"], s.get("pages"), s["kind"]
     at = (sh,) if pages is None else (sh, pages)
-    if kind == "attend":
+    if "portions" in s:  # causal tokens, the earlier ones before the later ones' rows are live
+        call = jq.attend if pages is None else jq.attend_paged
+        for part, (a, b) in zip(s["shapes"], s["portions"]):
+            out, lse = call(part, *at[1:], s["Q"][:, :, a:b].contiguous(), s["K"], s["V"], lens=s["lens"] - (sh.n_q - b), weights=s["weights"], ws=s["ws"])
+            s["out"][:, :, a:b], s["lse"][:, :, a:b] = out, lse
+    elif kind == "attend":
         call = jq.attend if pages is None else jq.attend_paged
         call(*at, s["Q"], s["K"], s["V"], lens=s["lens"], weights=s.get("weights"), out=s["out"], lse=s["lse"], ws=s["ws"])
     elif kind == "tree":
