@@ -34,6 +34,7 @@ constexpr int kAttendWaves = 4;
 constexpr int kAttendThreads = 64 * kAttendWaves;
 constexpr int kTileRows = 16;   // query rows of one MFMA tile
 constexpr int kOutStride = kHeadDim + 4;  // floats a row of partial output takes in LDS: rows of 128 would meet in the same banks
+constexpr int kMostJoinRows = 8;  // query rows whose shares the last workgroup of a sequence joins
 constexpr int kMostHeld = 65536;  // bytes of logits that a workgroup holds in LDS
 constexpr float kSlack = 8.0f;  // a row's running maximum may lag this far (in powers of two) behind before its sums are rescaled
 constexpr float kLargeSum = 16777216.0f;  // or, with many query rows, until a lane's share of the sum is this large
@@ -445,7 +446,7 @@ __global__ __launch_bounds__(kAttendThreads, RT == 1 ? 3 : 2) void jq_attend_ker
     for (int r = 0; r < RT; ++r) row_limit[r] += n - a.n_q;
     // The sequence's count of finished workgroups starts at zero for this call: it holds the call's tag or is given it here.
     uint64_t* arrived = a.arrived + (((int64_t)layer * a.n_seq + s) * a.h_kv + g) * a.row_groups + rg;
-    if (a.tag && ns > 1 && threadIdx.x == 0) {
+    if (RT == 1 && a.tag && ns > 1 && threadIdx.x == 0) {
         uint64_t was = __hip_atomic_load(arrived, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
         if ((was ^ a.tag) >> 24) __hip_atomic_compare_exchange_strong(arrived, &was, a.tag, __ATOMIC_RELAXED, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     }
@@ -565,7 +566,7 @@ __global__ __launch_bounds__(kAttendThreads, RT == 1 ? 3 : 2) void jq_attend_ker
             if (at < ((n + 31) & ~31)) put_pair(a.logits + to + r * a.logit_T + at, held[r * a.hold_keys + j], held[r * a.hold_keys + j + 1]);
         }
     }
-    if (!a.tag || ns == 1) return;
+    if (RT > 1 || !a.tag || ns == 1) return;
 
     // Whoever completes a sequence joins it; nobody waits.  Data first, then the count of those that have left theirs.
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
@@ -578,13 +579,13 @@ __global__ __launch_bounds__(kAttendThreads, RT == 1 ? 3 : 2) void jq_attend_ker
     // What the join begins with is requested together, statistics, sums and logits: each of them is a round trip past the caches.
     // Sixteen bytes of output a thread; where there are few rows several threads take shares of the shares.
     const int64_t first = (((int64_t)layer * a.n_splits + a.cu_split[s]) * a.h_kv + g) * a.rows + row0, next_share = (int64_t)a.h_kv * a.rows;
-    const int items = rows_here * 32;
+    static_assert(kMostJoinRows * 32 <= kAttendThreads, "a thread or more for every four sums");
+    const int items = rows_here * 32, part = (int)threadIdx.x / items, item = (int)threadIdx.x - part * items;
     int parts = 1;
     while (2 * parts * items <= kAttendThreads && parts < 8) parts *= 2;
     constexpr int kBatch = 8;
     float2 lo[kBatch], hi[kBatch];
-    auto request = [&](int t, int i) {  // shares i, i + parts, ... of thread t's sums
-        const int item = t % items;
+    auto request = [&](int i) {  // shares i, i + parts, ... of the thread's sums
         const float* from = a.part + (first + (item >> 5)) * kHeadDim + (item & 31) * 4;
 #pragma unroll
         for (int k = 0; k < kBatch; ++k) {
@@ -593,7 +594,7 @@ __global__ __launch_bounds__(kAttendThreads, RT == 1 ? 3 : 2) void jq_attend_ker
             hi[k] = get_pair(p + 2);
         }
     };
-    request(threadIdx.x, (int)threadIdx.x / items);
+    request(part);
     Weigher weigher(a, layer, s, g, 0, n);
     if (KEEP) weigher.request(0);
     // Factors of all shares' sums, [rows_here][ns], and the rows' (m, z).
@@ -601,7 +602,7 @@ __global__ __launch_bounds__(kAttendThreads, RT == 1 ? 3 : 2) void jq_attend_ker
     float* sums = factor + (rows_here * ns + 3) / 4 * 4;  // [parts][items] outputs of four, at multiples of sixteen bytes
     float* lse2 = (float*)(lds_stats + rows_here);
     __syncthreads();
-    for (int r = wave; r < rows_here; r += kAttendWaves) {  // a wave a row, a lane a share (there are 64 at most)
+    for (int r = wave; r < rows_here; r += kAttendWaves) {  // a wave a row, a lane a share (there are 20 at most)
         const float2 mz = lane < ns ? get_pair((const float*)(a.stats + first + r + lane * next_share)) : make_float2(-__builtin_inff(), 0.0f);
         float m = mz.x;
 #pragma unroll
@@ -617,28 +618,26 @@ __global__ __launch_bounds__(kAttendThreads, RT == 1 ? 3 : 2) void jq_attend_ker
         }
     }
     __syncthreads();
-    for (int t0 = 0; t0 < items * parts; t0 += kAttendThreads) {
-        const int t = t0 + threadIdx.x, part = t / items, item = t - part * items, r = item >> 5, d = (item & 31) * 4;
-        f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
-        if (part < parts) {
-            for (int i = part; i < ns; i += kBatch * parts) {
-                if (t0 > 0 || i > part) request(t, i);
+    const int r = item >> 5, d = (item & 31) * 4;
+    f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
+    if (part < parts) {
+        for (int i = part; i < ns; i += kBatch * parts) {
+            if (i > part) request(i);
 #pragma unroll
-                for (int k = 0; k < kBatch; ++k) {
-                    const bool there = i + k * parts < ns;  // (nothing times 0: a sum may be infinite)
-                    const float f = factor[there ? r * ns + i + k * parts : 0];
-                    o += f32x4{there ? lo[k].x : 0.0f, there ? lo[k].y : 0.0f, there ? hi[k].x : 0.0f, there ? hi[k].y : 0.0f} * f;
-                }
+            for (int k = 0; k < kBatch; ++k) {
+                const bool there = i + k * parts < ns;  // (nothing times 0: a sum may be infinite)
+                const float f = factor[there ? r * ns + i + k * parts : 0];
+                o += f32x4{there ? lo[k].x : 0.0f, there ? lo[k].y : 0.0f, there ? hi[k].x : 0.0f, there ? hi[k].y : 0.0f} * f;
             }
         }
-        if (parts > 1) {
-            if (part < parts) *(f32x4*)(sums + 4 * t) = o;
-            __syncthreads();
-            if (part == 0)
-                for (int k = 1; k < parts; ++k) o += *(const f32x4*)(sums + 4 * (k * items + item));
-        }
-        if (part == 0) store_out(a, layer, s, g, row0 + r, d, o, lds_stats[r].x, lds_stats[r].y);
     }
+    if (parts > 1) {
+        if (part < parts) *(f32x4*)(sums + 4 * (int)threadIdx.x) = o;
+        __syncthreads();
+        if (part == 0)
+            for (int k = 1; k < parts; ++k) o += *(const f32x4*)(sums + 4 * (k * items + item));
+    }
+    if (part == 0) store_out(a, layer, s, g, row0 + r, d, o, lds_stats[r].x, lds_stats[r].y);
     if (KEEP) weigher.add(lse2, true);
 }
 
@@ -1066,9 +1065,20 @@ __global__ __launch_bounds__(kAttendThreads) void jq_attend_finish_kernel(Attend
 // 177, and as they are 25 x 40 x 2099 103 (125 in smaller shares), 64 x 40 x 1099 96 (133).
 constexpr int kChip = 256, kRounds = 4;
 constexpr int kStart = 320, kWideStart = 1500;
-constexpr int kMostSums = 160;       // sums of 128 dimensions that it adds up
-constexpr int kMostJoined = 64;      // shares of a sequence that its last workgroup joins: a lane each
-constexpr int64_t kMostWeighed = 16384;  // logits of a (sequence, head) that it weighs
+// What a sequence's last workgroup joins, and weighs, instead of a second launch.  Its time grows with the shares, whose statistics and
+// sums it waits for, and with the rows times them, while the second launch costs some 1.7 us whatever there is (2 with weights).  Us a call
+// of 8 KV heads, joined / in a second launch, by shares of 128 rows of the cache:
+//   shares:          8            12           16           20           24           32
+//    1 query row  10.0 / 11.6  10.5 / 11.7  10.9 / 11.6  11.5 / 11.6  12.1 / 11.3  14.3 / 11.4
+//    4            10.0 / 11.7  10.4 / 11.7  10.8 / 11.6  12.2 / 11.6  12.8 / 11.3  15.0 / 11.4
+//    8            10.5 / 11.6  11.8 / 11.6  12.3 / 11.7  13.7 / 11.5  14.2 / 11.3  17.3 / 11.5
+//   16, 2 shares 12.4 / 11.5; 32, 2 shares 18.9 / 11.7
+//   1, weights    11.4 / 13.2  11.9 / 13.3  12.4 / 13.3               14.6 / 13.2
+//   4             11.7 / 13.3  12.2 / 13.3  12.6 / 13.3               16.1 / 13.1
+//   8, 4 shares   13.0 / 13.3; 8 13.4 / 13.3; 12 14.7 / 13.4; 16, 2 shares 16.7 / 15.4
+constexpr int kMostJoined = 20;          // shares (a lane each in the join)
+constexpr int kMostSums = 64;            // shares times query rows
+constexpr int64_t kMostWeighed = 8192;   // logits of a (sequence, head)
 static void plan_splits(const Plan& p, bool weights, AttendPlan* ap) {
     const int row_tiles = (p.rows + kTileRows - 1) / kTileRows;
     ap->row_tiles = row_tiles <= 1 ? 1 : row_tiles <= 2 ? 2 : row_tiles <= 4 ? 4 : row_tiles <= 8 ? 8 : 16;
@@ -1116,7 +1126,9 @@ static void plan_splits(const Plan& p, bool weights, AttendPlan* ap) {
         tiles = std::max(tiles, ((L + 31) / 32 + 4 * ns[s] - 1) / (4 * ns[s]));  // of 32 keys, a wave
     }
     ap->hold_keys = weights && row_tiles <= 2 ? (int32_t)(tiles * 32 * kAttendWaves) : 0;
-    ap->one_launch = row_tiles <= 2 && most_ns <= kMostJoined && most_ns * p.rows <= kMostSums && (!weights || most_ns == 1 || most_L * p.rows <= kMostWeighed);
+    // (without shares there is nothing to join, and the weights are the sweep's)
+    ap->one_launch = row_tiles <= 2 && (most_ns == 1 || (p.rows <= kMostJoinRows && most_ns <= kMostJoined && most_ns * p.rows <= kMostSums &&
+                                                         (!weights || most_L * p.rows <= kMostWeighed)));
 }
 
 // 40 bits that no other call of the process has, above 24 of zeros; never 0.
