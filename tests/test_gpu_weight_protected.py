@@ -82,3 +82,11 @@ def test_kept_rows_beyond_what_a_workgroup_holds(inplace, with_pos):
     caps, budgets = [150_001, 300, 16_384], [1800, 120, 9000]
     lens = np.array([[150_001, 300, 16_384], [131_073, 17, 16_383], [16_384, 0, 9001]], np.int32)
     evict(31, 3, caps, budgets, 1, lens=lens, inplace=inplace, first=3, last=40, ties=True, order="scrambled" if with_pos else "ascending", with_pos=with_pos)
+
+
+@pytest.mark.parametrize("inplace", [False, True])
+def test_pieces_with_budgets_of_each_layer(inplace):
+    """Pieces have room for the largest budget of a sequence; a layer's own may be smaller, down to the protected rows."""
+    from test_gpu_weight_eviction import evict
+    evict(33, 3, [50_000, 700], [1200, 300], 2, layer_budgets=np.array([[1200, 300], [333, 1], [-5, 2 ** 31 - 1]], np.int32), inplace=inplace, first=3, last=12,
+          ties=True, order="scrambled", lens=np.array([[50_000, 700], [32_769, 650], [49_151, 2]], np.int32))
