@@ -243,11 +243,15 @@ __device__ __forceinline__ void tile_step(RowState<RT>& st, KvTile& t, const Att
 #pragma unroll
             for (int e = 0; e < 4; ++e) exponents.add(t.v[i][e]);
         if (!__all(exponents.finite())) {
-            *was_cleared = true;
+            Exponents live;  // (rows that are not live may hold anything, and mark nothing)
 #pragma unroll
             for (int i = 0; i < 2; ++i)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) t.v[i][e] = cleared(t.v[i][e]);
+                for (int e = 0; e < 4; ++e) {
+                    live.add(t.v[i][e] & (key0 + 16 * i + 4 * (lane >> 4) + e < n ? 0xFFFFFFFFu : 0u));
+                    t.v[i][e] = cleared(t.v[i][e]);
+                }
+            *was_cleared |= !__all(live.finite());
         }
     }
     f32x4 s[RT][2];
@@ -768,9 +772,14 @@ __global__ __launch_bounds__(Wide<R>::kThreads, 2) void jq_attend_wide_kernel(At
 #pragma unroll
             for (int k = 0; k < W::kRequests; ++k) exponents.add(from[k]);
             if (!__all(exponents.finite())) {
-                was_cleared = true;
+                Exponents live;  // (rows that are not live may hold anything, and mark nothing)
+                const int key = (mine + stage * ns) * W::kKeys + 32 * my_tile + my_row;
 #pragma unroll
-                for (int k = 0; k < W::kRequests; ++k) from[k] = cleared(from[k]);
+                for (int k = 0; k < W::kRequests; ++k) {
+                    live.add(from[k] & (key + 4 * k < n ? 0xFFFFFFFFu : 0u));
+                    from[k] = cleared(from[k]);
+                }
+                was_cleared |= !__all(live.finite());
             }
         }
 #pragma unroll
