@@ -391,11 +391,12 @@ int jq_evict_traced(const jq_shape* shape, const void* Q, const void* K, const v
  * per KV head, otherwise JQ_ERR_UNSUPPORTED) every live row's weight grows by the attention it receives, summed over
  * the n_q tokens and the heads of the group: the statistic that jq_evict_weight and jq_replace_lightest evict by.
  * With the soft tokens' own rows appended (window = 1) lse is what jq_score_lse and jq_evict_lse take: the prompt is
- * then evicted in one pass over K.  Sums and softmax are held in fp32, the sums of p V before their division by the sum of p:
- * finite values of V above 2^80 in magnitude may overflow them.  A value of V that is not finite makes the outputs of its own
- * dimension infinite or NaN, of the queries that see its row; everything else is as if it were finite.  `ws` (DEVICE,
- * 16-byte aligned) must hold jq_attend_workspace_bytes (`with_weights`: 0, or 1 for calls that pass weights).
- * shape->budgets is not used. */
+ * then evicted in one pass over K.  Sums and softmax are held in fp32, the sums of p V before their division by the
+ * sum of p: finite values of V above 2^80 in magnitude may overflow them.  V is multiplied by p in two bf16 parts
+ * (2^-16 of p is lost), with more than 64 query rows per KV head in one (2^-8; out's own rounding is 2^-8 too).  A
+ * value of V that is not finite makes the outputs of its own dimension infinite or NaN, of the queries that see its
+ * row; everything else is as if it were finite.  `ws` (DEVICE, 16-byte aligned) must hold jq_attend_workspace_bytes
+ * (`with_weights`: 0, or 1 for calls that pass weights). shape->budgets is not used. */
 int jq_attend_workspace_bytes(const jq_shape* shape, int32_t with_weights, size_t* bytes);
 int jq_attend(const jq_shape* shape, const int32_t* lens, const void* Q, const void* K, const void* V, void* out,
               float* lse, float* weights, void* ws, size_t ws_bytes, void* stream);

@@ -8,9 +8,9 @@
 // K and V are read once, 512 bytes a (row, KV head); the few query rows stay in registers.  One pass with a running maximum m
 // and sum z per query row; workgroups that share a sequence leave (m, z, unnormalised out), which the last of them joins, or a
 // second launch where that is much.  All sums and statistics are fp32.  Measured on one MI355X, whole calls, 8 KV heads of 4 query
-// heads: one token over 131072 rows 101 us (5.3 TB/s; a copy of 2 GiB reaches 4.9), 32 sequences of 2048 rows with weights 55
+// heads: one token over 131072 rows 97 us (5.5 TB/s; a plain read reaches 6.2), 32 sequences of 2048 rows with weights 55
 // (bound by memory), one token over 1000 rows of 2 heads 11 (bound by the round trips of a join), 25 drafted tokens over eight
-// paged caches of 29909 rows together 42, 64 over 32832 rows 55 (matrix and vector instructions, which take turns).
+// paged caches of 29909 rows together 41, 64 over 32832 rows 53 (matrix and vector instructions, which take turns).
 //
 // Layout.  Both products are v_mfma_f32_16x16x32_bf16, of which lane l holds row (or column) l % 16 and the eight products'
 // terms 8 * (l / 16) .. + 7 of either operand, and of the result column l % 16 and rows 4 * (l / 16) .. + 3.  Scores are
@@ -655,7 +655,7 @@ __global__ __launch_bounds__(kAttendThreads, RT == 1 ? 3 : 2) void jq_attend_ker
 // Many query rows (more than 32 a KV head).  A wave still holds 32 of them, but the eight waves of a workgroup share the keys: R waves
 // over all rows of a group times KW over keys of their own.  K and V go through LDS, where every wave reads all of its keys' rows:
 // requested into registers stages ahead, written to one of two buffers, one barrier a stage.  (Every wave reading K and V for itself
-// took 117 us for 128 rows behind four prompts, 57 now.)
+// took 117 us for 128 rows behind four prompts, 58 this way.)
 // K's rows are read sixteen lanes a row of 256 bytes, piece p of row k at p ^ (k & 15), so that eight lanes' pieces meet in eight
 // different bank groups; V is read transposed (ds_read_b64_tr_b16: a lane receives four keys' values of one dimension out of four
 // rows of sixteen), piece p of row k at p ^ 2 (k & 7) for the same reason (no bank conflicts are counted).
@@ -670,8 +670,9 @@ struct Wide {
     static constexpr int kKeys = KW == 4 ? 128 : 64;           // of a stage
     static constexpr int kTiles = kKeys / 32 / KW;             // of 32 keys, a wave and stage
     static constexpr int kAhead = KW == 4 ? 1 : 2;             // stages requested ahead: 64 KB
-    // Probabilities in two bf16 parts only where memory is waited for anyway.  With one, out is off by 1.4 times its own rounding (2-norm
-    // against 64 bits 0.0023, 0.0017 with two), and a call is faster: 128 rows behind four prompts 60 us / 68, 256 over 32832 60 / 72.
+    // Probabilities in one bf16 part, off by 2^-8 of each at most, or in two, 2^-16, for which the second product doubles.  With one, out is off by 1.4
+    // times its own rounding (2-norm against 64 bits 0.0023, 0.0017 with two).  Us a call with one / two: 64 rows over 32832 39.3 / 40.4,
+    // 128 rows behind four prompts 58.8 / 65.2, 100 over eight caches 41.5 / 45.3, 256 over 32832 56 / 68: two while that costs 3 percent.
     static constexpr bool kExact = R == 2;
     static constexpr int kEarly = 2;                           // blocks of V requested ahead of their use
     static constexpr int kRequests = kKeys / 2 / kWaves;       // of 1 KB, a wave and stage
@@ -1071,10 +1072,10 @@ __global__ __launch_bounds__(kAttendThreads) void jq_attend_finish_kernel(Attend
 // ---- host ------------------------------------------------------------------------------------------------------------------
 
 // How many workgroups share each sequence.  Asked for more than one workgroup per CU, memory answers no faster, and there are more
-// sums to join (us a call, workgroups 256 / 512 / 768): one token over 131072 rows 100 / 109 / 106, 32 tokens behind four prompts of
-// 52296 rows together 61 / 72 / 83, a tree of 64 over 32832 rows 60 / 77 / 96.  So the smallest share is looked for that makes
-// no more workgroups than there are CUs -- not a share of the rows rounded up for every sequence, which made 288 for eight ragged
-// ones (63 us, 47 now).  Where sequences and heads alone are more than that, whole sequences leave CUs idle behind the longest, and
+// sums to join (us a call, workgroups 256 / 512 / 768): one token over 131072 rows 97 / 100 / 108, 32 tokens behind four prompts of
+// 52296 rows together 59 / 70 / 80, a tree of 64 over 32832 rows 56 / 71 / 92.  So the smallest share is looked for that makes
+// no more workgroups than there are CUs -- not a share of the rows rounded up for every sequence, which makes 288 for eight ragged
+// ones (63 us against 47).  Where sequences and heads alone are more than that, whole sequences leave CUs idle behind the longest, and
 // smaller shares in two to four rounds of the chip may be ahead; a round costs its share and a start, which is dearer where sums of
 // many query rows have to be joined afterwards.  In rows of the cache, fitted to (whole sequences / as chosen) one token, 40 x 4099 rows
 // 158 / 133 us, 36 x 2000 78 / 65, 64 ragged sequences of 80 to 7000 203 / 128; trees of 20 over those 257 / 161, 12 x 40 x 4099 189 /

@@ -352,7 +352,8 @@ __global__ __launch_bounds__(kWeightThreads) void jq_weight_select_kernel(Weight
     }
 }
 
-// The kept rows of K and V, out of one cache into another: sixteen bytes a lane, sixteen lanes a row.
+// The kept rows of K and V, out of one cache into another: sixteen bytes a lane, sixteen lanes a row.  Bound by memory where rows lie side
+// by side (2048 of 2560 rows in 32 layers 91 us, 5.9 TB/s), by each lane's chain of four reads where they do not (16 paged sequences 34 us, 4 TB/s).
 constexpr int kMoveThreads = 256;
 __global__ __launch_bounds__(kMoveThreads) void jq_weight_copy_kernel(WeightArgs a) {
     const int64_t item = a.first_item + ((int64_t)blockIdx.x * kMoveThreads + threadIdx.x) / 16;  // (layer, kept row, head), heads fastest
@@ -373,7 +374,8 @@ __global__ __launch_bounds__(kMoveThreads) void jq_weight_copy_kernel(WeightArgs
 
 // The same within one cache.  A workgroup moves one 64-byte column of one head's K or V, front to back: a slot lies at or before
 // the row that goes there and rows are in ascending order, so what a chunk overwrites has been read by it or by an earlier one.
-// Columns have nothing to do with each other, so a (layer, sequence, head) is the work of eight workgroups.
+// Columns have nothing to do with each other, so a (layer, sequence, head) is the work of eight workgroups.  Bound by its chunks, one
+// after the other: 2048 of 2560 rows in 32 layers 162 us (the copy 101), 2048 of 65536 in one 26 (the copy 6).
 constexpr int kShiftRows = 4 * kMoveThreads / 4;  // rows of a chunk: four lanes a row, four rows a lane
 __global__ __launch_bounds__(kMoveThreads) void jq_weight_shift_kernel(WeightArgs a) {
     const int column = blockIdx.x & 3, g = (int)blockIdx.x >> 3, s = blockIdx.y, layer = blockIdx.z;
