@@ -670,9 +670,9 @@ struct Wide {
     static constexpr int kKeys = KW == 4 ? 128 : 64;           // of a stage
     static constexpr int kTiles = kKeys / 32 / KW;             // of 32 keys, a wave and stage
     static constexpr int kAhead = KW == 4 ? 1 : 2;             // stages requested ahead: 64 KB
-    // Probabilities in one bf16 part, off by 2^-8 of each at most, or in two, 2^-16, for which the second product doubles.  With one, out is off by 1.4
-    // times its own rounding (2-norm against 64 bits 0.0023, 0.0017 with two).  Us a call with one / two: 64 rows over 32832 39.3 / 40.4,
-    // 128 rows behind four prompts 58.8 / 65.2, 100 over eight caches 41.5 / 45.3, 256 over 32832 56 / 68: two while that costs 3 percent.
+    // Probabilities in one bf16 part, off by 2^-8 of each at most, or in two, 2^-16, for which the second product doubles.  With one, out is
+    // off by 1.4 times its own rounding (2-norm against 64 bits 0.0023, 0.0017 with two).  Us a call with one / two: 64 rows over 32832
+    // 39.3 / 40.4, 128 behind four prompts 58.8 / 65.2, 100 over eight caches 41.5 / 45.3, 256 over 32832 56 / 68: two while they cost 3 percent.
     static constexpr bool kExact = R == 2;
     static constexpr int kEarly = 2;                           // blocks of V requested ahead of their use
     static constexpr int kRequests = kKeys / 2 / kWaves;       // of 1 KB, a wave and stage
@@ -768,7 +768,7 @@ __global__ __launch_bounds__(Wide<R>::kThreads, 2) void jq_attend_wide_kernel(At
             v_at[d] = W::kKeys * 256 + kw * W::kTiles * 8192 + vrow * 256 + ((2 * d + ((lane & 3) >> 1)) ^ 2 * (vrow & 7)) * 16 + (lane & 1) * 8;
     }
     auto deposit = [&](au32x4* from, int stage, int buf) {
-        if (is_v && (mine + stage * ns) * W::kKeys + W::kKeys > open) {
+        if (is_v && (mine + stage * ns) * W::kKeys + W::kKeys > open) {  // some row does not see some key: cleared of what is not finite
             Exponents exponents;
 #pragma unroll
             for (int k = 0; k < W::kRequests; ++k) exponents.add(from[k]);

@@ -12,3 +12,14 @@ pytestmark = pytest.mark.gpu
 def test_rows_and_shares_of_any_number(rows, shares):
     run(rows + 8 * shares, 1, [128 * shares - 3], rows, 1, 1, weigh=True)
     run(rows + 8 * shares, 1, [128 * shares], 2 * rows, 2, 1)
+
+
+@pytest.mark.parametrize("rows,shares", [(1, 20), (1, 21), (3, 20), (4, 16), (4, 17), (8, 8), (8, 9), (9, 2), (16, 3), (20, 2), (32, 3)])
+def test_both_sides_of_what_the_last_workgroup_joins(rows, shares):
+    run(100 + rows + shares, 1, [128 * shares - 5], 2 * rows, 2, 1, weigh=True)
+    run(200 + rows + shares, 1, [128 * shares - 5], 2 * rows, 2, 1)
+
+
+@pytest.mark.parametrize("rows,weigh", [(1, True), (4, True), (4, False), (20, True), (50, False)])
+def test_more_shares_than_a_wave_has_lanes(rows, weigh):
+    run(300 + rows, 1, [128 * 150 + 77], rows, 1, 1, weigh=weigh)

@@ -100,6 +100,12 @@ def test_values_in_a_cache_swept_by_one_workgroup_a_sequence(n_q):
     compare(700, n_q, "all", (699, 31), h_q=512, h_kv=256, weigh=True)
 
 
+@pytest.mark.parametrize("n_q", [1, 8, 16])
+@pytest.mark.parametrize("keys", [(7, 128 * 127 + 5), (17_999, 9_000)])
+def test_values_among_more_shares_than_a_wave_has_lanes(n_q, keys):
+    compare(18_000, n_q, "all", keys, weigh=True)
+
+
 @pytest.mark.parametrize("n_q", [1, 8, 16, 32, 64])
 @pytest.mark.parametrize("keys", [(3, 9), (2990, 2999), (3, 2999)])
 def test_values_of_rows_that_hardly_weigh_anything(n_q, keys):
