@@ -21,6 +21,8 @@
  *   jq_score_paged, jq_evict_paged  the same on a paged cache (pools + block table)
  *   jq_attend, jq_attend_tree     attention of the newest tokens, or of a tree of drafted ones, over a pruned cache
  *   jq_evict_weight, jq_replace_lightest   eviction by accumulated attention weight: of many rows, or of one for a new token's
+ *   jq_quantize, jq_dequantize    rows written into a cache of 8- or 4-bit codes, and read back
+ *   jq_attend_quantized, jq_attend_tree_quantized   jq_attend and jq_attend_tree over such a cache
  *   jq_hit_rate     critical-KV hit rate between two kept sets (Eq. 6)
  *   jq_map_mse      forward value of the training objective (Eq. 5) from two score maps
  *   jq_map_mse_fused  the same from the two query sets, neither map ever stored
@@ -451,6 +453,57 @@ int jq_replace_lightest(const jq_shape* shape, const int32_t* lens, const void* 
 int jq_replace_lightest_paged(const jq_shape* shape, const jq_pages* pages, const int32_t* lens, const void* k_new,
                               const void* v_new, const int32_t* token, void* K_pool, void* V_pool, float* weights,
                               int32_t* pos, int32_t* slot_out, void* stream);
+
+/* ---- A pruned cache in 8 or 4 bits (Section 4.3: decoding continues on the pruned cache) ---------------------
+ * Eviction keeps fewer rows of a cache; codes make each row that is left half or a quarter as large.  Every 32 neighbouring
+ * dimensions of a row of a head share a scale 2^x, kept as the byte x + 127, and each value is a code c with
+ *   value = c * 2^x,  c of e4m3 (8 bits: sign, 4 of exponent, 3 of mantissa; largest 448) or of e2m1 (4 bits; largest 6).
+ * Keys may take more bits than values (values bear coarse codes better), not fewer.  A cache of codes is laid out by head:
+ *   K, V              [n_layers, h_kv, T, d * bits / 8]  bytes; of two 4-bit codes the lower dimension's in the low half
+ *   K_scale, V_scale  [n_layers, h_kv, T, d / 32]        uint8
+ * or in pages [n_layers, n_pages, h_kv, page_size, ...] behind the block table of a jq_pages.  The limits on the sizes of a
+ * bf16 cache apply as they stand. */
+typedef struct jq_codes {
+    int32_t k_bits, v_bits; /* 8 or 4; k_bits >= v_bits, otherwise JQ_ERR_UNSUPPORTED          */
+    void* K;                /* DEVICE, 16-byte aligned                                         */
+    void* V;
+    void* K_scale;          /* DEVICE, 4-byte aligned                                          */
+    void* V_scale;
+} jq_codes;
+
+/* Rows K, V (DEVICE bf16 [n_layers, TB, h_kv, d], TB = sum of budgets: the layout of a pruned cache that jq_evict leaves, or,
+ * with budgets of 1, of one new token a sequence) written into a cache of codes: row b of sequence s, b < budgets[s] (or
+ * layer_budgets[l, s], if that is smaller; none where it is 0 or less), becomes row first[l, s] + b of the sequence (first: DEVICE
+ * int32 [n_layers, n_seq], its live rows before the call; NULL: 0).  Rows that fall outside 0 .. L_s - 1 are not written; no other
+ * row of the cache changes.  Per group of 32 dimensions x is the smallest integer for which 448 * 2^x (8 bits) or 6 * 2^x (4
+ * bits) reaches the largest magnitude, at least -100, and values are rounded to the nearest code, ties to the even one; magnitudes
+ * above 1.75 * 2^127 (8 bits) or 1.5 * 2^127 (4 bits) become that.  A group with a value that is not finite gets the scale byte
+ * 255: all its values read back as NaN.  shape->window must be 0; pool_k, n_q, h_q and scale (beyond their checks) do not matter.
+ * Paged: no page that is written may belong to two sequences. */
+int jq_quantize(const jq_shape* shape, const int32_t* first, const void* K, const void* V, const jq_codes* codes, void* stream);
+int jq_quantize_paged(const jq_shape* shape, const jq_pages* pages, const int32_t* first, const void* K, const void* V,
+                      const jq_codes* codes, void* stream);
+
+/* The reverse: rows first[l, s] .. first[l, s] + budgets[s] - 1 of every sequence, as the bf16 values that their codes stand for
+ * (exactly: a code has at most four significant bits).  Rows of K_out and V_out (DEVICE bf16 [n_layers, TB, h_kv, d]) that have no
+ * row in the cache are left as they were. */
+int jq_dequantize(const jq_shape* shape, const int32_t* first, const jq_codes* codes, void* K_out, void* V_out, void* stream);
+int jq_dequantize_paged(const jq_shape* shape, const jq_pages* pages, const int32_t* first, const jq_codes* codes, void* K_out,
+                        void* V_out, void* stream);
+
+/* jq_attend and jq_attend_tree over a cache of codes: the same results as over the bf16 rows that the codes stand for, up to the
+ * order of the sums, by the same rules (live rows, masks, weights, values of V that are not finite, workspace:
+ * jq_attend_workspace_bytes). */
+int jq_attend_quantized(const jq_shape* shape, const int32_t* lens, const void* Q, const jq_codes* codes, void* out,
+                        float* lse, float* weights, void* ws, size_t ws_bytes, void* stream);
+int jq_attend_quantized_paged(const jq_shape* shape, const jq_pages* pages, const int32_t* lens, const void* Q,
+                              const jq_codes* codes, void* out, float* lse, float* weights, void* ws, size_t ws_bytes,
+                              void* stream);
+int jq_attend_tree_quantized(const jq_shape* shape, const int32_t* lens, const uint32_t* seen, const void* Q,
+                             const jq_codes* codes, void* out, float* lse, void* ws, size_t ws_bytes, void* stream);
+int jq_attend_tree_quantized_paged(const jq_shape* shape, const jq_pages* pages, const int32_t* lens, const uint32_t* seen,
+                                   const void* Q, const jq_codes* codes, void* out, float* lse, void* ws, size_t ws_bytes,
+                                   void* stream);
 
 /* Measurement aid, not part of the method: a plain device-to-device copy kernel of
  * `bytes` bytes (a multiple of 16; 16-byte aligned, non-overlapping DEVICE buffers).

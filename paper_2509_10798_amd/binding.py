@@ -25,6 +25,8 @@ STATUS = {0: "JQ_OK", -1: "JQ_ERR_NULL", -2: "JQ_ERR_SHAPE", -3: "JQ_ERR_BUDGET"
 EXPORTS = ("jq_workspace_bytes", "jq_score", "jq_score_lse", "jq_evict_lse", "jq_score_tail", "jq_evict_tail", "jq_pool", "jq_select_topk", "jq_compact", "jq_compact_inplace_workspace_bytes", "jq_compact_inplace", "jq_evict", "jq_evict_inplace_workspace_bytes", "jq_evict_inplace", "jq_evict_stream", "jq_evict_static", "jq_score_paged", "jq_evict_paged", "jq_evict_paged_inplace_workspace_bytes", "jq_evict_paged_inplace", "jq_evict_traced", "jq_hit_rate", "jq_map_mse", "jq_map_mse_fused_workspace_bytes", "jq_map_mse_fused",
            "jq_attend_workspace_bytes", "jq_attend", "jq_attend_paged", "jq_attend_tree", "jq_attend_tree_paged",
            "jq_evict_weight_workspace_bytes", "jq_evict_weight", "jq_evict_weight_paged", "jq_replace_lightest", "jq_replace_lightest_paged",
+           "jq_quantize", "jq_quantize_paged", "jq_dequantize", "jq_dequantize_paged",
+           "jq_attend_quantized", "jq_attend_quantized_paged", "jq_attend_tree_quantized", "jq_attend_tree_quantized_paged",
            "jq_copy_probe", "jq_reload_knobs", "jq_status_string")
 TRACE_KERNELS = ("jq_stats_kernel", "jq_score_kernel", "jq_pool_kernel", "jq_select_finalize_kernel")
 TRACE_MARKS = 2 * len(TRACE_KERNELS)
@@ -48,6 +50,11 @@ class _CShape(ctypes.Structure):
 class _CPages(ctypes.Structure):
     _fields_ = [("page_size", ctypes.c_int32), ("n_pages", ctypes.c_int32), ("max_pages_per_seq", ctypes.c_int32),
                 ("block_table", ctypes.c_void_p)]
+
+
+class _CCodes(ctypes.Structure):
+    _fields_ = [("k_bits", ctypes.c_int32), ("v_bits", ctypes.c_int32), ("K", ctypes.c_void_p), ("V", ctypes.c_void_p),
+                ("K_scale", ctypes.c_void_p), ("V_scale", ctypes.c_void_p)]
 
 
 def lib() -> ctypes.CDLL:
@@ -99,6 +106,15 @@ def lib() -> ctypes.CDLL:
         L.jq_evict_weight_paged.argtypes = [shp, pgp] + [vp] * 11 + [sz, vp]
         L.jq_replace_lightest.argtypes = [shp] + [vp] * 10
         L.jq_replace_lightest_paged.argtypes = [shp, pgp] + [vp] * 10
+        cdp = ctypes.POINTER(_CCodes)
+        L.jq_quantize.argtypes = [shp, vp, vp, vp, cdp, vp]
+        L.jq_quantize_paged.argtypes = [shp, pgp, vp, vp, vp, cdp, vp]
+        L.jq_dequantize.argtypes = [shp, vp, cdp, vp, vp, vp]
+        L.jq_dequantize_paged.argtypes = [shp, pgp, vp, cdp, vp, vp, vp]
+        L.jq_attend_quantized.argtypes = [shp, vp, vp, cdp, vp, vp, vp, vp, sz, vp]
+        L.jq_attend_quantized_paged.argtypes = [shp, pgp, vp, vp, cdp, vp, vp, vp, vp, sz, vp]
+        L.jq_attend_tree_quantized.argtypes = [shp, vp, vp, vp, cdp, vp, vp, vp, sz, vp]
+        L.jq_attend_tree_quantized_paged.argtypes = [shp, pgp, vp, vp, vp, cdp, vp, vp, vp, sz, vp]
         L.jq_copy_probe.argtypes = [vp, vp, sz, vp]
         L.jq_reload_knobs.argtypes = []
         L.jq_status_string.argtypes = [ctypes.c_int]
@@ -552,17 +568,22 @@ def alloc_attend_workspace(shape: Shape, weights: bool = False, device="cuda"):
     return torch.empty(attend_workspace_bytes(shape, weights), dtype=torch.uint8, device=device)
 
 
-def _attend(name, shape: Shape, pages, seen, Q, K, V, lens, out, lse, want_lse, weights, ws, stream):
+def _attend(name, shape: Shape, pages, seen, Q, K, V, lens, out, lse, want_lse, weights, ws, stream, codes=None):
     import torch
-    dev, bf, f32, i32 = _device_of(K), torch.bfloat16, torch.float32, torch.int32
+    bf, f32, i32 = torch.bfloat16, torch.float32, torch.int32
     rows = (shape.n_layers, shape.n_seq, shape.n_q, shape.h_q)
-    q, kv = rows + (shape.d,), _cache_size(shape, pages, K)
+    q = rows + (shape.d,)
+    if codes is None:
+        dev, kv = _device_of(K), _cache_size(shape, pages, K)
+        cache = lambda: (_tensor("K", K, bf, kv, dev), _tensor("V", V, bf, kv, dev))
+    else:
+        dev = _device_of(codes.K)
+        cache = lambda: (ctypes.byref(codes.c_struct(shape, pages, dev)),)
     if out is None:
         out = _empty(q, bf, dev, stream)
     if lse is None and want_lse:
         lse = _empty(rows, f32, dev, stream)
-    ins = (_tensor("Q", Q, bf, q, dev), _tensor("K", K, bf, kv, dev), _tensor("V", V, bf, kv, dev), _tensor("out", out, bf, q, dev),
-           _tensor("lse", lse, f32, rows, dev))
+    ins = (_tensor("Q", Q, bf, q, dev),) + cache() + (_tensor("out", out, bf, q, dev), _tensor("lse", lse, f32, rows, dev))
     front = (_tensor("lens", lens, i32, rows[:2], dev),)
     if seen is not None:
         front += (_tensor("seen", seen, i32, (shape.n_seq, shape.n_q, -(-shape.n_q // 32)), dev),)
@@ -672,6 +693,123 @@ def replace_lightest_paged(shape: Shape, pages: Pages, k_new, v_new, token, K_po
                            stream=None):
     """replace_lightest() on a paged cache."""
     return _replace("jq_replace_lightest_paged", shape, pages, k_new, v_new, token, K_pool, V_pool, weights, pos, lens, slot_out, stream)
+
+
+# ---- a pruned cache in 8 or 4 bits -----------------------------------------------------------------------------------
+
+@dataclass
+class Codes:
+    """A cache of 8- or 4-bit codes; mirrors ``jq_codes``.  K, V: uint8 [n_layers, h_kv, T, 128 (8 bits) or 64 (4 bits)], in
+    pages [n_layers, n_pages, h_kv, page_size, ...]; K_scale, V_scale: uint8 [..., 4], one byte for every 32 dimensions."""
+    K: object
+    V: object
+    K_scale: object
+    V_scale: object
+
+    @property
+    def k_bits(self) -> int:
+        return self.K.shape[-1] // 16
+
+    @property
+    def v_bits(self) -> int:
+        return self.V.shape[-1] // 16
+
+    def c_struct(self, shape: Shape, pages: Optional[Pages], device) -> _CCodes:
+        import torch
+        u8, rows = torch.uint8, _code_rows(shape, pages)
+        for name, t in (("codes.K", self.K), ("codes.V", self.V)):
+            if t.shape[-1] not in (shape.d, shape.d // 2):
+                raise ValueError("%s: rows of %d (8 bits) or %d bytes (4 bits) are wanted, got %d" % (name, shape.d, shape.d // 2, t.shape[-1]))
+        return _CCodes(self.k_bits, self.v_bits, _tensor("codes.K", self.K, u8, rows + self.K.shape[-1:], device),
+                       _tensor("codes.V", self.V, u8, rows + self.V.shape[-1:], device),
+                       _tensor("codes.K_scale", self.K_scale, u8, rows + (shape.d // 32,), device),
+                       _tensor("codes.V_scale", self.V_scale, u8, rows + (shape.d // 32,), device))
+
+
+def _code_rows(shape: Shape, pages):
+    if pages is None:
+        return (shape.n_layers, shape.h_kv, shape.T)
+    return (shape.n_layers, pages.n_pages, shape.h_kv, pages.page_size)
+
+
+def alloc_codes(shape: Shape, k_bits: int = 8, v_bits: int = 8, pages: Optional[Pages] = None, device="cuda") -> Codes:
+    """A cache of codes with room for shape.seq_lens rows, or for the pages of `pages`; nothing in it is written."""
+    import torch
+    if k_bits not in (8, 4) or v_bits not in (8, 4):
+        raise ValueError("codes have 8 or 4 bits, not %s and %s" % (k_bits, v_bits))
+    rows = _code_rows(shape, pages)
+    return Codes(*(torch.empty(rows + (n,), dtype=torch.uint8, device=device) for n in (shape.d * k_bits // 8, shape.d * v_bits // 8, shape.d // 32, shape.d // 32)))
+
+
+def _rows_of_codes(name, shape: Shape, pages, K, V, codes, first, stream):
+    import torch
+    dev, bf, i32 = _device_of(codes.K), torch.bfloat16, torch.int32
+    kept = (shape.n_layers, shape.TB, shape.h_kv, shape.d)
+    kv = lambda what: (_tensor("K" + what, K, bf, kept, dev), _tensor("V" + what, V, bf, kept, dev))
+    at = _tensor("first", first, i32, (shape.n_layers, shape.n_seq), dev)
+    _tensor("layer_budgets", shape.layer_budgets, i32, (shape.n_layers, shape.n_seq), dev)
+    c = ctypes.byref(codes.c_struct(shape, pages, dev))
+    args = (at,) + kv("") + (c,) if name.startswith("jq_quantize") else (at, c) + kv("_out")
+    _call(name, shape, pages, dev, stream, *args)
+
+
+def quantize(shape: Shape, K, V, codes: Codes, first=None, stream=None):
+    """Rows K, V [n_layers, sum of budgets, h_kv, d] bf16 (a pruned cache, or new tokens' rows) written into a cache of codes: row
+    b of sequence s becomes row first[l, s] + b (int32 [n_layers, n_seq], the live rows so far; None: 0).  Rows for which there is no
+    room are not written.  Returns codes."""
+    _rows_of_codes("jq_quantize", shape, None, K, V, codes, first, stream)
+    return codes
+
+
+def quantize_paged(shape: Shape, pages: Pages, K, V, codes: Codes, first=None, stream=None):
+    """quantize() into a paged cache of codes."""
+    _rows_of_codes("jq_quantize_paged", shape, pages, K, V, codes, first, stream)
+    return codes
+
+
+def _dequantize(name, shape: Shape, pages, codes, first, K_out, V_out, stream):
+    import torch
+    dev, kept = _device_of(codes.K), (shape.n_layers, shape.TB, shape.h_kv, shape.d)
+    K_out, V_out = (_empty(kept, torch.bfloat16, dev, stream) if x is None else x for x in (K_out, V_out))
+    _rows_of_codes(name, shape, pages, K_out, V_out, codes, first, stream)
+    return K_out, V_out
+
+
+def dequantize(shape: Shape, codes: Codes, first=None, K_out=None, V_out=None, stream=None):
+    """Rows first[l, s] .. first[l, s] + shape.budgets[s] - 1 of a cache of codes as bf16 [n_layers, sum of budgets, h_kv, d], exactly what
+    the codes stand for.  Rows that the cache does not have are left as they were.  Returns (K_out, V_out)."""
+    return _dequantize("jq_dequantize", shape, None, codes, first, K_out, V_out, stream)
+
+
+def dequantize_paged(shape: Shape, pages: Pages, codes: Codes, first=None, K_out=None, V_out=None, stream=None):
+    """dequantize() of a paged cache of codes."""
+    return _dequantize("jq_dequantize_paged", shape, pages, codes, first, K_out, V_out, stream)
+
+
+def attend_quantized(shape: Shape, Q, codes: Codes, lens=None, weights=None, out=None, lse=None, ws=None, stream=None, want_lse=True):
+    """attend() over a cache of codes."""
+    return _attend("jq_attend_quantized", shape, None, None, Q, None, None, lens, out, lse, want_lse, weights, ws, stream, codes)
+
+
+def attend_quantized_paged(shape: Shape, pages: Pages, Q, codes: Codes, lens=None, weights=None, out=None, lse=None, ws=None, stream=None,
+                           want_lse=True):
+    """attend_paged() over a paged cache of codes."""
+    return _attend("jq_attend_quantized_paged", shape, pages, None, Q, None, None, lens, out, lse, want_lse, weights, ws, stream, codes)
+
+
+def attend_tree_quantized(shape: Shape, seen, Q, codes: Codes, lens=None, out=None, lse=None, ws=None, stream=None, want_lse=True):
+    """attend_tree() over a cache of codes."""
+    if seen is None:
+        raise JQError(-1, "jq_attend_tree_quantized")
+    return _attend("jq_attend_tree_quantized", shape, None, seen, Q, None, None, lens, out, lse, want_lse, None, ws, stream, codes)
+
+
+def attend_tree_quantized_paged(shape: Shape, pages: Pages, seen, Q, codes: Codes, lens=None, out=None, lse=None, ws=None, stream=None,
+                                want_lse=True):
+    """attend_tree_paged() over a paged cache of codes."""
+    if seen is None:
+        raise JQError(-1, "jq_attend_tree_quantized_paged")
+    return _attend("jq_attend_tree_quantized_paged", shape, pages, seen, Q, None, None, lens, out, lse, want_lse, None, ws, stream, codes)
 
 
 def reload_knobs() -> None:

@@ -731,8 +731,23 @@ int jq_attend_workspace_bytes(const jq_shape* shape, int32_t with_weights, size_
     return JQ_OK;
 }
 
+// One of K and V in a cache of codes, or its scales.
+static size_t code_bytes(const Plan& p, int row_bytes) { return kv_bytes(p) / (kHeadDim * 2) * row_bytes; }
+constexpr int kScaleBytes = kHeadDim / 32;
+static int check_codes(const jq_codes* c, Codes* out) {
+    if (!c) return JQ_ERR_NULL;
+    if ((c->k_bits != 8 && c->k_bits != 4) || (c->v_bits != 8 && c->v_bits != 4)) return JQ_ERR_SHAPE;
+    if (c->k_bits < c->v_bits) return JQ_ERR_UNSUPPORTED;
+    if (!c->K || !c->V || !c->K_scale || !c->V_scale) return JQ_ERR_NULL;
+    if (misaligned(c->K, 16) || misaligned(c->V, 16) || misaligned(c->K_scale, 4) || misaligned(c->V_scale, 4)) return JQ_ERR_UNSUPPORTED;
+    *out = Codes{c->k_bits, c->v_bits, c->K, c->V, c->K_scale, c->V_scale};
+    return JQ_OK;
+}
+
+// (With `coded` the cache is `codes`, and K and V are not looked at.)
 static int attend_impl(const jq_shape* shape, const jq_pages* pages, bool paged, const int32_t* lens, const uint32_t* seen, bool tree, const void* Q,
-                       const void* K, const void* V, void* out, float* lse, float* weights, void* ws, size_t ws_bytes, void* stream) {
+                       const void* K, const void* V, void* out, float* lse, float* weights, void* ws, size_t ws_bytes, void* stream, bool coded = false,
+                       const jq_codes* codes = nullptr) {
     Plan p;
     AttendPlan ap;
     int rc = attend_plan(shape, weights != nullptr, &p, &ap);
@@ -744,16 +759,21 @@ static int attend_impl(const jq_shape* shape, const jq_pages* pages, bool paged,
         for (int s = 0; s < p.n_seq; ++s)
             if (p.tab.cu_seq[s + 1] - p.tab.cu_seq[s] < p.n_q) return JQ_ERR_SHAPE;  // no room for the drafted tokens' rows
     }
+    Codes c{};
+    if (coded && (rc = check_codes(codes, &c)) != JQ_OK) return rc;
+    if (coded) { K = c.K; V = c.V; }
     if (!Q || !K || !V || !out || (tree && !seen) || !ws) return JQ_ERR_NULL;
     if (misaligned(ws, 16) || ws_bytes < ap.ws_bytes) return JQ_ERR_WORKSPACE;
     if (misaligned(Q, 16) || misaligned(K, 16) || misaligned(V, 16) || misaligned(out, 16) || (lse && misaligned(lse, 4)) ||
         (weights && misaligned(weights, 4)) || (lens && misaligned(lens, 4)) || (seen && misaligned(seen, 4)))
         return JQ_ERR_UNSUPPORTED;
-    const Buf ins[6] = {{Q, q_bytes(p)}, {K, kv_bytes(p)}, {V, kv_bytes(p)}, {lens, lens_bytes(p)},
-                        {seen, (size_t)p.n_seq * p.n_q * ((p.n_q + 31) / 32) * 4}, {p.block_table, table_bytes(p)}};
+    const Buf ins[8] = {{Q, q_bytes(p)}, {K, coded ? code_bytes(p, c.k_bits * (kHeadDim / 8)) : kv_bytes(p)},
+                        {V, coded ? code_bytes(p, c.v_bits * (kHeadDim / 8)) : kv_bytes(p)}, {lens, lens_bytes(p)},
+                        {seen, (size_t)p.n_seq * p.n_q * ((p.n_q + 31) / 32) * 4}, {p.block_table, table_bytes(p)},
+                        {c.K_scale, code_bytes(p, kScaleBytes)}, {c.V_scale, code_bytes(p, kScaleBytes)}};
     const Buf outs[4] = {{out, q_bytes(p)}, {lse, lse_bytes(p)}, {weights, score_bytes(p)}, {ws, ap.ws_bytes}};
-    if (any_overlap(outs, 4, ins, 6)) return JQ_ERR_ALIAS;
-    return launch_status(launch_attend(p, ap, lens, seen, Q, K, V, out, lse, weights, (char*)ws, (hipStream_t)stream));
+    if (any_overlap(outs, 4, ins, 8)) return JQ_ERR_ALIAS;
+    return launch_status(launch_attend(p, ap, lens, seen, Q, K, V, out, lse, weights, (char*)ws, (hipStream_t)stream, coded ? &c : nullptr));
 }
 
 int jq_attend(const jq_shape* shape, const int32_t* lens, const void* Q, const void* K, const void* V, void* out, float* lse, float* weights, void* ws,
@@ -774,6 +794,70 @@ int jq_attend_tree(const jq_shape* shape, const int32_t* lens, const uint32_t* s
 int jq_attend_tree_paged(const jq_shape* shape, const jq_pages* pages, const int32_t* lens, const uint32_t* seen, const void* Q, const void* K_pool,
                          const void* V_pool, void* out, float* lse, void* ws, size_t ws_bytes, void* stream) {
     return attend_impl(shape, pages, true, lens, seen, true, Q, K_pool, V_pool, out, lse, nullptr, ws, ws_bytes, stream);
+}
+
+int jq_attend_quantized(const jq_shape* shape, const int32_t* lens, const void* Q, const jq_codes* codes, void* out, float* lse, float* weights, void* ws,
+                        size_t ws_bytes, void* stream) {
+    return attend_impl(shape, nullptr, false, lens, nullptr, false, Q, nullptr, nullptr, out, lse, weights, ws, ws_bytes, stream, true, codes);
+}
+
+int jq_attend_quantized_paged(const jq_shape* shape, const jq_pages* pages, const int32_t* lens, const void* Q, const jq_codes* codes, void* out, float* lse,
+                              float* weights, void* ws, size_t ws_bytes, void* stream) {
+    return attend_impl(shape, pages, true, lens, nullptr, false, Q, nullptr, nullptr, out, lse, weights, ws, ws_bytes, stream, true, codes);
+}
+
+int jq_attend_tree_quantized(const jq_shape* shape, const int32_t* lens, const uint32_t* seen, const void* Q, const jq_codes* codes, void* out, float* lse,
+                             void* ws, size_t ws_bytes, void* stream) {
+    return attend_impl(shape, nullptr, false, lens, seen, true, Q, nullptr, nullptr, out, lse, nullptr, ws, ws_bytes, stream, true, codes);
+}
+
+int jq_attend_tree_quantized_paged(const jq_shape* shape, const jq_pages* pages, const int32_t* lens, const uint32_t* seen, const void* Q,
+                                   const jq_codes* codes, void* out, float* lse, void* ws, size_t ws_bytes, void* stream) {
+    return attend_impl(shape, pages, true, lens, seen, true, Q, nullptr, nullptr, out, lse, nullptr, ws, ws_bytes, stream, true, codes);
+}
+
+// Rows written into a cache of codes (`write`), or read back.
+static int codes_impl(const jq_shape* shape, const jq_pages* pages, bool paged, bool write, const int32_t* first, const void* K, const void* V,
+                      const jq_codes* codes, void* stream) {
+    Plan p;
+    Codes c;
+    int rc = make_plan(shape, true, &p, false);
+    if (rc != JQ_OK) return rc;
+    if (p.window) return JQ_ERR_SHAPE;  // no queries here
+    if (!codes_fit(p)) return JQ_ERR_UNSUPPORTED;
+    if (paged && (rc = apply_pages(pages, &p)) != JQ_OK) return rc;
+    if ((rc = check_codes(codes, &c)) != JQ_OK) return rc;
+    if (!K || !V) return JQ_ERR_NULL;
+    if (misaligned(K, 16) || misaligned(V, 16) || (first && misaligned(first, 4))) return JQ_ERR_UNSUPPORTED;
+    const size_t rows = kv_out_bytes(p), scales = code_bytes(p, kScaleBytes);
+    const Buf in_codes[4] = {{c.K, code_bytes(p, c.k_bits * (kHeadDim / 8))}, {c.V, code_bytes(p, c.v_bits * (kHeadDim / 8))}, {c.K_scale, scales}, {c.V_scale, scales}};
+    const Buf small[3] = {{first, lens_bytes(p)}, {p.block_table, table_bytes(p)}, {p.layer_budgets, lb_bytes(p)}};
+    Buf ins[7] = {small[0], small[1], small[2]}, outs[4];
+    if (write) {
+        ins[3] = Buf{K, rows}; ins[4] = Buf{V, rows};
+        if (any_overlap(in_codes, 4, ins, 5)) return JQ_ERR_ALIAS;
+        return launch_status(launch_quantize(p, c, first, K, V, (hipStream_t)stream));
+    }
+    outs[0] = Buf{K, rows}; outs[1] = Buf{V, rows};
+    for (int i = 0; i < 4; ++i) ins[3 + i] = in_codes[i];
+    if (any_overlap(outs, 2, ins, 7)) return JQ_ERR_ALIAS;
+    return launch_status(launch_dequantize(p, c, first, const_cast<void*>(K), const_cast<void*>(V), (hipStream_t)stream));
+}
+
+int jq_quantize(const jq_shape* shape, const int32_t* first, const void* K, const void* V, const jq_codes* codes, void* stream) {
+    return codes_impl(shape, nullptr, false, true, first, K, V, codes, stream);
+}
+
+int jq_quantize_paged(const jq_shape* shape, const jq_pages* pages, const int32_t* first, const void* K, const void* V, const jq_codes* codes, void* stream) {
+    return codes_impl(shape, pages, true, true, first, K, V, codes, stream);
+}
+
+int jq_dequantize(const jq_shape* shape, const int32_t* first, const jq_codes* codes, void* K_out, void* V_out, void* stream) {
+    return codes_impl(shape, nullptr, false, false, first, K_out, V_out, codes, stream);
+}
+
+int jq_dequantize_paged(const jq_shape* shape, const jq_pages* pages, const int32_t* first, const jq_codes* codes, void* K_out, void* V_out, void* stream) {
+    return codes_impl(shape, pages, true, false, first, K_out, V_out, codes, stream);
 }
 
 int jq_evict_weight_workspace_bytes(const jq_shape* shape, size_t* bytes) {

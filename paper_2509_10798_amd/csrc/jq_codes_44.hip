@@ -1,0 +1,6 @@
+// Attention over a cache of codes: keys in 4 bits, values in 4.
+#include "jq_codes.h"
+
+namespace jq {
+template hipError_t launch_sweeps<RowsCoded<4, 4>>(const AttendArgs&, int, bool, dim3, hipStream_t);
+}  // namespace jq

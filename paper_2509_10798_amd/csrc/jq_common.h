@@ -363,8 +363,17 @@ struct AttendPlan {
 void plan_attend(const Plan& p, bool weights, AttendPlan* ap);
 bool attend_fits(const Plan& p, const AttendPlan& ap, bool weights);  // every launch stays below 2^32 threads
 // `lens`, `seen`, `lse`, `weights` may be null; with `seen` the queries are drafted tokens, otherwise p.window says whether they are causal.
+// With `codes` the cache is one of codes, and K and V are null.
+struct Codes {
+    int32_t k_bits, v_bits;
+    void *K, *V, *K_scale, *V_scale;
+};
 hipError_t launch_attend(const Plan& p, const AttendPlan& ap, const int32_t* lens, const uint32_t* seen, const void* Q, const void* K, const void* V,
-                         void* out, float* lse, float* weights, char* ws, hipStream_t st);
+                         void* out, float* lse, float* weights, char* ws, hipStream_t st, const Codes* codes = nullptr);
+// Rows written into a cache of codes at rows first[layer][sequence] (null: 0) and up, and read back (jq_codes.hip).
+bool codes_fit(const Plan& p);
+hipError_t launch_quantize(const Plan& p, const Codes& c, const int32_t* first, const void* K, const void* V, hipStream_t st);
+hipError_t launch_dequantize(const Plan& p, const Codes& c, const int32_t* first, void* K, void* V, hipStream_t st);
 // K_out == K (then V_out == V, weights_out == weights and pos_out == pos too): within one cache.  `idx` [n_layers][h_kv][TB] takes the kept rows.
 // `cu_piece`, `cu_cand`: pieces of the long sequences, rows that they leave, summed up (none: sequences are selected from whole).
 struct WeightPlan {
