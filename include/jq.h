@@ -21,6 +21,7 @@
  *   jq_score_paged, jq_evict_paged  the same on a paged cache (pools + block table)
  *   jq_attend, jq_attend_tree     attention of the newest tokens, or of a tree of drafted ones, over a pruned cache
  *   jq_evict_weight, jq_replace_lightest   eviction by accumulated attention weight: of many rows, or of one for a new token's
+ *   jq_attend_shared   jq_attend of sequences that continue shared prefixes, each of which is read once
  *   jq_quantize, jq_dequantize    rows written into a cache of 8- or 4-bit codes, and read back
  *   jq_attend_quantized, jq_attend_tree_quantized   jq_attend and jq_attend_tree over such a cache
  *   jq_hit_rate     critical-KV hit rate between two kept sets (Eq. 6)
@@ -453,6 +454,31 @@ int jq_replace_lightest(const jq_shape* shape, const int32_t* lens, const void* 
 int jq_replace_lightest_paged(const jq_shape* shape, const jq_pages* pages, const int32_t* lens, const void* k_new,
                               const void* v_new, const int32_t* token, void* K_pool, void* V_pool, float* weights,
                               int32_t* pos, int32_t* slot_out, void* stream);
+
+/* jq_attend of sequences that continue shared prefixes: many answers begun from one prompt, whose (pruned) cache they then
+ * share.  Sequences cu_members[p] .. cu_members[p+1] - 1 continue prefix p: each of their queries attends to all live rows of
+ * the prefix and to those of the sequence's own live rows that jq_attend would show it (shape->window = 1: causal among the last
+ * n_q of them), under one softmax.  A prefix is read once, whatever the number of sequences that continue it.  Prefixes have
+ * room for cu_rows[p+1] - cu_rows[p] rows, of which lens[l, p] are live, and lie in K_prefix, V_prefix (DEVICE bf16
+ * [n_layers, cu_rows[n_prefix], h_kv, d]); a sequence that shares none is the only one to continue a prefix of its own, which may
+ * have no live rows.  Paged: prefixes and sequences lie in the same pools, each behind a block table of their own.  Conditions,
+ * accuracy and values of V that are not finite as for jq_attend, with the query rows of all sequences that continue a prefix for
+ * those of one KV head; `ws` must hold jq_attend_shared_workspace_bytes. */
+typedef struct jq_prefixes {
+    int32_t n_prefix;             /* 1..n_seq                                                           */
+    const int32_t* cu_members;    /* HOST [n_prefix+1]; 0 first, strictly increasing, n_seq last        */
+    const int32_t* cu_rows;       /* HOST [n_prefix+1]; 0 first, strictly increasing                    */
+    const int32_t* lens;          /* DEVICE int32 [n_layers, n_prefix], or NULL: all rows are live      */
+    int32_t max_pages_per_prefix; /* paged calls: row length of block_table                             */
+    const int32_t* block_table;   /* paged calls: DEVICE int32 [n_prefix, max_pages_per_prefix]         */
+} jq_prefixes;
+int jq_attend_shared_workspace_bytes(const jq_shape* shape, const jq_prefixes* prefixes, size_t* bytes);
+int jq_attend_shared(const jq_shape* shape, const jq_prefixes* prefixes, const int32_t* lens, const void* Q,
+                     const void* K_prefix, const void* V_prefix, const void* K, const void* V, void* out, float* lse,
+                     void* ws, size_t ws_bytes, void* stream);
+int jq_attend_shared_paged(const jq_shape* shape, const jq_pages* pages, const jq_prefixes* prefixes, const int32_t* lens,
+                           const void* Q, const void* K_pool, const void* V_pool, void* out, float* lse, void* ws,
+                           size_t ws_bytes, void* stream);
 
 /* ---- A pruned cache in 8 or 4 bits (Section 4.3: decoding continues on the pruned cache) ---------------------
  * Eviction keeps fewer rows of a cache; codes make each row that is left half or a quarter as large.  Every 32 neighbouring

@@ -12,7 +12,7 @@ LIB = os.path.join(PKG, "libjq.so")
 OBJ = os.path.join(PKG, "_build")
 # the eviction path is one translation unit (csrc/jq_lib.hip says why), the kernels of decoding on a pruned cache another; the
 # other .hip files are their parts
-SOURCES = ["jq_lib.hip", "jq_decode.hip", "jq_codes.hip", "jq_codes_88.hip", "jq_codes_84.hip", "jq_codes_44.hip"]
+SOURCES = ["jq_lib.hip", "jq_decode.hip", "jq_codes.hip", "jq_codes_88.hip", "jq_codes_84.hip", "jq_codes_44.hip", "jq_shared.hip"]
 FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall",
     "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",

@@ -25,6 +25,7 @@ STATUS = {0: "JQ_OK", -1: "JQ_ERR_NULL", -2: "JQ_ERR_SHAPE", -3: "JQ_ERR_BUDGET"
 EXPORTS = ("jq_workspace_bytes", "jq_score", "jq_score_lse", "jq_evict_lse", "jq_score_tail", "jq_evict_tail", "jq_pool", "jq_select_topk", "jq_compact", "jq_compact_inplace_workspace_bytes", "jq_compact_inplace", "jq_evict", "jq_evict_inplace_workspace_bytes", "jq_evict_inplace", "jq_evict_stream", "jq_evict_static", "jq_score_paged", "jq_evict_paged", "jq_evict_paged_inplace_workspace_bytes", "jq_evict_paged_inplace", "jq_evict_traced", "jq_hit_rate", "jq_map_mse", "jq_map_mse_fused_workspace_bytes", "jq_map_mse_fused",
            "jq_attend_workspace_bytes", "jq_attend", "jq_attend_paged", "jq_attend_tree", "jq_attend_tree_paged",
            "jq_evict_weight_workspace_bytes", "jq_evict_weight", "jq_evict_weight_paged", "jq_replace_lightest", "jq_replace_lightest_paged",
+           "jq_attend_shared_workspace_bytes", "jq_attend_shared", "jq_attend_shared_paged",
            "jq_quantize", "jq_quantize_paged", "jq_dequantize", "jq_dequantize_paged",
            "jq_attend_quantized", "jq_attend_quantized_paged", "jq_attend_tree_quantized", "jq_attend_tree_quantized_paged",
            "jq_copy_probe", "jq_reload_knobs", "jq_status_string")
@@ -55,6 +56,11 @@ class _CPages(ctypes.Structure):
 class _CCodes(ctypes.Structure):
     _fields_ = [("k_bits", ctypes.c_int32), ("v_bits", ctypes.c_int32), ("K", ctypes.c_void_p), ("V", ctypes.c_void_p),
                 ("K_scale", ctypes.c_void_p), ("V_scale", ctypes.c_void_p)]
+
+
+class _CPrefixes(ctypes.Structure):
+    _fields_ = [("n_prefix", ctypes.c_int32), ("cu_members", ctypes.POINTER(ctypes.c_int32)), ("cu_rows", ctypes.POINTER(ctypes.c_int32)),
+                ("lens", ctypes.c_void_p), ("max_pages_per_prefix", ctypes.c_int32), ("block_table", ctypes.c_void_p)]
 
 
 def lib() -> ctypes.CDLL:
@@ -106,6 +112,10 @@ def lib() -> ctypes.CDLL:
         L.jq_evict_weight_paged.argtypes = [shp, pgp] + [vp] * 11 + [sz, vp]
         L.jq_replace_lightest.argtypes = [shp] + [vp] * 10
         L.jq_replace_lightest_paged.argtypes = [shp, pgp] + [vp] * 10
+        pfp = ctypes.POINTER(_CPrefixes)
+        L.jq_attend_shared_workspace_bytes.argtypes = [shp, pfp, ctypes.POINTER(sz)]
+        L.jq_attend_shared.argtypes = [shp, pfp] + [vp] * 9 + [sz, vp]
+        L.jq_attend_shared_paged.argtypes = [shp, pgp, pfp] + [vp] * 7 + [sz, vp]
         cdp = ctypes.POINTER(_CCodes)
         L.jq_quantize.argtypes = [shp, vp, vp, vp, cdp, vp]
         L.jq_quantize_paged.argtypes = [shp, pgp, vp, vp, vp, cdp, vp]
@@ -693,6 +703,83 @@ def replace_lightest_paged(shape: Shape, pages: Pages, k_new, v_new, token, K_po
                            stream=None):
     """replace_lightest() on a paged cache."""
     return _replace("jq_replace_lightest_paged", shape, pages, k_new, v_new, token, K_pool, V_pool, weights, pos, lens, slot_out, stream)
+
+
+@dataclass
+class Prefixes:
+    """Prefixes that sequences of a batch continue; mirrors ``jq_prefixes``.  `seq_lens`: rows that each has room for; `members`: how
+    many sequences continue each, in the batch's order; `lens`: int32 device tensor [n_layers, n_prefix] of live rows (None: all);
+    `block_table`: for paged calls, int32 device tensor [n_prefix, pages]."""
+    seq_lens: Sequence[int]
+    members: Sequence[int]
+    lens: object = None
+    block_table: object = None
+    _keep: list = field(default_factory=list, repr=False)
+
+    @property
+    def T(self) -> int:
+        return int(sum(self.seq_lens))
+
+    def c_struct(self) -> _CPrefixes:
+        bt = self.block_table
+        key = (tuple(self.seq_lens), tuple(self.members), _ptr(self.lens), _ptr(bt), None if bt is None else tuple(bt.shape))
+        if self._keep and self._keep[0] == key:
+            return self._keep[3]
+        if len(self.members) != len(self.seq_lens):
+            raise ValueError("%d prefixes, members of %d" % (len(self.seq_lens), len(self.members)))
+        cu = [np.concatenate([[0], np.cumsum(np.asarray(x, dtype=np.int64))]).astype(np.int32) for x in (self.members, self.seq_lens)]
+        i32p = ctypes.POINTER(ctypes.c_int32)
+        cs = _CPrefixes(len(self.seq_lens), cu[0].ctypes.data_as(i32p), cu[1].ctypes.data_as(i32p), _ptr(self.lens), 0 if bt is None else int(bt.shape[1]), _ptr(bt))
+        self._keep = [key, cu[0], cu[1], cs]  # the host arrays must outlive the struct
+        return cs
+
+
+def attend_shared_workspace_bytes(shape: Shape, prefixes: Prefixes) -> int:
+    n = ctypes.c_size_t(0)
+    _check(lib().jq_attend_shared_workspace_bytes(ctypes.byref(shape.c_struct()), ctypes.byref(prefixes.c_struct()), ctypes.byref(n)),
+           "jq_attend_shared_workspace_bytes")
+    return int(n.value)
+
+
+def alloc_attend_shared_workspace(shape: Shape, prefixes: Prefixes, device="cuda"):
+    import torch
+    return torch.empty(attend_shared_workspace_bytes(shape, prefixes), dtype=torch.uint8, device=device)
+
+
+def _attend_shared(name, shape: Shape, pages, prefixes, Q, K_prefix, V_prefix, K, V, lens, out, lse, want_lse, ws, stream):
+    import torch
+    dev, bf, f32, i32 = _device_of(K), torch.bfloat16, torch.float32, torch.int32
+    rows = (shape.n_layers, shape.n_seq, shape.n_q, shape.h_q)
+    q, kv, n = rows + (shape.d,), _cache_size(shape, pages, K), len(prefixes.seq_lens)
+    if out is None:
+        out = _empty(q, bf, dev, stream)
+    if lse is None and want_lse:
+        lse = _empty(rows, f32, dev, stream)
+    c = ctypes.byref(prefixes.c_struct())
+    _tensor("prefixes.lens", prefixes.lens, i32, (shape.n_layers, n), dev)
+    caches = (_tensor("K", K, bf, kv, dev), _tensor("V", V, bf, kv, dev))
+    if pages is None:
+        pkv = (shape.n_layers, prefixes.T, shape.h_kv, shape.d)
+        caches = (_tensor("K_prefix", K_prefix, bf, pkv, dev), _tensor("V_prefix", V_prefix, bf, pkv, dev)) + caches
+    elif prefixes.block_table is not None:
+        _tensor("prefixes.block_table", prefixes.block_table, i32, (n, prefixes.block_table.shape[-1]), dev)
+    args = (c, _tensor("lens", lens, i32, rows[:2], dev), _tensor("Q", Q, bf, q, dev)) + caches + (_tensor("out", out, bf, q, dev), _tensor("lse", lse, f32, rows, dev))
+    sp, size, ws = _workspace(ws, lambda: attend_shared_workspace_bytes(shape, prefixes), dev, stream)
+    _call(name, shape, pages, dev, stream, *args, sp, size)
+    return out, lse
+
+
+def attend_shared(shape: Shape, prefixes: Prefixes, Q, K_prefix, V_prefix, K, V, lens=None, out=None, lse=None, ws=None, stream=None, want_lse=True):
+    """attend() of sequences that continue shared prefixes: every query attends to the live rows of its sequence's prefix (K_prefix,
+    V_prefix [n_layers, prefixes.T, h_kv, d]) and to the sequence's own (K, V, lens, shape.window as in attend()), under one
+    softmax.  A prefix is read once for all the sequences that continue it.  Returns (out, log-sum-exps)."""
+    return _attend_shared("jq_attend_shared", shape, None, prefixes, Q, K_prefix, V_prefix, K, V, lens, out, lse, want_lse, ws, stream)
+
+
+def attend_shared_paged(shape: Shape, pages: Pages, prefixes: Prefixes, Q, K_pool, V_pool, lens=None, out=None, lse=None, ws=None, stream=None,
+                        want_lse=True):
+    """attend_shared() on a paged cache: sequences behind the block table of `pages`, prefixes behind their own, in the same pools."""
+    return _attend_shared("jq_attend_shared_paged", shape, pages, prefixes, Q, None, None, K_pool, V_pool, lens, out, lse, want_lse, ws, stream)
 
 
 # ---- a pruned cache in 8 or 4 bits -----------------------------------------------------------------------------------

@@ -860,6 +860,67 @@ int jq_dequantize_paged(const jq_shape* shape, const jq_pages* pages, const int3
     return codes_impl(shape, pages, true, false, first, K_out, V_out, codes, stream);
 }
 
+// The plans of a call over shared prefixes.
+static int shared_plan(const jq_shape* shape, const jq_prefixes* pre, Plan* p, Plan* pp, SharedPlan* sp) {
+    int rc = make_plan(shape, false, p, false);
+    if (rc != JQ_OK) return rc;
+    if (!pre || !pre->cu_members || !pre->cu_rows) return JQ_ERR_NULL;
+    if (pre->n_prefix < 1 || pre->n_prefix > p->n_seq || pre->cu_members[0] != 0 || pre->cu_members[pre->n_prefix] != p->n_seq) return JQ_ERR_SHAPE;
+    for (int i = 0; i < pre->n_prefix; ++i) {
+        if (pre->cu_members[i + 1] <= pre->cu_members[i]) return JQ_ERR_SHAPE;
+        if ((int64_t)(pre->cu_members[i + 1] - pre->cu_members[i]) * p->rows > (1 << 20)) return JQ_ERR_UNSUPPORTED;
+    }
+    jq_shape of = *shape;  // the prefixes as a batch of their own
+    of.n_seq = pre->n_prefix; of.cu_seqlens = pre->cu_rows; of.n_q = 1; of.window = 0; of.budgets = nullptr; of.layer_budgets = nullptr;
+    if ((rc = make_plan(&of, false, pp, false)) != JQ_OK) return rc;
+    plan_shared(*p, *pp, pre->cu_members, sp);
+    return sp->fits ? JQ_OK : JQ_ERR_UNSUPPORTED;
+}
+
+int jq_attend_shared_workspace_bytes(const jq_shape* shape, const jq_prefixes* prefixes, size_t* bytes) {
+    if (!bytes) return JQ_ERR_NULL;
+    Plan p, pp;
+    SharedPlan sp;
+    const int rc = shared_plan(shape, prefixes, &p, &pp, &sp);
+    if (rc != JQ_OK) return rc;
+    *bytes = sp.ws_bytes;
+    return JQ_OK;
+}
+
+static int shared_impl(const jq_shape* shape, const jq_pages* pages, bool paged, const jq_prefixes* pre, const int32_t* lens, const void* Q, const void* K_prefix,
+                       const void* V_prefix, const void* K, const void* V, void* out, float* lse, void* ws, size_t ws_bytes, void* stream) {
+    Plan p, pp;
+    SharedPlan sp;
+    int rc = shared_plan(shape, pre, &p, &pp, &sp);
+    if (rc != JQ_OK) return rc;
+    if (paged) {
+        if ((rc = apply_pages(pages, &p)) != JQ_OK) return rc;
+        jq_pages of = *pages;
+        of.max_pages_per_seq = pre->max_pages_per_prefix; of.block_table = pre->block_table;
+        if ((rc = apply_pages(&of, &pp)) != JQ_OK) return rc;
+    }
+    if (!Q || !K_prefix || !V_prefix || !K || !V || !out || !ws) return JQ_ERR_NULL;
+    if (misaligned(ws, 16) || ws_bytes < sp.ws_bytes) return JQ_ERR_WORKSPACE;
+    if (misaligned(Q, 16) || misaligned(K_prefix, 16) || misaligned(V_prefix, 16) || misaligned(K, 16) || misaligned(V, 16) || misaligned(out, 16) ||
+        (lse && misaligned(lse, 4)) || (lens && misaligned(lens, 4)) || (pre->lens && misaligned(pre->lens, 4)))
+        return JQ_ERR_UNSUPPORTED;
+    const Buf ins[9] = {{Q, q_bytes(p)}, {K_prefix, kv_bytes(pp)}, {V_prefix, kv_bytes(pp)}, {K, kv_bytes(p)}, {V, kv_bytes(p)}, {lens, lens_bytes(p)},
+                        {pre->lens, lens_bytes(pp)}, {p.block_table, table_bytes(p)}, {pp.block_table, table_bytes(pp)}};
+    const Buf outs[3] = {{out, q_bytes(p)}, {lse, lse_bytes(p)}, {ws, sp.ws_bytes}};
+    if (any_overlap(outs, 3, ins, 9)) return JQ_ERR_ALIAS;
+    return launch_status(launch_attend_shared(p, pp, sp, pre->cu_members, lens, pre->lens, Q, K_prefix, V_prefix, K, V, out, lse, (char*)ws, (hipStream_t)stream));
+}
+
+int jq_attend_shared(const jq_shape* shape, const jq_prefixes* prefixes, const int32_t* lens, const void* Q, const void* K_prefix, const void* V_prefix,
+                     const void* K, const void* V, void* out, float* lse, void* ws, size_t ws_bytes, void* stream) {
+    return shared_impl(shape, nullptr, false, prefixes, lens, Q, K_prefix, V_prefix, K, V, out, lse, ws, ws_bytes, stream);
+}
+
+int jq_attend_shared_paged(const jq_shape* shape, const jq_pages* pages, const jq_prefixes* prefixes, const int32_t* lens, const void* Q, const void* K_pool,
+                           const void* V_pool, void* out, float* lse, void* ws, size_t ws_bytes, void* stream) {
+    return shared_impl(shape, pages, true, prefixes, lens, Q, K_pool, V_pool, K_pool, V_pool, out, lse, ws, ws_bytes, stream);
+}
+
 int jq_evict_weight_workspace_bytes(const jq_shape* shape, size_t* bytes) {
     if (!bytes) return JQ_ERR_NULL;
     Plan p;

@@ -44,6 +44,7 @@ constexpr float kLargeSum = 16777216.0f;  // or, with many query rows, until a l
 enum AttendMask { kSeeAll = 0, kSeeCausal, kSeeTree };
 
 struct AttendArgs {
+    static constexpr int kShare = 0;
     const char* Q; const char* K; const char* V;
     const int32_t* lens;   // DEVICE [n_layers][n_seq] live rows, or null: all
     const uint32_t* seen;  // kSeeTree: DEVICE [n_seq][n_q][words]
@@ -63,6 +64,34 @@ struct AttendArgs {
     int32_t cu_split[JQ_MAX_SEQ + 1];
     const uint8_t* K_scale; const uint8_t* V_scale;  // of codes
 };
+
+// Sequences that continue shared prefixes (jq_shared.hip): a sweep over the prefixes, whose query rows are those of all the sequences
+// that continue one, and a sweep over the sequences' own rows.  Both always leave parts.
+struct PrefixArgs : AttendArgs {  // n_seq, lens, cu_seq, cu_split: of prefixes; rows: of the one with most
+    static constexpr int kShare = 1;
+    int32_t cu_member[JQ_MAX_SEQ + 1];  // sequences that continue a prefix
+    int32_t cu_part[JQ_MAX_SEQ + 1];    // parts of a prefix: splits times query rows, of each layer and KV head
+};
+struct OwnArgs : AttendArgs {
+    static constexpr int kShare = 2;
+    int32_t causal;
+};
+
+// The query rows that meet the keys of a (layer, sequence, KV head): how many, where the row of token i and head h lies among all
+// calls' queries, and where the rows' part of the output begins.
+__device__ __forceinline__ int query_rows(const AttendArgs& a, int) { return a.rows; }
+__device__ __forceinline__ int64_t query_at(const AttendArgs& a, int layer, int s, int i, int h) { return (((int64_t)layer * a.n_seq + s) * a.n_q + i) * a.h_q + h; }
+__device__ __forceinline__ int64_t part_at(const AttendArgs& a, int layer, int, int split, int, int g) {
+    return (((int64_t)layer * a.n_splits + split) * a.h_kv + g) * a.rows;
+}
+__device__ __forceinline__ int query_rows(const PrefixArgs& a, int s) { return (a.cu_member[s + 1] - a.cu_member[s]) * a.n_q * a.group; }
+__device__ __forceinline__ int64_t query_at(const PrefixArgs& a, int layer, int s, int i, int h) {
+    return (((int64_t)layer * a.cu_member[a.n_seq] + a.cu_member[s]) * a.n_q + i) * a.h_q + h;
+}
+__device__ __forceinline__ int64_t part_at(const PrefixArgs& a, int layer, int s, int, int mine, int g) {
+    const int rows = query_rows(a, s);
+    return ((int64_t)layer * a.cu_part[a.n_seq] + a.cu_part[s] + (int64_t)mine * rows) * a.h_kv + (int64_t)g * rows;
+}
 
 __device__ __forceinline__ int32_t live_rows(const int32_t* lens, int n_seq, int layer, int s, int cap) {
     return lens ? min(max(lens[(int64_t)layer * n_seq + s], 0), cap) : cap;
@@ -443,26 +472,36 @@ struct Weigher {
     }
 };
 
-template <class Rows, int RT, int MASK, bool KEEP>
-__global__ __launch_bounds__(kAttendThreads, RT == 1 && !Rows::kCoded ? 3 : 2) void jq_attend_kernel(AttendArgs a) {
+// A kernel's only argument, where it lies: read through a reference to the parameter itself, stores in between make the compiler (ROCm
+// 7.2) load and divide by its fields once more for every four dimensions of output.
+template <class Args>
+__device__ __forceinline__ const Args& kernel_args() { return *(const Args*)__builtin_amdgcn_kernarg_segment_ptr(); }
+
+// bx, layer: the workgroup's place in the grid.
+template <class Rows, int RT, int MASK, bool KEEP, int WAVES, class Args>
+__device__ __forceinline__ void attend_few_rows(const Args& a, int bx, int layer) {
     extern __shared__ __align__(16) float lds[];  // [waves][16 RT][kOutStride], then (m, z) [waves][16 RT]
-    float2* lds_stats = (float2*)(lds + kAttendWaves * RT * kTileRows * kOutStride);
-    // blockIdx.x: groups of query rows over the same keys eight apart, so that they meet in one XCD's L2
+    constexpr int kThreads = 64 * WAVES;
+    constexpr bool kParts = Args::kShare != 0;
+    static_assert(!(KEEP && kParts), "weights are those of one sweep");
+    float2* lds_stats = (float2*)(lds + WAVES * RT * kTileRows * kOutStride);
+    // bx: groups of query rows over the same keys eight apart, so that they meet in one XCD's L2
     const int per = 8 * a.row_groups;
-    const int u = (int)blockIdx.x / per * 8 + ((int)blockIdx.x & 7), rg = ((int)blockIdx.x % per) >> 3;
+    const int u = bx / per * 8 + (bx & 7), rg = (bx % per) >> 3;
     if (u >= a.units) return;
-    const int layer = blockIdx.y, split = u / a.h_kv, g = u - split * a.h_kv;
+    const int split = u / a.h_kv, g = u - split * a.h_kv;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
     const int s = seq_of_split(a, split, lane);
     const int ns = a.cu_split[s + 1] - a.cu_split[s], mine = split - a.cu_split[s];
     const int row0 = rg * RT * kTileRows;
+    if (Args::kShare == 1 && row0 >= query_rows(a, s)) return;  // (a prefix that fewer sequences continue)
 
     // Tiles of 32 keys, dealt to the sequence's waves in turn, so that all of them sweep one moving window of the cache.
     const Rows rows(a, layer, s, g);
     // The first tile is requested before anything else is looked at, the live count too, which only decides whether it matters: rows
     // that are not live yet are the caller's as well, and masked.
-    const int step = 32 * kAttendWaves * ns, cap = a.cu_seq[s + 1] - a.cu_seq[s];
-    int key = 32 * (kAttendWaves * mine + wave);
+    const int step = 32 * WAVES * ns, cap = a.cu_seq[s + 1] - a.cu_seq[s];
+    int key = 32 * (WAVES * mine + wave);
     constexpr int kAhead = Rows::kAhead;
     typename Rows::Tile t[kAhead];
 #pragma unroll
@@ -473,9 +512,9 @@ __global__ __launch_bounds__(kAttendThreads, RT == 1 && !Rows::kCoded ? 3 : 2) v
     const uint32_t* row_seen[RT];
 #pragma unroll
     for (int r = 0; r < RT; ++r) {
-        const int row = min(row0 + r * kTileRows + (lane & 15), a.rows - 1);  // rows past the last repeat it and are not stored
+        const int row = min(row0 + r * kTileRows + (lane & 15), query_rows(a, s) - 1);  // rows past the last repeat it and are not stored
         const int i = row / a.group, h = g * a.group + row - i * a.group;
-        const char* q = a.Q + ((((int64_t)layer * a.n_seq + s) * a.n_q + i) * a.h_q + h) * (kHeadDim * 2);
+        const char* q = a.Q + query_at(a, layer, s, i, h) * (kHeadDim * 2);
 #pragma unroll
         for (int c = 0; c < 4; ++c) st.q[r][c] = __builtin_bit_cast(bf16x8, *(const au32x4*)(q + Rows::q_at(c, lane)));
 #pragma unroll
@@ -483,23 +522,25 @@ __global__ __launch_bounds__(kAttendThreads, RT == 1 && !Rows::kCoded ? 3 : 2) v
         st.m[r] = -__builtin_inff();
         st.z[r] = 0.0f;
         row_limit[r] = i + 1;  // (and the rows in front of the queries' own, below)
+        if constexpr (Args::kShare == 2) row_limit[r] = a.causal ? i + 1 : a.n_q;
         row_seen[r] = MASK == kSeeTree ? a.seen + ((int64_t)s * a.n_q + i) * a.words : nullptr;
     }
 
     const int n = live_rows(a.lens, a.n_seq, layer, s, cap);
     // keys from `open` on are not seen by every row
-    const int open = MASK == kSeeAll ? n : max(n - a.n_q + (MASK == kSeeCausal ? 1 : 0), 0);
+    int open = MASK == kSeeAll ? n : max(n - a.n_q + (MASK == kSeeCausal ? 1 : 0), 0);
+    if constexpr (Args::kShare == 2) open = a.causal ? open : n;
 #pragma unroll
     for (int r = 0; r < RT; ++r) row_limit[r] += n - a.n_q;
     // The sequence's count of finished workgroups starts at zero for this call: it holds the call's tag or is given it here.
     uint64_t* arrived = a.arrived + (((int64_t)layer * a.n_seq + s) * a.h_kv + g) * a.row_groups + rg;
-    if (RT == 1 && a.tag && ns > 1 && threadIdx.x == 0) {
+    if (RT == 1 && !kParts && a.tag && ns > 1 && threadIdx.x == 0) {
         uint64_t was = __hip_atomic_load(arrived, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
         if ((was ^ a.tag) >> 24) __hip_atomic_compare_exchange_strong(arrived, &was, a.tag, __ATOMIC_RELAXED, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     }
     // With weights every row's logits stay in LDS until its sums are known, [rows][hold_keys], a wave's tiles four apart.  (Written
     // out as they are formed they kept reads from being under way: 32 sequences of 2048 rows 71.7 us a call, without weights 58.3.)
-    float* held = (float*)(lds_stats + kAttendWaves * RT * kTileRows);
+    float* held = (float*)(lds_stats + WAVES * RT * kTileRows);
     float* hold = KEEP ? held + (lane & 15) * a.hold_keys + 32 * wave + 4 * (lane >> 4) : nullptr;
     bool was_cleared = false;
     // One tile, and the request of the one that takes its place.
@@ -514,7 +555,7 @@ __global__ __launch_bounds__(kAttendThreads, RT == 1 && !Rows::kCoded ? 3 : 2) v
             tile_step<RT, masked.value, MASK, KEEP>(st, tile, a, lane, key, n, row_limit, row_seen, hold, &was_cleared);
             if (next < n) rows.load(tile, rows.row(next), n - 1 - next, lane);
         }
-        if (KEEP) hold += 32 * kAttendWaves;
+        if (KEEP) hold += 32 * WAVES;
         key += step;
     };
     while (key + (kAhead - 1) * step + 32 <= open) {
@@ -539,7 +580,7 @@ __global__ __launch_bounds__(kAttendThreads, RT == 1 && !Rows::kCoded ? 3 : 2) v
     }
     if (__any(marked)) {
         f32x4 marks[RT][8];
-        auto tile = [&](int i) { const int k = 32 * (kAttendWaves * mine + wave) + i * step; return k < n ? k : -1; };
+        auto tile = [&](int i) { const int k = 32 * (WAVES * mine + wave) + i * step; return k < n ? k : -1; };
         auto sees = [&](int r, int k) { return row_sees<MASK>(a, k, n, row_limit[r], row_seen[r]); };
         mark_kinds<RT>(marks, rows, n, lane, tile, sees, [&](int d) { return 8 * (lane & 15) + d; });
 #pragma unroll
@@ -560,7 +601,7 @@ __global__ __launch_bounds__(kAttendThreads, RT == 1 && !Rows::kCoded ? 3 : 2) v
     for (int r = 0; r < RT; ++r) {
         float m = -__builtin_inff();
 #pragma unroll
-        for (int w = 0; w < kAttendWaves; ++w) m = fmaxf(m, lds_stats[(w * RT + r) * kTileRows + (lane & 15)].x);
+        for (int w = 0; w < WAVES; ++w) m = fmaxf(m, lds_stats[(w * RT + r) * kTileRows + (lane & 15)].x);
         const float f = rescale(st.m[r], m);
         float* to = lds + ((wave * RT + r) * kTileRows + (lane & 15)) * kOutStride + 32 * (lane >> 4);
 #pragma unroll
@@ -574,28 +615,28 @@ __global__ __launch_bounds__(kAttendThreads, RT == 1 && !Rows::kCoded ? 3 : 2) v
             }
     }
     __syncthreads();
-    const int64_t part_row = (((int64_t)layer * a.n_splits + split) * a.h_kv + g) * a.rows;
-    const int rows_here = min(a.rows - row0, RT * kTileRows);
-    for (int item = threadIdx.x; item < rows_here * 32; item += kAttendThreads) {
+    const int64_t part_row = part_at(a, layer, s, split, mine, g);
+    const int rows_here = min(query_rows(a, s) - row0, RT * kTileRows);
+    for (int item = threadIdx.x; item < rows_here * 32; item += kThreads) {
         const int r = item >> 5, d = (item & 31) * 4, row = row0 + r;
         float m = -__builtin_inff(), z = 0.0f;
 #pragma unroll
-        for (int w = 0; w < kAttendWaves; ++w) m = fmaxf(m, lds_stats[w * RT * kTileRows + r].x);
+        for (int w = 0; w < WAVES; ++w) m = fmaxf(m, lds_stats[w * RT * kTileRows + r].x);
         f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-        for (int w = 0; w < kAttendWaves; ++w) {
+        for (int w = 0; w < WAVES; ++w) {
             const float2 mz = lds_stats[w * RT * kTileRows + r];
             z += mz.x == m ? mz.y : mz.y * __builtin_amdgcn_exp2f(mz.x - m);
             o += *(const f32x4*)(lds + (w * RT * kTileRows + r) * kOutStride + d);
         }
-        if (ns == 1) {
+        if (ns == 1 && !kParts) {
             store_out(a, layer, s, g, row, d, o, m, z);
         } else {
             float* to = a.part + (part_row + row) * kHeadDim + d;
             put_pair(to, o[0], o[1]);
             put_pair(to + 2, o[2], o[3]);
         }
-        if (d == 0 && (ns > 1 || KEEP)) put_pair((float*)(a.stats + part_row + row), m, z);
+        if (d == 0 && (ns > 1 || KEEP || kParts)) put_pair((float*)(a.stats + part_row + row), m, z);
     }
     if (KEEP && ns == 1) {  // all of the sequence is here
         float* lse2 = lds;  // (the sums above have been read by the threads that wait here)
@@ -603,9 +644,9 @@ __global__ __launch_bounds__(kAttendThreads, RT == 1 && !Rows::kCoded ? 3 : 2) v
         if ((int)threadIdx.x < a.rows) {
             float m = -__builtin_inff(), z = 0.0f;
 #pragma unroll
-            for (int w = 0; w < kAttendWaves; ++w) m = fmaxf(m, lds_stats[w * RT * kTileRows + threadIdx.x].x);
+            for (int w = 0; w < WAVES; ++w) m = fmaxf(m, lds_stats[w * RT * kTileRows + threadIdx.x].x);
 #pragma unroll
-            for (int w = 0; w < kAttendWaves; ++w) {
+            for (int w = 0; w < WAVES; ++w) {
                 const float2 mz = lds_stats[w * RT * kTileRows + threadIdx.x];
                 z += mz.x == m ? mz.y : mz.y * __builtin_amdgcn_exp2f(mz.x - m);
             }
@@ -613,7 +654,7 @@ __global__ __launch_bounds__(kAttendThreads, RT == 1 && !Rows::kCoded ? 3 : 2) v
         }
         __syncthreads();
         float* w = a.weights + ((int64_t)layer * a.h_kv + g) * a.T + a.cu_seq[s];
-        for (int j = threadIdx.x; j < n; j += kAttendThreads) {  // (one workgroup: row j of the cache is held at j)
+        for (int j = threadIdx.x; j < n; j += kThreads) {  // (one workgroup: row j of the cache is held at j)
             float sum = 0.0f;
             for (int r = 0; r < a.rows; ++r) sum += __builtin_amdgcn_exp2f(held[r * a.hold_keys + j] - lse2[r]);
             w[j] += sum;
@@ -623,13 +664,13 @@ __global__ __launch_bounds__(kAttendThreads, RT == 1 && !Rows::kCoded ? 3 : 2) v
     if (KEEP) {  // the whole share's logits at once, to where the workgroup that weighs finds them
         const int64_t to = ((int64_t)layer * a.h_kv + g) * a.rows * a.logit_T + logit_at(a.cu_seq, s);
         const int pairs = a.hold_keys / 2;
-        for (int item = threadIdx.x; item < a.rows * pairs; item += kAttendThreads) {
+        for (int item = threadIdx.x; item < a.rows * pairs; item += kThreads) {
             const int r = item / pairs, j = (item - r * pairs) * 2, tile = j >> 5;
-            const int at = ((tile >> 2) * ns + mine) * 32 * kAttendWaves + 32 * (tile & 3) + (j & 31);
+            const int at = ((tile >> 2) * ns + mine) * 32 * WAVES + 32 * (tile & 3) + (j & 31);
             if (at < ((n + 31) & ~31)) put_pair(a.logits + to + r * a.logit_T + at, held[r * a.hold_keys + j], held[r * a.hold_keys + j + 1]);
         }
     }
-    if (RT > 1 || !a.tag || ns == 1) return;
+    if (RT > 1 || kParts || !a.tag || ns == 1) return;
 
     // Whoever completes a sequence joins it; nobody waits.  Data first, then the count of those that have left theirs.
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
@@ -642,10 +683,10 @@ __global__ __launch_bounds__(kAttendThreads, RT == 1 && !Rows::kCoded ? 3 : 2) v
     // What the join begins with is requested together, statistics, sums and logits: each of them is a round trip past the caches.
     // Sixteen bytes of output a thread; where there are few rows several threads take shares of the shares.
     const int64_t first = (((int64_t)layer * a.n_splits + a.cu_split[s]) * a.h_kv + g) * a.rows + row0, next_share = (int64_t)a.h_kv * a.rows;
-    static_assert(kMostJoinRows * 32 <= kAttendThreads, "a thread or more for every four sums");
+    static_assert(kMostJoinRows * 32 <= kThreads, "a thread or more for every four sums");
     const int items = rows_here * 32, part = (int)threadIdx.x / items, item = (int)threadIdx.x - part * items;
     int parts = 1;
-    while (2 * parts * items <= kAttendThreads && parts < 8) parts *= 2;
+    while (2 * parts * items <= kThreads && parts < 8) parts *= 2;
     constexpr int kBatch = 8;
     float2 lo[kBatch], hi[kBatch];
     auto request = [&](int i) {  // shares i, i + parts, ... of the thread's sums
@@ -665,7 +706,7 @@ __global__ __launch_bounds__(kAttendThreads, RT == 1 && !Rows::kCoded ? 3 : 2) v
     float* sums = factor + (rows_here * ns + 3) / 4 * 4;  // [parts][items] outputs of four, at multiples of sixteen bytes
     float* lse2 = (float*)(lds_stats + rows_here);
     __syncthreads();
-    for (int r = wave; r < rows_here; r += kAttendWaves) {  // a wave a row, a lane a share (there are 20 at most)
+    for (int r = wave; r < rows_here; r += WAVES) {  // a wave a row, a lane a share (there are 20 at most)
         const float2 mz = lane < ns ? get_pair((const float*)(a.stats + first + r + lane * next_share)) : make_float2(-__builtin_inff(), 0.0f);
         float m = mz.x;
 #pragma unroll
@@ -704,6 +745,11 @@ __global__ __launch_bounds__(kAttendThreads, RT == 1 && !Rows::kCoded ? 3 : 2) v
     if (KEEP) weigher.add(lse2, true);
 }
 
+template <class Rows, int RT, int MASK, bool KEEP>
+__global__ __launch_bounds__(kAttendThreads, RT == 1 && !Rows::kCoded ? 3 : 2) void jq_attend_kernel(AttendArgs a) {
+    attend_few_rows<Rows, RT, MASK, KEEP, kAttendWaves>(kernel_args<AttendArgs>(), (int)blockIdx.x, (int)blockIdx.y);
+}
+
 // Many query rows (more than 32 a KV head).  A wave still holds 32 of them, but the eight waves of a workgroup share the keys: R waves
 // over all rows of a group times KW over keys of their own.  K and V go through LDS, where every wave reads all of its keys' rows:
 // requested into registers stages ahead, written to one of two buffers, one barrier a stage.  (Every wave reading K and V for itself
@@ -736,23 +782,25 @@ struct Wide {
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) s16x4* lds_s16x4;
 
-template <class Rows, int R, int MASK, bool KEEP>
-__global__ __launch_bounds__(Wide<R>::kThreads, 2) void jq_attend_wide_kernel(AttendArgs a) {
+template <class Rows, int R, int MASK, bool KEEP, class Args>
+__device__ __forceinline__ void attend_many_rows(const Args& a, int bx, int layer) {
+    extern __shared__ __align__(16) char wide_lds[];
     using W = Wide<R>;
     constexpr int KW = W::KW;
-    extern __shared__ __align__(16) char wide_lds[];
+    constexpr bool kParts = Args::kShare != 0;
     uint8_t* marked = (uint8_t*)wide_lds + W::kFlags;  // [kWaves]: the wave has cleared values of V, or has sums that are not finite
     bool was_cleared = false;
     const int per = 8 * a.row_groups;
-    const int u = (int)blockIdx.x / per * 8 + ((int)blockIdx.x & 7), rg = ((int)blockIdx.x % per) >> 3;
+    const int u = bx / per * 8 + (bx & 7), rg = (bx % per) >> 3;
     if (u >= a.units) return;
-    const int layer = blockIdx.y, split = u / a.h_kv, g = u - split * a.h_kv;
+    const int split = u / a.h_kv, g = u - split * a.h_kv;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
     const int s = seq_of_split(a, split, lane);
     const int ns = a.cu_split[s + 1] - a.cu_split[s], mine = split - a.cu_split[s];
     const int cap = a.cu_seq[s + 1] - a.cu_seq[s];
     const int rw = wave % R, kw = wave / R;
     const int row0 = rg * W::kRows + 32 * rw;
+    if (Args::kShare == 1 && rg * W::kRows >= query_rows(a, s)) return;  // (a prefix that fewer sequences continue)
 
     const Rows rows(a, layer, s, g);
 
@@ -790,9 +838,9 @@ __global__ __launch_bounds__(Wide<R>::kThreads, 2) void jq_attend_wide_kernel(At
     int token[2];   // the query rows' tokens
 #pragma unroll
     for (int r = 0; r < 2; ++r) {
-        const int row = min(row0 + r * kTileRows + (lane & 15), a.rows - 1);
+        const int row = min(row0 + r * kTileRows + (lane & 15), query_rows(a, s) - 1);
         const int i = row / a.group, h = g * a.group + row - i * a.group;
-        const char* from = a.Q + ((((int64_t)layer * a.n_seq + s) * a.n_q + i) * a.h_q + h) * (kHeadDim * 2);
+        const char* from = a.Q + query_at(a, layer, s, i, h) * (kHeadDim * 2);
 #pragma unroll
         for (int c = 0; c < 4; ++c) q[r][c] = __builtin_bit_cast(bf16x8, *(const au32x4*)(from + 64 * c + 16 * (lane >> 4)));
 #pragma unroll
@@ -981,7 +1029,7 @@ __global__ __launch_bounds__(Wide<R>::kThreads, 2) void jq_attend_wide_kernel(At
 #pragma unroll
                 for (int e = 0; e < 4; ++e) o[r][d][e] = marks[r][d][e] == 0.0f ? o[r][d][e] : marks[r][d][e];
     }
-    const int64_t part_row = (((int64_t)layer * a.n_splits + split) * a.h_kv + g) * a.rows;
+    const int64_t part_row = part_at(a, layer, s, split, mine, g);
     if (KW > 1) {  // the waves over other keys of the same rows
         float* sums = (float*)wide_lds;                                         // [kWaves - R][32][kOutStride]
         float2* stats = (float2*)(sums + (W::kWaves - R) * 32 * kOutStride);    // [kWaves - R][32]
@@ -1020,15 +1068,20 @@ __global__ __launch_bounds__(Wide<R>::kThreads, 2) void jq_attend_wide_kernel(At
 #pragma unroll
     for (int r = 0; r < 2; ++r) {
         const int row = row0 + r * kTileRows + (lane & 15);
-        if (row >= a.rows) continue;
-        if (lane < 16 && (ns > 1 || KEEP)) a.stats[part_row + row] = make_float2(m[r], z[r]);
+        if (row >= query_rows(a, s)) continue;
+        if (lane < 16 && (ns > 1 || KEEP || kParts)) a.stats[part_row + row] = make_float2(m[r], z[r]);
 #pragma unroll
         for (int d = 0; d < 8; ++d) {
             const int at = 16 * d + 4 * (lane >> 4);
-            if (ns == 1) store_out(a, layer, s, g, row, at, o[r][d], m[r], z[r]);
+            if (ns == 1 && !kParts) store_out(a, layer, s, g, row, at, o[r][d], m[r], z[r]);
             else *(f32x4*)(a.part + (part_row + row) * kHeadDim + at) = o[r][d];
         }
     }
+}
+
+template <class Rows, int R, int MASK, bool KEEP>
+__global__ __launch_bounds__(Wide<R>::kThreads, 2) void jq_attend_wide_kernel(AttendArgs a) {
+    attend_many_rows<Rows, R, MASK, KEEP>(kernel_args<AttendArgs>(), (int)blockIdx.x, (int)blockIdx.y);
 }
 
 // ---- launches ----------------------------------------------------------------------------------------------------------------

@@ -370,6 +370,20 @@ struct Codes {
 };
 hipError_t launch_attend(const Plan& p, const AttendPlan& ap, const int32_t* lens, const uint32_t* seen, const void* Q, const void* K, const void* V,
                          void* out, float* lse, float* weights, char* ws, hipStream_t st, const Codes* codes = nullptr);
+// Sequences that continue shared prefixes (jq_shared.hip); `pp`: the plan of the prefixes.
+struct SharedPlan {
+    int32_t prefix_tiles, prefix_groups, own_tiles, own_groups;  // tiles of 16 query rows a workgroup takes, workgroups over the same keys
+    int32_t cu_split[JQ_MAX_SEQ + 1], own_split[JQ_MAX_SEQ + 1];  // workgroups that share a prefix, a sequence, summed up
+    int32_t cu_part[JQ_MAX_SEQ + 1];                              // splits times query rows of the prefixes, summed up
+    bool fits;                                                    // every launch stays below 2^32 threads
+    size_t off_prefix_stats, off_prefix_part, off_own_stats, off_own_part, ws_bytes;
+};
+// Workgroups of a sweep; eight heads or shares side by side lie on eight XCDs, groups of query rows over the same keys on one.
+inline int64_t shared_blocks(int64_t splits, int h_kv, int groups) { return (splits * h_kv + 7) / 8 * 8 * groups; }
+void plan_shared(const Plan& p, const Plan& pp, const int32_t* cu_members, SharedPlan* sp);
+hipError_t launch_attend_shared(const Plan& p, const Plan& pp, const SharedPlan& sp, const int32_t* cu_members, const int32_t* lens, const int32_t* prefix_lens,
+                                const void* Q, const void* K_prefix, const void* V_prefix, const void* K, const void* V, void* out, float* lse, char* ws,
+                                hipStream_t st);
 // Rows written into a cache of codes at rows first[layer][sequence] (null: 0) and up, and read back (jq_codes.hip).
 bool codes_fit(const Plan& p);
 hipError_t launch_quantize(const Plan& p, const Codes& c, const int32_t* first, const void* K, const void* V, hipStream_t st);
