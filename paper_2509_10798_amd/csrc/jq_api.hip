@@ -712,11 +712,11 @@ bool any_overlap(const Buf* outs, int n_out, const Buf* ins, int n_in) {
 }
 size_t lens_bytes(const Plan& p) { return (size_t)p.n_layers * p.n_seq * 4; }
 
-int attend_plan(const jq_shape* shape, bool weights, Plan* p, AttendPlan* ap) {
+int attend_plan(const jq_shape* shape, bool weights, Plan* p, AttendPlan* ap, bool coded = false) {
     const int rc = make_plan(shape, false, p, false);
     if (rc != JQ_OK) return rc;
     if (weights && p->rows > kMaxWeighRows) return JQ_ERR_UNSUPPORTED;
-    plan_attend(*p, weights, ap);
+    plan_attend(*p, weights, coded, ap);
     return attend_fits(*p, *ap, weights) ? JQ_OK : JQ_ERR_UNSUPPORTED;
 }
 }  // namespace
@@ -750,7 +750,7 @@ static int attend_impl(const jq_shape* shape, const jq_pages* pages, bool paged,
                        const jq_codes* codes = nullptr) {
     Plan p;
     AttendPlan ap;
-    int rc = attend_plan(shape, weights != nullptr, &p, &ap);
+    int rc = attend_plan(shape, weights != nullptr, &p, &ap, coded);
     if (rc != JQ_OK) return rc;
     if (paged && (rc = apply_pages(pages, &p)) != JQ_OK) return rc;
     if (tree) {

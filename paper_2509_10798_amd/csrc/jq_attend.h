@@ -29,6 +29,8 @@ namespace jq {
 
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t au32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kAttendWaves = 4;
@@ -224,12 +226,22 @@ __device__ __forceinline__ void mark_kinds(f32x4 (&marks)[RT][8], const Rows& ro
 // 16 t + 4 (l / 16) + e.
 struct KvTile {
     au32x4 k[2][4], v[2][4];
+    __device__ __forceinline__ au32x4 key_piece(int i, int c) const { return k[i][c]; }
+    // The lane's dimensions 2 w and 2 w + 1 of its eight keys of V.
+    template <int W>
+    __device__ __forceinline__ void value_words(uint32_t (&x)[2][4]) const {
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) x[i][e] = v[i][e][W];
+    }
 };
 
 // One head's rows of one sequence in a bf16 cache [.., rows, KV heads, 128], dense or in pages.
 struct Rows16 {
     static constexpr bool kCoded = false;
-    static constexpr int kAhead = 1;  // tiles requested ahead
+    static constexpr int waves(int, bool) { return kAttendWaves; }  // of a workgroup, by its tiles of 16 query rows and whether there are weights
+    static constexpr int least_waves(int row_tiles) { return row_tiles == 1 ? 3 : 2; }  // of a SIMD that registers have to leave room for
     using Tile = KvTile;
     using Piece = au32x4;             // eight dimensions of a row
     const char* K; const char* V;
@@ -305,10 +317,10 @@ __device__ __forceinline__ bool row_sees(const AttendArgs& a, int key, int n, in
 }
 
 // One tile of 32 keys.  MASKED: some row may not see some key of it, or the tile reaches past the live rows.
-template <int RT, bool MASKED, int MASK, bool KEEP>
-__device__ __forceinline__ void tile_step(RowState<RT>& st, KvTile& t, const AttendArgs& a, int lane, int key0, int n, const int* row_limit,
+template <int RT, bool MASKED, int MASK, bool KEEP, class Tile>
+__device__ __forceinline__ void tile_step(RowState<RT>& st, Tile& t, const AttendArgs& a, int lane, int key0, int n, const int* row_limit,
                                           const uint32_t* const* row_seen, float* hold, bool* was_cleared) {
-    if (MASKED) {
+    if constexpr (MASKED) {
         Exponents exponents;
 #pragma unroll
         for (int i = 0; i < 2; ++i)
@@ -333,7 +345,7 @@ __device__ __forceinline__ void tile_step(RowState<RT>& st, KvTile& t, const Att
         for (int i = 0; i < 2; ++i) {
             f32x4 x = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-            for (int c = 0; c < 4; ++c) x = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, t.k[i][c]), st.q[r][c], x, 0, 0, 0);
+            for (int c = 0; c < 4; ++c) x = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, t.key_piece(i, c)), st.q[r][c], x, 0, 0, 0);
             s[r][i] = x * a.scale2;
         }
     if (MASKED) {
@@ -380,28 +392,47 @@ __device__ __forceinline__ void tile_step(RowState<RT>& st, KvTile& t, const Att
 #pragma unroll
         for (int i = 0; i < 2; ++i)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const float p = __builtin_amdgcn_exp2f(s[r][i][e] - m);
-                st.z[r] += p;
-                hi[r][4 * i + e] = (__bf16)p;
-                lo[r][4 * i + e] = (__bf16)(p - (float)hi[r][4 * i + e]);
+            for (int e = 0; e < 4; e += 2) {
+                f32x2 p;
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                    p[k] = __builtin_amdgcn_exp2f(s[r][i][e + k] - m);
+                    st.z[r] += p[k];
+                }
+                const bf16x2 h = __builtin_convertvector(p, bf16x2);  // (two at a time: one instruction)
+                const f32x2 rest = {p[0] - (float)h[0], p[1] - (float)h[1]};
+                const bf16x2 l = __builtin_convertvector(rest, bf16x2);
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                    hi[r][4 * i + e + k] = h[k];
+                    lo[r][4 * i + e + k] = l[k];
+                }
             }
     }
+    auto add_values = [&](auto word) {
+        uint32_t x[2][4];
+        t.template value_words<word.value>(x);
 #pragma unroll
-    for (int d = 0; d < 8; ++d) {
-        au32x4 v;
-        const uint32_t sel = d & 1 ? 0x07060302u : 0x05040100u;  // the upper or the lower halves of two registers
+        for (int odd = 0; odd < 2; ++odd) {
+            const int d = 2 * word.value + odd;
+            au32x4 v;
+            const uint32_t sel = odd ? 0x07060302u : 0x05040100u;  // the upper or the lower halves of two registers
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
+            for (int i = 0; i < 2; ++i)
 #pragma unroll
-            for (int e = 0; e < 2; ++e) v[2 * i + e] = __builtin_amdgcn_perm(t.v[i][2 * e + 1][d >> 1], t.v[i][2 * e][d >> 1], sel);
-        const bf16x8 vt = __builtin_bit_cast(bf16x8, v);
+                for (int e = 0; e < 2; ++e) v[2 * i + e] = __builtin_amdgcn_perm(x[i][2 * e + 1], x[i][2 * e], sel);
+            const bf16x8 vt = __builtin_bit_cast(bf16x8, v);
 #pragma unroll
-        for (int r = 0; r < RT; ++r) {
-            st.o[r][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vt, hi[r], st.o[r][d], 0, 0, 0);
-            st.o[r][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vt, lo[r], st.o[r][d], 0, 0, 0);
+            for (int r = 0; r < RT; ++r) {
+                st.o[r][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vt, hi[r], st.o[r][d], 0, 0, 0);
+                st.o[r][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vt, lo[r], st.o[r][d], 0, 0, 0);
+            }
         }
-    }
+    };
+    add_values(std::integral_constant<int, 0>{});
+    add_values(std::integral_constant<int, 1>{});
+    add_values(std::integral_constant<int, 2>{});
+    add_values(std::integral_constant<int, 3>{});
 }
 
 // Four dimensions of a query row's output out of its sums; a row that has seen nothing: zeros, and -inf for its log-sum-exp.
@@ -419,6 +450,7 @@ __device__ __forceinline__ void store_out(const AttendArgs& a, int layer, int s,
 // weights[j] += sum_r 2^(x[r,j] - lse2[r]) for the rows j from `begin` to `end` of the cache, all threads of the workgroup together;
 // the logits may have been left by other workgroups of the launch.  A thread takes four pairs of rows at a time, so that sixteen
 // loads are under way; the first of them may have been requested earlier (request()).
+template <int THREADS>
 struct Weigher {
     static constexpr int kPairs = 4;
     const float* x;
@@ -431,7 +463,7 @@ struct Weigher {
         : x(a.logits + ((int64_t)layer * a.h_kv + g) * a.rows * a.logit_T + logit_at(a.cu_seq, s)),
           w(a.weights + ((int64_t)layer * a.h_kv + g) * a.T + a.cu_seq[s]), logit_T(a.logit_T), rows(a.rows), end(end_),
           j0(begin + 2 * (int)threadIdx.x) {}
-    __device__ __forceinline__ int row(int k) const { return j0 + 2 * k * kAttendThreads; }
+    __device__ __forceinline__ int row(int k) const { return j0 + 2 * k * THREADS; }
     __device__ __forceinline__ void request(int r0) {
         if (j0 >= end) return;
 #pragma unroll
@@ -443,7 +475,7 @@ struct Weigher {
         }
     }
     __device__ __forceinline__ void add(const float* lse2, bool requested) {
-        for (; j0 < end; j0 += 2 * kPairs * kAttendThreads) {
+        for (; j0 < end; j0 += 2 * kPairs * THREADS) {
             float2 sum[kPairs];
             for (int r0 = 0; r0 < rows; r0 += 4) {
                 if (!requested) request(r0);
@@ -502,11 +534,8 @@ __device__ __forceinline__ void attend_few_rows(const Args& a, int bx, int layer
     // that are not live yet are the caller's as well, and masked.
     const int step = 32 * WAVES * ns, cap = a.cu_seq[s + 1] - a.cu_seq[s];
     int key = 32 * (WAVES * mine + wave);
-    constexpr int kAhead = Rows::kAhead;
-    typename Rows::Tile t[kAhead];
-#pragma unroll
-    for (int i = 0; i < kAhead; ++i)
-        if (key + i * step < cap) rows.load(t[i], rows.row(key + i * step), cap - 1 - key - i * step, lane);
+    typename Rows::Tile t;
+    if (key < cap) rows.load(t, rows.row(key), cap - 1 - key, lane);
     RowState<RT> st;
     int row_limit[RT];
     const uint32_t* row_seen[RT];
@@ -544,31 +573,35 @@ __device__ __forceinline__ void attend_few_rows(const Args& a, int bx, int layer
     float* hold = KEEP ? held + (lane & 15) * a.hold_keys + 32 * wave + 4 * (lane >> 4) : nullptr;
     bool was_cleared = false;
     // One tile, and the request of the one that takes its place.
-    auto turn = [&](auto masked, typename Rows::Tile& tile) {
-        const int next = key + kAhead * step;
-        if constexpr (Rows::kCoded) {
-            KvTile values;
-            Rows::unpack(values, tile, lane);
-            if (next < n) rows.load(tile, rows.row(next), n - 1 - next, lane);
-            tile_step<RT, masked.value, MASK, KEEP>(st, values, a, lane, key, n, row_limit, row_seen, hold, &was_cleared);
-        } else {
-            tile_step<RT, masked.value, MASK, KEEP>(st, tile, a, lane, key, n, row_limit, row_seen, hold, &was_cleared);
-            if (next < n) rows.load(tile, rows.row(next), n - 1 - next, lane);
-        }
+    auto step_of = [&](auto masked, auto& tile) {
+        tile_step<RT, masked.value, MASK, KEEP>(st, tile, a, lane, key, n, row_limit, row_seen, hold, &was_cleared);
         if (KEEP) hold += 32 * WAVES;
         key += step;
     };
-    while (key + (kAhead - 1) * step + 32 <= open) {
-#pragma unroll
-        for (int i = 0; i < kAhead; ++i) turn(std::false_type{}, t[i]);
-    }
-    while (key < n) {
-        turn(std::true_type{}, t[0]);
-        if constexpr (kAhead > 1) {  // (the tile just requested becomes the last one; a few tiles at most)
-            const typename Rows::Tile last = t[0];
-#pragma unroll
-            for (int i = 0; i + 1 < kAhead; ++i) t[i] = t[i + 1];
-            t[kAhead - 1] = last;
+    if constexpr (Rows::kCoded) {
+        // Whole tiles are requested from uniform addresses; where the wave's last one is not whole, the last that is stands in for it
+        // until it is known which it is: a branch between two ways of requesting a tile cost a move for each of its registers.
+        const int last_whole = (cap & ~31) - 32;
+        const bool turns = key + 32 <= open;
+        while (key + 32 <= open) {
+            step_of(std::false_type{}, t);
+            if (key < n) rows.load_whole(t, rows.row(min(key, last_whole)), lane);
+        }
+        if (turns && key < n && key > last_whole) rows.load(t, rows.row(key), n - 1 - key, lane);
+        while (key < n) {
+            KvTile values;
+            Rows::unpack(values, t, lane);
+            step_of(std::true_type{}, values);
+            if (key < n) rows.load(t, rows.row(key), n - 1 - key, lane);
+        }
+    } else {
+        while (key + 32 <= open) {
+            step_of(std::false_type{}, t);
+            if (key < n) rows.load(t, rows.row(key), n - 1 - key, lane);
+        }
+        while (key < n) {
+            step_of(std::true_type{}, t);
+            if (key < n) rows.load(t, rows.row(key), n - 1 - key, lane);
         }
     }
 
@@ -666,7 +699,7 @@ __device__ __forceinline__ void attend_few_rows(const Args& a, int bx, int layer
         const int pairs = a.hold_keys / 2;
         for (int item = threadIdx.x; item < a.rows * pairs; item += kThreads) {
             const int r = item / pairs, j = (item - r * pairs) * 2, tile = j >> 5;
-            const int at = ((tile >> 2) * ns + mine) * 32 * WAVES + 32 * (tile & 3) + (j & 31);
+            const int at = (tile / WAVES * ns + mine) * 32 * WAVES + 32 * (tile % WAVES) + (j & 31);
             if (at < ((n + 31) & ~31)) put_pair(a.logits + to + r * a.logit_T + at, held[r * a.hold_keys + j], held[r * a.hold_keys + j + 1]);
         }
     }
@@ -699,7 +732,7 @@ __device__ __forceinline__ void attend_few_rows(const Args& a, int bx, int layer
         }
     };
     request(part);
-    Weigher weigher(a, layer, s, g, 0, n);
+    Weigher<kThreads> weigher(a, layer, s, g, 0, n);
     if (KEEP) weigher.request(0);
     // Factors of all shares' sums, [rows_here][ns], and the rows' (m, z).
     float* factor = lds;
@@ -746,8 +779,8 @@ __device__ __forceinline__ void attend_few_rows(const Args& a, int bx, int layer
 }
 
 template <class Rows, int RT, int MASK, bool KEEP>
-__global__ __launch_bounds__(kAttendThreads, RT == 1 && !Rows::kCoded ? 3 : 2) void jq_attend_kernel(AttendArgs a) {
-    attend_few_rows<Rows, RT, MASK, KEEP, kAttendWaves>(kernel_args<AttendArgs>(), (int)blockIdx.x, (int)blockIdx.y);
+__global__ __launch_bounds__(64 * Rows::waves(RT, KEEP), Rows::least_waves(RT)) void jq_attend_kernel(AttendArgs a) {
+    attend_few_rows<Rows, RT, MASK, KEEP, Rows::waves(RT, KEEP)>(kernel_args<AttendArgs>(), (int)blockIdx.x, (int)blockIdx.y);
 }
 
 // Many query rows (more than 32 a KV head).  A wave still holds 32 of them, but the eight waves of a workgroup share the keys: R waves
@@ -1088,14 +1121,15 @@ __global__ __launch_bounds__(Wide<R>::kThreads, 2) void jq_attend_wide_kernel(At
 
 template <class Rows, int RT, int MASK, bool KEEP>
 static hipError_t launch_sweep(const AttendArgs& a, dim3 grid, hipStream_t st) {
-    constexpr int most = kAttendWaves * RT * kTileRows * (kOutStride * 4 + 8) + (KEEP ? kMostHeld : 0);
-    const int lds = kAttendWaves * RT * kTileRows * (kOutStride * 4 + 8) + (KEEP ? a.rows * a.hold_keys * 4 : 0);
+    constexpr int waves = Rows::waves(RT, KEEP), sums = waves * RT * kTileRows * (kOutStride * 4 + 8);
+    constexpr int most = sums + (KEEP ? kMostHeld + (waves - kAttendWaves) * 32 * kTileRows * RT * 4 : 0);  // (whole turns of all waves are held)
+    const int lds = sums + (KEEP ? a.rows * a.hold_keys * 4 : 0);
     if (most > 65536) {
         static std::atomic<uint64_t> done{0};
         const hipError_t e = allow_dynamic_lds((const void*)jq_attend_kernel<Rows, RT, MASK, KEEP>, most, done);
         if (e != hipSuccess) return e;
     }
-    return launch_kernel(jq_attend_kernel<Rows, RT, MASK, KEEP>, grid, dim3(kAttendThreads), lds, st, nullptr, -1, a);
+    return launch_kernel(jq_attend_kernel<Rows, RT, MASK, KEEP>, grid, dim3(64 * waves), lds, st, nullptr, -1, a);
 }
 
 template <class Rows, int R, int MASK, bool KEEP>

@@ -92,7 +92,7 @@ __global__ __launch_bounds__(kAttendThreads) void jq_attend_finish_kernel(Attend
         if (lane == 0) lse2[r] = mz.y == 0.0f ? 0.0f : mz.x + log2_of(mz.y);  // nothing seen: all its logits are -inf
     }
     __syncthreads();
-    Weigher(a, layer, s, g, b * kWeighKeys, min((b + 1) * kWeighKeys, n)).add(lse2, false);
+    Weigher<kAttendThreads>(a, layer, s, g, b * kWeighKeys, min((b + 1) * kWeighKeys, n)).add(lse2, false);
 }
 
 // ---- host ------------------------------------------------------------------------------------------------------------------
@@ -122,12 +122,13 @@ constexpr int kStart = 320, kWideStart = 1500;
 constexpr int kMostJoined = 20;          // shares (a lane each in the join)
 constexpr int kMostSums = 64;            // shares times query rows
 constexpr int64_t kMostWeighed = 8192;   // logits of a (sequence, head)
-static void plan_splits(const Plan& p, bool weights, AttendPlan* ap) {
+// `waves` of a workgroup that takes 32 or fewer query rows; shares of multiples of `step` rows of the cache.
+static void plan_splits(const Plan& p, bool weights, int waves, int64_t step, AttendPlan* ap) {
     const int row_tiles = (p.rows + kTileRows - 1) / kTileRows;
     ap->row_tiles = row_tiles <= 1 ? 1 : row_tiles <= 2 ? 2 : row_tiles <= 4 ? 4 : row_tiles <= 8 ? 8 : 16;
     ap->row_groups = (row_tiles + ap->row_tiles - 1) / ap->row_tiles;
     // Shares are counted in what a workgroup takes at a time; workgroups left over go to the sequences with the largest.
-    const int64_t heads = (int64_t)p.n_layers * p.h_kv * ap->row_groups, unit = ap->row_tiles > 4 ? 64 : 128;
+    const int64_t heads = (int64_t)p.n_layers * p.h_kv * ap->row_groups, unit = ap->row_tiles > 4 ? 64 : step;
     int32_t units[JQ_MAX_SEQ];
     for (int s = 0; s < p.n_seq; ++s) units[s] = (int32_t)(((int64_t)p.tab.cu_seq[s + 1] - p.tab.cu_seq[s] + unit - 1) / unit);
     auto workgroups = [&](int64_t share) {
@@ -166,9 +167,10 @@ static void plan_splits(const Plan& p, bool weights, AttendPlan* ap) {
         ap->cu_split[s + 1] = ap->cu_split[s] + ns[s];
         most_L = std::max(most_L, L);
         most_ns = std::max(most_ns, ns[s]);
-        tiles = std::max(tiles, ((L + 31) / 32 + 4 * ns[s] - 1) / (4 * ns[s]));  // of 32 keys, a wave
+        tiles = std::max(tiles, ((L + 31) / 32 + waves * ns[s] - 1) / (waves * ns[s]));  // of 32 keys, a wave
     }
-    ap->hold_keys = weights && row_tiles <= 2 ? (int32_t)(tiles * 32 * kAttendWaves) : 0;
+    ap->waves = waves;
+    ap->hold_keys = weights && row_tiles <= 2 ? (int32_t)(tiles * 32 * waves) : 0;
     // (without shares there is nothing to join, and the weights are the sweep's)
     ap->one_launch = row_tiles <= 2 && (most_ns == 1 || (p.rows <= kMostJoinRows && most_ns <= kMostJoined && most_ns * p.rows <= kMostSums &&
                                                          (!weights || most_L * p.rows <= kMostWeighed)));
@@ -182,8 +184,8 @@ static uint64_t next_tag() {
     return (x ? x : 1) << 24;
 }
 
-void plan_attend(const Plan& p, bool weights, AttendPlan* ap) {
-    plan_splits(p, weights, ap);
+static void plan_attend(const Plan& p, bool weights, int waves, int64_t step, AttendPlan* ap) {
+    plan_splits(p, weights, waves, step, ap);
     const size_t parts = (size_t)p.n_layers * ap->cu_split[p.n_seq] * p.h_kv * p.rows;
     auto up = [](size_t x) { return (x + 255) / 256 * 256; };
     ap->logit_T = 32 * (p.T / 32 + p.n_seq);
@@ -192,6 +194,15 @@ void plan_attend(const Plan& p, bool weights, AttendPlan* ap) {
     ap->off_part = ap->off_stats + up(parts * sizeof(float2));
     ap->off_logits = ap->off_part + up(parts * kHeadDim * sizeof(float));
     ap->ws_bytes = ap->off_logits + (weights ? up((size_t)p.n_layers * p.h_kv * p.rows * ap->logit_T * sizeof(float)) : 0);
+}
+
+void plan_attend(const Plan& p, bool weights, bool coded, AttendPlan* ap) {
+    plan_attend(p, weights, kAttendWaves, 32 * kAttendWaves, ap);
+    const int waves = coded ? RowsCoded<8, 8>::waves(ap->row_tiles, weights) : kAttendWaves;
+    if (waves == kAttendWaves) return;
+    const size_t most = ap->ws_bytes;
+    plan_attend(p, weights, waves, 32 * waves, ap);
+    if (ap->ws_bytes > most) plan_attend(p, weights, waves, 32 * kAttendWaves, ap);  // (callers have one size for either kind of cache)
 }
 
 // Workgroups of a layer's sweep, and of the launch behind it: those that join, blocks of weights a (sequence, head).
@@ -210,7 +221,7 @@ static Finish finish_groups(const Plan& p, const AttendPlan& ap, bool weights) {
     return f;
 }
 bool attend_fits(const Plan& p, const AttendPlan& ap, bool weights) {
-    return sweep_groups(p, ap) * (ap.row_tiles > 2 ? 512 : kAttendThreads) <= UINT32_MAX && finish_groups(p, ap, weights).groups * kAttendThreads <= UINT32_MAX;
+    return sweep_groups(p, ap) * (ap.row_tiles > 2 ? 512 : 64 * ap.waves) <= UINT32_MAX && finish_groups(p, ap, weights).groups * kAttendThreads <= UINT32_MAX;
 }
 
 hipError_t launch_attend(const Plan& p, const AttendPlan& ap, const int32_t* lens, const uint32_t* seen, const void* Q, const void* K, const void* V,

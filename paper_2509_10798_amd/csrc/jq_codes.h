@@ -4,7 +4,8 @@
 //
 // These are the formats that the conversions v_cvt_scalef32_* take, two values an instruction, with the scale as the exponent of a
 // float.  A code has at most four significant bits, so its value is exact in bf16: attention over codes is attention over the bf16
-// rows that they stand for, and differs from it in nothing but how the rows come into registers.
+// rows that they stand for, and differs from it in nothing but how the rows come into registers.  The matrix instruction that takes codes
+// and scales as they lie (16x16x128, f8f6f4) was measured and left: its sums of 128 products are off by 2^-13 of the sum of their sizes.
 //
 // Layout: [layers][KV heads][rows][bytes], in pages [layers][pages][KV heads][rows of a page][bytes], the four scales of a row apart in
 // the same order.  Heads lie outside the rows, other than in a bf16 cache, because a workgroup reads one head's: rows of 64 or 128 bytes
@@ -17,7 +18,6 @@ namespace jq {
 constexpr int kGroupDims = 32;
 constexpr int kGroups = kHeadDim / kGroupDims;
 
-typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef short s16x2 __attribute__((ext_vector_type(2)));
 
 __device__ __forceinline__ float scale_of(uint32_t byte) { return __uint_as_float(byte << 23); }
@@ -48,12 +48,34 @@ __device__ __forceinline__ void load_eight(uint32_t* codes, const char* p) {
 template <int KB, int VB>
 struct RowsCoded {
     static constexpr bool kCoded = true;
-    static constexpr int kAhead = 2;
+    // Two waves a SIMD: one issues a vector instruction every five cycles, two of them every other.  Twice the tiles of a bf16 cache
+    // go through a CU in the time that memory takes, and with four waves a workgroup that bounded the call (us with four / eight:
+    // one token over 131072 rows in 4 bits 46.7 / 37, 32 sequences of 2048 rows in 8 bits with weights 34.6 / 29.2).  Tiles requested two and
+    // four ahead took 1.5 and 7 us more: a call this short is over before the longer start has paid.  (17 to 32 query rows with weights: the
+    // sums of eight waves and the logits held do not fit LDS together.)
+    static constexpr int waves(int row_tiles, bool weights) { return row_tiles == 1 || !weights ? 8 : kAttendWaves; }
+    static constexpr int least_waves(int) { return 2; }
     static constexpr int kKRow = kHeadDim * KB / 8, kVRow = kHeadDim * VB / 8;
+    // The scale that lane `E` of the lane's four holds.
+    template <int E>
+    static __device__ __forceinline__ float scale_in_four(uint32_t byte) {
+        return scale_of((uint32_t)__builtin_amdgcn_mov_dpp((int)byte, E * 0x55, 0xF, 0xF, true));
+    }
     // 32 keys: of key 16 i + l % 16 the group l / 16 of K, whose 32 terms of a sum are then the lane's; of V eight dimensions of key
     // 16 i + 4 (l / 16) + e as in a KvTile, whose group is (l % 16) / 4, and of the four lanes that share this group one scale each.
     struct Tile {
         uint32_t k[2][KB], v[2][4][VB / 4], k_scale[2], v_scale[2];
+        __device__ __forceinline__ au32x4 key_piece(int i, int c) const { return eight_values<KB>(k[i] + c * (KB / 4), scale_of(k_scale[i])); }
+        template <int W>
+        __device__ __forceinline__ void value_words(uint32_t (&x)[2][4]) const {
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                x[i][0] = two_values<VB, W>(v[i][0], scale_in_four<0>(v_scale[i]));
+                x[i][1] = two_values<VB, W>(v[i][1], scale_in_four<1>(v_scale[i]));
+                x[i][2] = two_values<VB, W>(v[i][2], scale_in_four<2>(v_scale[i]));
+                x[i][3] = two_values<VB, W>(v[i][3], scale_in_four<3>(v_scale[i]));
+            }
+        }
     };
     struct Piece {
         uint32_t codes[2], scale;
@@ -102,10 +124,28 @@ struct RowsCoded {
             }
         }
     }
-    // The scale that lane `E` of the lane's four holds.
-    template <int E>
-    static __device__ __forceinline__ float scale_in_four(uint32_t byte) {
-        return scale_of((uint32_t)__builtin_amdgcn_update_dpp(0, (int)byte, E * 0x55, 0xF, 0xF, false));
+    // The same of a tile that is all there: a uniform address, the lane's offset from it, the rest in the instruction.
+    __device__ __forceinline__ void load_whole(Tile& t, uint32_t row0, int lane) const {
+        const uint32_t quarter = (uint32_t)(lane >> 4), part = (uint32_t)(lane & 15);
+        const char* k = K + row0 * kKRow;
+        const char* v = V + row0 * kVRow;
+        const uint8_t* ks = K_scale + row0 * kGroups;
+        const uint8_t* vs = V_scale + row0 * kGroups;
+        const uint32_t k_at = part * kKRow + quarter * (kKRow / 4), v_at = quarter * (4 * kVRow) + part * VB;
+        const uint32_t ks_at = part * kGroups + quarter, vs_at = (4 * quarter + (part & 3)) * kGroups + (part >> 2);
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            t.k_scale[i] = (ks + ks_at)[16 * i * kGroups];
+            t.v_scale[i] = (vs + vs_at)[16 * i * kGroups];
+#pragma unroll
+            for (int h = 0; h < KB / 4; ++h) {
+                const au32x4 x = *(const au32x4*)((k + k_at) + (16 * i * kKRow + 16 * h));
+#pragma unroll
+                for (int w = 0; w < 4; ++w) t.k[i][4 * h + w] = x[w];
+            }
+#pragma unroll
+            for (int e = 0; e < 4; ++e) load_eight<VB>(t.v[i][e], (v + v_at) + (16 * i + e) * kVRow);
+        }
     }
     static __device__ __forceinline__ void unpack(KvTile& to, const Tile& t, int) {
 #pragma unroll

@@ -355,12 +355,13 @@ constexpr int kMaxWeighRows = 128;  // most query rows per KV head whose weights
 struct AttendPlan {
     int32_t hold_keys;                  // rows of the cache whose logits a workgroup holds, with weights
     int32_t row_tiles, row_groups;      // tiles of 16 query rows a workgroup takes, workgroups over the same keys
+    int32_t waves;                      // of a workgroup that takes one or two tiles
     int32_t cu_split[JQ_MAX_SEQ + 1];   // workgroups that share a sequence (per layer, KV head and group of rows), summed up
     bool one_launch;                    // the workgroup that completes a sequence joins it (and weighs)
     int64_t logit_T;
     size_t off_arrived, off_stats, off_part, off_logits, ws_bytes;
 };
-void plan_attend(const Plan& p, bool weights, AttendPlan* ap);
+void plan_attend(const Plan& p, bool weights, bool coded, AttendPlan* ap);
 bool attend_fits(const Plan& p, const AttendPlan& ap, bool weights);  // every launch stays below 2^32 threads
 // `lens`, `seen`, `lse`, `weights` may be null; with `seen` the queries are drafted tokens, otherwise p.window says whether they are causal.
 // With `codes` the cache is one of codes, and K and V are null.
