@@ -16,31 +16,35 @@ constexpr int kSharedWaves = 8, kSharedThreads = 64 * kSharedWaves;
 struct SharedArgs {
     PrefixArgs prefix;
     OwnArgs own;
-    int32_t prefix_blocks;
+    int32_t prefix_blocks, own_blocks;  // shares of either sweep; a workgroup may take one of each
 };
 
 // P: tiles of 16 query rows of a prefix that a workgroup takes, RT: of a sequence.
 template <class Rows, int P, int RT>
 __global__ __launch_bounds__(kSharedThreads, 2) void jq_attend_shared_kernel(SharedArgs) {
     const SharedArgs& a = kernel_args<SharedArgs>();
-    const int bx = (int)blockIdx.x;
+    const int bx = (int)blockIdx.x, grid = (int)gridDim.x;
     if (bx < a.prefix_blocks) {
         if constexpr (P <= 2) attend_few_rows<Rows, P, kSeeAll, false, kSharedWaves>(a.prefix, bx, (int)blockIdx.y);
         else attend_many_rows<Rows, P / 2, kSeeAll, false>(a.prefix, bx, (int)blockIdx.y);
-    } else {
-        attend_few_rows<Rows, RT, kSeeCausal, false, kSharedWaves>(a.own, bx - a.prefix_blocks, (int)blockIdx.y);
+    }
+    // Shares of the sequences go to the workgroups that have none of a prefix, then around.
+    for (int u = bx - a.prefix_blocks + (bx < a.prefix_blocks ? grid : 0); u < a.own_blocks; u += grid) {
+        __syncthreads();  // (LDS: what the sums before lie in)
+        attend_few_rows<Rows, RT, kSeeCausal, false, kSharedWaves>(a.own, u, (int)blockIdx.y);
     }
 }
 
-// A wave joins the parts of one (layer, sequence, KV head, query row).
+// A workgroup joins the parts of one (layer, sequence, KV head, query row): each of its waves every fourth, two at a time, all of them
+// requested together ahead of the statistics (up to 64 parts; one wave a row, in turns of sixteen parts, took 2 us more).
+constexpr int kJoinBatch = 8;
 __global__ __launch_bounds__(kAttendThreads) void jq_attend_shared_join_kernel(SharedArgs) {
+    __shared__ __align__(16) float sums[kAttendWaves][kHeadDim];
     const SharedArgs& a = kernel_args<SharedArgs>();
     const OwnArgs& own = a.own;
     const PrefixArgs& pre = a.prefix;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), layer = blockIdx.y;
-    const int item = (int)blockIdx.x * kAttendWaves + wave;
-    if (item >= own.n_seq * own.h_kv * own.rows) return;
-    const int unit = item / own.rows, row = item - unit * own.rows, s = unit / own.h_kv, g = unit - s * own.h_kv;
+    const int unit = (int)blockIdx.x / own.rows, row = (int)blockIdx.x - unit * own.rows, s = unit / own.h_kv, g = unit - s * own.h_kv;
     int p = 0;  // the sequence's prefix
     if (pre.n_seq > 1) {
         p = __popcll(__ballot(lane + 1 < pre.n_seq && pre.cu_member[min(lane + 1, pre.n_seq)] <= s));
@@ -50,16 +54,17 @@ __global__ __launch_bounds__(kAttendThreads) void jq_attend_shared_join_kernel(S
     const int64_t own_at = part_at(own, layer, s, own.cu_split[s], 0, g) + row, own_step = (int64_t)own.h_kv * own.rows;
     const int64_t pre_at = part_at(pre, layer, p, 0, 0, g) + (s - pre.cu_member[p]) * own.rows + row, pre_step = (int64_t)own.h_kv * query_rows(pre, p);
     auto stat = [&](int i) { return i < n_own ? own.stats[own_at + i * own_step] : pre.stats[pre_at + (i - n_own) * pre_step]; };
-    // two parts at a time, 16 bytes a lane; the first sixteen are requested ahead of the statistics
-    const int half = lane >> 5, d = (lane & 31) * 4;
+    const int d = (lane & 31) * 4;
     auto part = [&](int i) {
         const float* from = i < n_own ? own.part + (own_at + i * own_step) * kHeadDim : pre.part + (pre_at + (i - n_own) * pre_step) * kHeadDim;
         return *(const f32x4*)(from + d);
     };
-    constexpr int kBatch = 8;
-    f32x4 x[kBatch];
+    const int first = 2 * wave + (lane >> 5);  // the lane's parts: first, first + 8, ..
+    constexpr int kStep = 2 * kAttendWaves;
+    f32x4 x[kJoinBatch];
 #pragma unroll
-    for (int k = 0; k < kBatch; ++k) x[k] = part(min(half + 2 * k, n - 1));
+    for (int k = 0; k < kJoinBatch; ++k)
+        if (kStep * k < n) x[k] = part(min(first + kStep * k, n - 1));
     const float2 mine = lane < n ? stat(lane) : make_float2(-__builtin_inff(), 0.0f);
     float m = mine.x;
     for (int i = lane + 64; i < n; i += 64) m = fmaxf(m, stat(i).x);
@@ -74,13 +79,12 @@ __global__ __launch_bounds__(kAttendThreads) void jq_attend_shared_join_kernel(S
 #pragma unroll
     for (int k = 32; k; k >>= 1) z += __shfl_xor(z, k);
     f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
-    for (int i0 = 0; i0 < n; i0 += 2 * kBatch) {
-        if (i0)
+    for (int i0 = 0; i0 < n; i0 += kStep * kJoinBatch) {
 #pragma unroll
-            for (int k = 0; k < kBatch; ++k) x[k] = part(min(i0 + half + 2 * k, n - 1));
-#pragma unroll
-        for (int k = 0; k < kBatch; ++k) {
-            const int i = i0 + half + 2 * k;
+        for (int k = 0; k < kJoinBatch; ++k) {
+            const int i = i0 + first + kStep * k;
+            if (i0 + kStep * k >= n) break;
+            if (i0) x[k] = part(min(i, n - 1));
             float f = __shfl(factor, i & 63);
             if (i >= 64) f = rescale(stat(min(i, n - 1)).x, m);
 #pragma unroll
@@ -89,57 +93,95 @@ __global__ __launch_bounds__(kAttendThreads) void jq_attend_shared_join_kernel(S
     }
 #pragma unroll
     for (int e = 0; e < 4; ++e) o[e] += __shfl_xor(o[e], 32);
-    if (lane < 32) store_out(own, layer, s, g, row, d, o, m, z);
+    if (lane < 32) *(f32x4*)(sums[wave] + d) = o;
+    __syncthreads();
+    if (threadIdx.x >= 32) return;
+    o = *(const f32x4*)(sums[0] + d);
+#pragma unroll
+    for (int w = 1; w < kAttendWaves; ++w) o += *(const f32x4*)(sums[w] + d);
+    store_out(own, layer, s, g, row, d, o, m, z);
 }
 
 // ---- host ------------------------------------------------------------------------------------------------------------------
 
 constexpr int kSharedChip = 256;  // workgroups that run at a time, one a CU
 
-// How the work is shared out: every prefix and every sequence in shares of at most so many rows, one size for all of them.
+// How the work is shared out.  Prefixes and sequences are cut into shares, either side by side, on CUs of their own, or, where there is
+// much of both, one behind the other on all of them: what a CU reads in a given time is limited, some 25 GB/s, however many of its
+// waves ask, so a sweep that has few CUs takes long.  Fewer shares leave fewer parts to write and to join; fewer query rows a workgroup
+// (and the prefix read twice, which meets in an XCD's L2) halve them too.  In nanoseconds, as measured on one MI355X.
+constexpr int64_t kSharedStart = 6000, kSharedNext = 3000, kOwnRow = 22, kPartBytes = 4000;  // (the last: bytes a nanosecond, there and back)
+static int64_t prefix_row_time(int tiles) { return tiles <= 8 ? 25 : 36; }
 void plan_shared(const Plan& p, const Plan& pp, const int32_t* cu_members, SharedPlan* sp) {
-    int32_t most_rows = 0;
-    for (int i = 0; i < pp.n_seq; ++i) most_rows = std::max(most_rows, (cu_members[i + 1] - cu_members[i]) * p.rows);
-    const int tiles = (most_rows + kTileRows - 1) / kTileRows;
-    sp->prefix_tiles = tiles <= 1 ? 1 : tiles <= 2 ? 2 : tiles <= 4 ? 4 : tiles <= 8 ? 8 : 16;
-    sp->prefix_groups = (tiles + sp->prefix_tiles - 1) / sp->prefix_tiles;
     const int own_tiles = (p.rows + kTileRows - 1) / kTileRows;
     sp->own_tiles = own_tiles <= 1 ? 1 : 2;
     sp->own_groups = (own_tiles + sp->own_tiles - 1) / sp->own_tiles;
-    const int64_t heads = (int64_t)p.n_layers * p.h_kv, unit = 256, start = 512;
-    auto length = [](const Plan& q, int s) { return (int64_t)q.tab.cu_seq[s + 1] - q.tab.cu_seq[s]; };
-    auto groups = [&](int i) { return ((cu_members[i + 1] - cu_members[i]) * p.rows + sp->prefix_tiles * kTileRows - 1) / (sp->prefix_tiles * kTileRows); };
-    int64_t total = 0;
-    for (int i = 0; i < pp.n_seq; ++i) total += length(pp, i) * heads * groups(i);
-    for (int s = 0; s < p.n_seq; ++s) total += length(p, s) * heads * sp->own_groups;
-    // from four rounds of the chip to half of one
-    int64_t best = INT64_MAX, share = 1;
-    const int64_t even = total / (kSharedChip * unit);
-    for (int64_t c = even / 4 + 1; c <= 2 * even + 2; c += 1 + c / 8) {
-        const uint32_t size = (uint32_t)std::min(c * unit, (int64_t)INT32_MAX);
-        int64_t n = 0, all = 0, largest = 0, last = 0;
-        auto add = [&](int64_t rows, int64_t times) {
-            const uint32_t k = ((uint32_t)rows + size - 1) / size;
-            last = ((uint32_t)rows + k - 1) / k + start;
-            n += k * times;
-            all += k * times * last;
-            largest = std::max(largest, last);
-        };
-        for (int i = 0; i < pp.n_seq; ++i) add(length(pp, i), heads * groups(i));
-        for (int s = 0; s < p.n_seq; ++s) add(length(p, s), heads * sp->own_groups);
-        const int64_t cost = n <= kSharedChip ? largest : std::max(largest, all / kSharedChip + last / 2);
-        if (cost < best) { best = cost; share = c; }
+    const int64_t heads = (int64_t)p.n_layers * p.h_kv;
+    int32_t longest = 0, longest_own = 0, most_rows = 0;
+    int32_t length[JQ_MAX_SEQ], own_length[JQ_MAX_SEQ], rows[JQ_MAX_SEQ];
+    for (int i = 0; i < pp.n_seq; ++i) {
+        length[i] = pp.tab.cu_seq[i + 1] - pp.tab.cu_seq[i];
+        rows[i] = (cu_members[i + 1] - cu_members[i]) * p.rows;
+        longest = std::max(longest, length[i]);
+        most_rows = std::max(most_rows, rows[i]);
     }
-    const int64_t size = share * unit;
+    for (int s = 0; s < p.n_seq; ++s) {
+        own_length[s] = p.tab.cu_seq[s + 1] - p.tab.cu_seq[s];
+        longest_own = std::max(longest_own, own_length[s]);
+    }
+    auto split = [](int32_t rows, int64_t share) { return (int64_t)(((uint32_t)rows + (uint32_t)share - 1) / (uint32_t)share); };
+    // The smallest share, in multiples of `unit` rows, that makes no more than `most` workgroups, if any does.
+    auto smallest = [](auto blocks, int32_t rows, int64_t unit, int64_t most) {
+        int64_t lo = 1, hi = (rows + unit - 1) / unit;
+        while (lo < hi) {
+            const int64_t mid = (lo + hi) / 2;
+            if (blocks(mid * unit) <= most) hi = mid; else lo = mid + 1;
+        }
+        return lo * unit;
+    };
+    auto own_blocks = [&](int64_t share) {
+        int64_t n = 0;
+        for (int s = 0; s < p.n_seq; ++s) n += split(own_length[s], share);
+        return n * heads * sp->own_groups;
+    };
+    constexpr int kChoices = 4;  // all CUs for both, or three, two, one quarter for the prefixes
+    int64_t own_of[kChoices], own_n[kChoices];
+    for (int c = 0; c < kChoices; ++c) {
+        own_of[c] = smallest(own_blocks, longest_own, 256, c ? c * kSharedChip / kChoices : kSharedChip);
+        own_n[c] = own_blocks(own_of[c]);
+    }
+    const int tiles = (most_rows + kTileRows - 1) / kTileRows, natural = tiles <= 1 ? 1 : tiles <= 2 ? 2 : tiles <= 4 ? 4 : tiles <= 8 ? 8 : 16;
+    int64_t best = INT64_MAX, share = 1, own_share = 1;
+    for (int each = natural; each >= std::max(natural / 2, std::min(natural, 4)); each /= 2) {
+        int64_t groups[JQ_MAX_SEQ];
+        for (int i = 0; i < pp.n_seq; ++i) groups[i] = (rows[i] + each * kTileRows - 1) / (each * kTileRows);
+        auto prefix_blocks = [&](int64_t share) {
+            int64_t n = 0;
+            for (int i = 0; i < pp.n_seq; ++i) n += split(length[i], share) * groups[i];
+            return n * heads;
+        };
+        for (int c = 0; c < kChoices; ++c) {
+            const int64_t size = smallest(prefix_blocks, longest, each <= 2 ? 256 : each == 4 ? 128 : 64, kSharedChip - c * kSharedChip / kChoices);
+            const int64_t n = prefix_blocks(size), m = own_n[c];
+            const int64_t time = std::min(size, (int64_t)longest) * prefix_row_time(each), own_time = std::min(own_of[c], (int64_t)longest_own) * kOwnRow;
+            const int64_t rounds = (n + kSharedChip - 1) / kSharedChip, own_rounds = (m + kSharedChip - 1) / kSharedChip;
+            int64_t cost = n + m <= kSharedChip ? kSharedStart + std::max(time, own_time) : rounds * (kSharedStart + time) + own_rounds * (kSharedNext + own_time);
+            int64_t parts = 0;
+            for (int i = 0; i < pp.n_seq; ++i) parts += split(length[i], size) * rows[i];
+            cost += (parts * heads + m * p.rows) * (2 * kHeadDim * (int64_t)sizeof(float)) / kPartBytes;
+            if (cost < best) { best = cost; share = size; own_share = own_of[c]; sp->prefix_tiles = each; }
+        }
+    }
+    sp->prefix_groups = (tiles + sp->prefix_tiles - 1) / sp->prefix_tiles;
     sp->cu_split[0] = sp->cu_part[0] = sp->own_split[0] = 0;
     int64_t parts = 0;
     for (int i = 0; i < pp.n_seq; ++i) {
-        const int64_t ns = (length(pp, i) + size - 1) / size;
+        const int64_t ns = split(length[i], share);
         sp->cu_split[i + 1] = sp->cu_split[i] + (int32_t)ns;
-        parts += ns * (cu_members[i + 1] - cu_members[i]) * p.rows;
+        parts += ns * rows[i];
         sp->cu_part[i + 1] = (int32_t)parts;
     }
-    for (int s = 0; s < p.n_seq; ++s) sp->own_split[s + 1] = sp->own_split[s] + (int32_t)((length(p, s) + size - 1) / size);
+    for (int s = 0; s < p.n_seq; ++s) sp->own_split[s + 1] = sp->own_split[s] + (int32_t)split(own_length[s], own_share);
     sp->fits = parts <= INT32_MAX;
     auto up = [](size_t x) { return (x + 255) / 256 * 256; };
     const size_t pre = (size_t)heads * (size_t)parts, own = (size_t)heads * sp->own_split[p.n_seq] * p.rows;
@@ -149,7 +191,7 @@ void plan_shared(const Plan& p, const Plan& pp, const int32_t* cu_members, Share
     sp->off_own_part = sp->off_own_stats + up(own * sizeof(float2));
     sp->ws_bytes = sp->off_own_part + up(own * kHeadDim * sizeof(float));
     const int64_t blocks = shared_blocks(sp->cu_split[pp.n_seq], p.h_kv, sp->prefix_groups) + shared_blocks(sp->own_split[p.n_seq], p.h_kv, sp->own_groups);
-    const int64_t joins = ((int64_t)p.n_seq * p.h_kv * p.rows + kAttendWaves - 1) / kAttendWaves;
+    const int64_t joins = (int64_t)p.n_seq * p.h_kv * p.rows;
     sp->fits = sp->fits && blocks * kSharedThreads <= UINT32_MAX && joins * kAttendThreads <= UINT32_MAX;
 }
 
@@ -198,7 +240,10 @@ hipError_t launch_attend_shared(const Plan& p, const Plan& pp, const SharedPlan&
     for (int s = 0; s <= p.n_seq; ++s) a.own.cu_split[s] = sp.own_split[s];
     a.own.causal = p.window && p.n_q > 1;
     a.prefix_blocks = (int32_t)shared_blocks(a.prefix.n_splits, p.h_kv, sp.prefix_groups);
-    const dim3 grid((unsigned)(a.prefix_blocks + shared_blocks(a.own.n_splits, p.h_kv, sp.own_groups)), (unsigned)p.n_layers);
+    a.own_blocks = (int32_t)shared_blocks(a.own.n_splits, p.h_kv, sp.own_groups);
+    // more than the CUs take at a time, with layers on top: all in one round of workgroups if the prefixes are
+    const int64_t all = (int64_t)a.prefix_blocks + a.own_blocks, most = std::max<int64_t>(kSharedChip / p.n_layers, 1);
+    const dim3 grid((unsigned)(all <= most || a.prefix_blocks > most ? all : most), (unsigned)p.n_layers);
     hipError_t e;
     switch (sp.prefix_tiles) {
         case 1: e = launch_shared_sweep<1>(a, sp.own_tiles, grid, st); break;
@@ -208,7 +253,7 @@ hipError_t launch_attend_shared(const Plan& p, const Plan& pp, const SharedPlan&
         default: e = launch_shared_sweep<16>(a, sp.own_tiles, grid, st); break;
     }
     if (e != hipSuccess) return e;
-    const int64_t joins = ((int64_t)p.n_seq * p.h_kv * p.rows + kAttendWaves - 1) / kAttendWaves;
+    const int64_t joins = (int64_t)p.n_seq * p.h_kv * p.rows;
     return launch_kernel(jq_attend_shared_join_kernel, dim3((unsigned)joins, (unsigned)p.n_layers), dim3(kAttendThreads), 0, st, nullptr, -1, a);
 }
 
