@@ -69,7 +69,7 @@ struct AttendArgs {
 
 // Sequences that continue shared prefixes (jq_shared.hip): a sweep over the prefixes, whose query rows are those of all the sequences
 // that continue one, and a sweep over the sequences' own rows.  Both always leave parts.
-struct PrefixArgs : AttendArgs {  // n_seq, lens, cu_seq, cu_split: of prefixes; rows: of the one with most
+struct PrefixArgs : AttendArgs {  // n_seq, lens, cu_seq: of prefixes; cu_split: in place of splits, eighths of their workgroups
     static constexpr int kShare = 1;
     int32_t cu_member[JQ_MAX_SEQ + 1];  // sequences that continue a prefix
     int32_t cu_part[JQ_MAX_SEQ + 1];    // parts of a prefix: splits times query rows, of each layer and KV head
@@ -117,6 +117,34 @@ __device__ __forceinline__ int seq_of_split(const AttendArgs& a, int split, int 
     int s = __popcll(__ballot(lane + 1 < a.n_seq && a.cu_split[min(lane + 1, a.n_seq)] <= split));
     if (a.n_seq > 64) s += __popcll(__ballot(lane + 65 < a.n_seq && a.cu_split[min(lane + 65, a.n_seq)] <= split));
     return s;
+}
+
+// What the workgroup `bx` of a layer does: which share of a sequence's keys it sweeps, for which KV head and group of query rows.
+// Groups of query rows over the same keys lie eight workgroups apart, so that they meet in one XCD's L2.
+struct KeyShare {
+    int s, split, ns, mine, g, rg;  // sequence, share among all, shares of the sequence, share among these, KV head, group
+    bool none;
+};
+__device__ __forceinline__ KeyShare key_share_of(const AttendArgs& a, int bx, int, int lane) {
+    const int per = 8 * a.row_groups;
+    const int u = bx / per * 8 + (bx & 7), rg = (bx % per) >> 3;
+    if (u >= a.units) return KeyShare{0, 0, 0, 0, 0, 0, true};
+    const int split = u / a.h_kv, g = u - split * a.h_kv, s = seq_of_split(a, split, lane);
+    return KeyShare{s, split, a.cu_split[s + 1] - a.cu_split[s], split - a.cu_split[s], g, rg, false};
+}
+// Prefixes have as many groups as their own rows ask for (`rows` each): with as many as the largest, workgroups that had nothing to do
+// stood between the others, and some CUs were left two of these (three prefixes with 192, 80 and 16 query rows 92 us for 64).
+__device__ __forceinline__ KeyShare key_share_of(const PrefixArgs& a, int bx, int rows, int lane) {
+    int s = 0, ns = a.n_splits, per = 8 * a.row_groups;  // of one prefix
+    if (a.n_seq > 1) {
+        s = seq_of_split(a, bx >> 3, lane);
+        const int mine_rows = (a.cu_member[s + 1] - a.cu_member[s]) * a.n_q * a.group;
+        ns = (a.cu_part[s + 1] - a.cu_part[s]) / mine_rows;
+        per = 8 * ((mine_rows + rows - 1) / rows);
+    }
+    const int at = bx - 8 * a.cu_split[s];
+    const int u = at / per * 8 + (at & 7), mine = u / a.h_kv;
+    return KeyShare{s, 0, ns, mine, u - mine * a.h_kv, (at % per) >> 3, u >= ns * a.h_kv};
 }
 
 // log2 of a sum: v_log_f32 rounds towards zero and is off by more the larger its result, so it only sees the mantissa.
@@ -517,16 +545,11 @@ __device__ __forceinline__ void attend_few_rows(const Args& a, int bx, int layer
     constexpr bool kParts = Args::kShare != 0;
     static_assert(!(KEEP && kParts), "weights are those of one sweep");
     float2* lds_stats = (float2*)(lds + WAVES * RT * kTileRows * kOutStride);
-    // bx: groups of query rows over the same keys eight apart, so that they meet in one XCD's L2
-    const int per = 8 * a.row_groups;
-    const int u = bx / per * 8 + (bx & 7), rg = (bx % per) >> 3;
-    if (u >= a.units) return;
-    const int split = u / a.h_kv, g = u - split * a.h_kv;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
-    const int s = seq_of_split(a, split, lane);
-    const int ns = a.cu_split[s + 1] - a.cu_split[s], mine = split - a.cu_split[s];
+    const KeyShare share = key_share_of(a, bx, RT * kTileRows, lane);
+    if (share.none) return;
+    const int split = share.split, g = share.g, s = share.s, rg = share.rg, ns = share.ns, mine = share.mine;
     const int row0 = rg * RT * kTileRows;
-    if (Args::kShare == 1 && row0 >= query_rows(a, s)) return;  // (a prefix that fewer sequences continue)
 
     // Tiles of 32 keys, dealt to the sequence's waves in turn, so that all of them sweep one moving window of the cache.
     const Rows rows(a, layer, s, g);
@@ -823,17 +846,13 @@ __device__ __forceinline__ void attend_many_rows(const Args& a, int bx, int laye
     constexpr bool kParts = Args::kShare != 0;
     uint8_t* marked = (uint8_t*)wide_lds + W::kFlags;  // [kWaves]: the wave has cleared values of V, or has sums that are not finite
     bool was_cleared = false;
-    const int per = 8 * a.row_groups;
-    const int u = bx / per * 8 + (bx & 7), rg = (bx % per) >> 3;
-    if (u >= a.units) return;
-    const int split = u / a.h_kv, g = u - split * a.h_kv;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
-    const int s = seq_of_split(a, split, lane);
-    const int ns = a.cu_split[s + 1] - a.cu_split[s], mine = split - a.cu_split[s];
+    const KeyShare share = key_share_of(a, bx, W::kRows, lane);
+    if (share.none) return;
+    const int split = share.split, g = share.g, s = share.s, rg = share.rg, ns = share.ns, mine = share.mine;
     const int cap = a.cu_seq[s + 1] - a.cu_seq[s];
     const int rw = wave % R, kw = wave / R;
     const int row0 = rg * W::kRows + 32 * rw;
-    if (Args::kShare == 1 && rg * W::kRows >= query_rows(a, s)) return;  // (a prefix that fewer sequences continue)
 
     const Rows rows(a, layer, s, g);
 

@@ -373,8 +373,10 @@ hipError_t launch_attend(const Plan& p, const AttendPlan& ap, const int32_t* len
                          void* out, float* lse, float* weights, char* ws, hipStream_t st, const Codes* codes = nullptr);
 // Sequences that continue shared prefixes (jq_shared.hip); `pp`: the plan of the prefixes.
 struct SharedPlan {
-    int32_t prefix_tiles, prefix_groups, own_tiles, own_groups;  // tiles of 16 query rows a workgroup takes, workgroups over the same keys
-    int32_t cu_split[JQ_MAX_SEQ + 1], own_split[JQ_MAX_SEQ + 1];  // workgroups that share a prefix, a sequence, summed up
+    int32_t prefix_tiles, own_tiles, own_groups;  // tiles of 16 query rows a workgroup takes, workgroups over the same keys
+    int32_t first_groups, first_splits;           // of the first prefix
+    int32_t cu_split[JQ_MAX_SEQ + 1];             // eighths of a prefix's workgroups (of a layer), summed up
+    int32_t own_split[JQ_MAX_SEQ + 1];            // workgroups that share a sequence, summed up
     int32_t cu_part[JQ_MAX_SEQ + 1];                              // splits times query rows of the prefixes, summed up
     bool fits;                                                    // every launch stays below 2^32 threads
     size_t off_prefix_stats, off_prefix_part, off_own_stats, off_own_part, ws_bytes;

@@ -50,7 +50,7 @@ __global__ __launch_bounds__(kAttendThreads) void jq_attend_shared_join_kernel(S
         p = __popcll(__ballot(lane + 1 < pre.n_seq && pre.cu_member[min(lane + 1, pre.n_seq)] <= s));
         if (pre.n_seq > 64) p += __popcll(__ballot(lane + 65 < pre.n_seq && pre.cu_member[min(lane + 65, pre.n_seq)] <= s));
     }
-    const int n_own = own.cu_split[s + 1] - own.cu_split[s], n = n_own + pre.cu_split[p + 1] - pre.cu_split[p];
+    const int n_own = own.cu_split[s + 1] - own.cu_split[s], n = n_own + (pre.cu_part[p + 1] - pre.cu_part[p]) / query_rows(pre, p);
     const int64_t own_at = part_at(own, layer, s, own.cu_split[s], 0, g) + row, own_step = (int64_t)own.h_kv * own.rows;
     const int64_t pre_at = part_at(pre, layer, p, 0, 0, g) + (s - pre.cu_member[p]) * own.rows + row, pre_step = (int64_t)own.h_kv * query_rows(pre, p);
     auto stat = [&](int i) { return i < n_own ? own.stats[own_at + i * own_step] : pre.stats[pre_at + (i - n_own) * pre_step]; };
@@ -172,17 +172,19 @@ void plan_shared(const Plan& p, const Plan& pp, const int32_t* cu_members, Share
             if (cost < best) { best = cost; share = size; own_share = own_of[c]; sp->prefix_tiles = each; }
         }
     }
-    sp->prefix_groups = (tiles + sp->prefix_tiles - 1) / sp->prefix_tiles;
     sp->cu_split[0] = sp->cu_part[0] = sp->own_split[0] = 0;
-    int64_t parts = 0;
+    int64_t parts = 0, eighths = 0;
     for (int i = 0; i < pp.n_seq; ++i) {
         const int64_t ns = split(length[i], share);
-        sp->cu_split[i + 1] = sp->cu_split[i] + (int32_t)ns;
+        const int64_t groups = (rows[i] + sp->prefix_tiles * kTileRows - 1) / (sp->prefix_tiles * kTileRows);
+        eighths += (ns * p.h_kv + 7) / 8 * groups;
+        if (i == 0) { sp->first_groups = (int32_t)groups; sp->first_splits = (int32_t)ns; }
+        sp->cu_split[i + 1] = (int32_t)eighths;
         parts += ns * rows[i];
         sp->cu_part[i + 1] = (int32_t)parts;
     }
     for (int s = 0; s < p.n_seq; ++s) sp->own_split[s + 1] = sp->own_split[s] + (int32_t)split(own_length[s], own_share);
-    sp->fits = parts <= INT32_MAX;
+    sp->fits = parts <= INT32_MAX && eighths <= INT32_MAX / 8;
     auto up = [](size_t x) { return (x + 255) / 256 * 256; };
     const size_t pre = (size_t)heads * (size_t)parts, own = (size_t)heads * sp->own_split[p.n_seq] * p.rows;
     sp->off_prefix_stats = 0;
@@ -190,7 +192,7 @@ void plan_shared(const Plan& p, const Plan& pp, const int32_t* cu_members, Share
     sp->off_own_stats = sp->off_prefix_part + up(pre * kHeadDim * sizeof(float));
     sp->off_own_part = sp->off_own_stats + up(own * sizeof(float2));
     sp->ws_bytes = sp->off_own_part + up(own * kHeadDim * sizeof(float));
-    const int64_t blocks = shared_blocks(sp->cu_split[pp.n_seq], p.h_kv, sp->prefix_groups) + shared_blocks(sp->own_split[p.n_seq], p.h_kv, sp->own_groups);
+    const int64_t blocks = 8 * eighths + shared_blocks(sp->own_split[p.n_seq], p.h_kv, sp->own_groups);
     const int64_t joins = (int64_t)p.n_seq * p.h_kv * p.rows;
     sp->fits = sp->fits && blocks * kSharedThreads <= UINT32_MAX && joins * kAttendThreads <= UINT32_MAX;
 }
@@ -233,13 +235,14 @@ hipError_t launch_attend_shared(const Plan& p, const Plan& pp, const SharedPlan&
     a.prefix.stats = (float2*)(ws + sp.off_prefix_stats); a.prefix.part = (float*)(ws + sp.off_prefix_part);
     a.own.stats = (float2*)(ws + sp.off_own_stats); a.own.part = (float*)(ws + sp.off_own_part);
     a.own.rows = p.rows;
-    a.prefix.row_groups = sp.prefix_groups; a.own.row_groups = sp.own_groups;
-    a.prefix.n_splits = sp.cu_split[pp.n_seq]; a.own.n_splits = sp.own_split[p.n_seq];
-    a.prefix.units = a.prefix.n_splits * p.h_kv; a.own.units = a.own.n_splits * p.h_kv;
+    a.prefix.row_groups = sp.first_groups; a.prefix.n_splits = sp.first_splits;
+    a.own.row_groups = sp.own_groups;
+    a.own.n_splits = sp.own_split[p.n_seq];
+    a.own.units = a.own.n_splits * p.h_kv;
     for (int i = 0; i <= pp.n_seq; ++i) { a.prefix.cu_split[i] = sp.cu_split[i]; a.prefix.cu_part[i] = sp.cu_part[i]; a.prefix.cu_member[i] = cu_members[i]; }
     for (int s = 0; s <= p.n_seq; ++s) a.own.cu_split[s] = sp.own_split[s];
     a.own.causal = p.window && p.n_q > 1;
-    a.prefix_blocks = (int32_t)shared_blocks(a.prefix.n_splits, p.h_kv, sp.prefix_groups);
+    a.prefix_blocks = 8 * sp.cu_split[pp.n_seq];
     a.own_blocks = (int32_t)shared_blocks(a.own.n_splits, p.h_kv, sp.own_groups);
     // more than the CUs take at a time, with layers on top: all in one round of workgroups if the prefixes are
     const int64_t all = (int64_t)a.prefix_blocks + a.own_blocks, most = std::max<int64_t>(kSharedChip / p.n_layers, 1);
