@@ -803,14 +803,13 @@ class Codes:
 
     def c_struct(self, shape: Shape, pages: Optional[Pages], device) -> _CCodes:
         import torch
-        u8, rows = torch.uint8, _code_rows(shape, pages)
-        for name, t in (("codes.K", self.K), ("codes.V", self.V)):
-            if t.shape[-1] not in (shape.d, shape.d // 2):
-                raise ValueError("%s: rows of %d (8 bits) or %d bytes (4 bits) are wanted, got %d" % (name, shape.d, shape.d // 2, t.shape[-1]))
-        return _CCodes(self.k_bits, self.v_bits, _tensor("codes.K", self.K, u8, rows + self.K.shape[-1:], device),
-                       _tensor("codes.V", self.V, u8, rows + self.V.shape[-1:], device),
-                       _tensor("codes.K_scale", self.K_scale, u8, rows + (shape.d // 32,), device),
-                       _tensor("codes.V_scale", self.V_scale, u8, rows + (shape.d // 32,), device))
+        u8, rows, d = torch.uint8, _code_rows(shape, pages), shape.d
+        k, v, scales = self.K.shape[-1], self.V.shape[-1], rows + (d // 32,)
+        for name, n in (("codes.K", k), ("codes.V", v)):
+            if n != d and 2 * n != d:
+                raise ValueError("%s: rows of %d (8 bits) or %d bytes (4 bits) are wanted, got %d" % (name, d, d // 2, n))
+        return _CCodes(k // 16, v // 16, _tensor("codes.K", self.K, u8, rows + (k,), device), _tensor("codes.V", self.V, u8, rows + (v,), device),
+                       _tensor("codes.K_scale", self.K_scale, u8, scales, device), _tensor("codes.V_scale", self.V_scale, u8, scales, device))
 
 
 def _code_rows(shape: Shape, pages):
@@ -831,13 +830,13 @@ def alloc_codes(shape: Shape, k_bits: int = 8, v_bits: int = 8, pages: Optional[
 def _rows_of_codes(name, shape: Shape, pages, K, V, codes, first, stream):
     import torch
     dev, bf, i32 = _device_of(codes.K), torch.bfloat16, torch.int32
-    kept = (shape.n_layers, shape.TB, shape.h_kv, shape.d)
-    kv = lambda what: (_tensor("K" + what, K, bf, kept, dev), _tensor("V" + what, V, bf, kept, dev))
-    at = _tensor("first", first, i32, (shape.n_layers, shape.n_seq), dev)
-    _tensor("layer_budgets", shape.layer_budgets, i32, (shape.n_layers, shape.n_seq), dev)
-    c = ctypes.byref(codes.c_struct(shape, pages, dev))
-    args = (at,) + kv("") + (c,) if name.startswith("jq_quantize") else (at, c) + kv("_out")
-    _call(name, shape, pages, dev, stream, *args)
+    kept, per = (shape.n_layers, shape.TB, shape.h_kv, shape.d), (shape.n_layers, shape.n_seq)
+    at, c = _tensor("first", first, i32, per, dev), ctypes.byref(codes.c_struct(shape, pages, dev))
+    _tensor("layer_budgets", shape.layer_budgets, i32, per, dev)
+    if name.startswith("jq_quantize"):
+        _call(name, shape, pages, dev, stream, at, _tensor("K", K, bf, kept, dev), _tensor("V", V, bf, kept, dev), c)
+    else:
+        _call(name, shape, pages, dev, stream, at, c, _tensor("K_out", K, bf, kept, dev), _tensor("V_out", V, bf, kept, dev))
 
 
 def quantize(shape: Shape, K, V, codes: Codes, first=None, stream=None):
