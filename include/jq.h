@@ -504,8 +504,8 @@ typedef struct jq_codes {
  * row of the cache changes.  Per group of 32 dimensions x is the smallest integer for which 448 * 2^x (8 bits) or 6 * 2^x (4
  * bits) reaches the largest magnitude, at least -100, and values are rounded to the nearest code, ties to the even one; magnitudes
  * above 1.75 * 2^127 (8 bits) or 1.5 * 2^127 (4 bits) become that.  A group with a value that is not finite gets the scale byte
- * 255: all its values read back as NaN.  shape->window must be 0; pool_k, n_q, h_q and scale (beyond their checks) do not matter.
- * Paged: no page that is written may belong to two sequences. */
+ * 255: all its values read back as NaN.  shape->window must be 0; keep_first and keep_last are not used; pool_k, n_q, h_q and scale (beyond their checks) do not
+ * matter.  Paged: no page that is written may belong to two sequences. */
 int jq_quantize(const jq_shape* shape, const int32_t* first, const void* K, const void* V, const jq_codes* codes, void* stream);
 int jq_quantize_paged(const jq_shape* shape, const jq_pages* pages, const int32_t* first, const void* K, const void* V,
                       const jq_codes* codes, void* stream);

@@ -821,9 +821,12 @@ static int codes_impl(const jq_shape* shape, const jq_pages* pages, bool paged, 
                       const jq_codes* codes, void* stream) {
     Plan p;
     Codes c;
-    int rc = make_plan(shape, true, &p, false);
+    if (!shape) return JQ_ERR_NULL;
+    jq_shape of = *shape;
+    of.keep_first = of.keep_last = 0;  // nothing is selected: budgets are numbers of rows
+    if (of.window) return JQ_ERR_SHAPE;  // no queries here
+    int rc = make_plan(&of, true, &p, false);
     if (rc != JQ_OK) return rc;
-    if (p.window) return JQ_ERR_SHAPE;  // no queries here
     if (!codes_fit(p)) return JQ_ERR_UNSUPPORTED;
     if (paged && (rc = apply_pages(pages, &p)) != JQ_OK) return rc;
     if ((rc = check_codes(codes, &c)) != JQ_OK) return rc;

@@ -18,6 +18,7 @@ struct SharedArgs {
     OwnArgs own;
     int32_t prefix_blocks, own_blocks;  // shares of either sweep; a workgroup may take one of each
 };
+static_assert(sizeof(SharedArgs) <= 4096, "a kernel's arguments");
 
 // P: tiles of 16 query rows of a prefix that a workgroup takes, RT: of a sequence.
 template <class Rows, int P, int RT>

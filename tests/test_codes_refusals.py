@@ -75,6 +75,28 @@ def test_rows(name):
     assert call(name, sh=shape(n_layers=1, n_q=1, h_q=256, h_kv=256, seq_lens=[60000] * 128, budgets=[60000] * 128)) == UNSUPPORTED
 
 
+def test_what_a_selection_keeps_does_not_limit_rows():
+    """One new token a sequence with the shape of an eviction: refused for the address that is misaligned, not for its budgets."""
+    for name in ("quantize", "dequantize"):
+        assert call(name, sh=shape(budgets=[1, 1], keep_first=4, keep_last=32), k=K + 8) == UNSUPPORTED
+
+
+def test_a_workspace_serves_either_kind_of_cache():
+    """Sized by jq_attend_workspace_bytes: the call over codes, which shares the work out in its own way, goes on to the address that is
+    misaligned."""
+    import random
+    rng = random.Random(5)
+    for _ in range(400):
+        h_kv = rng.choice([1, 2, 3, 8, 16, 64])
+        sh = jq.Shape(n_layers=rng.choice([1, 1, 2, 7]), seq_lens=[int(2 ** rng.uniform(0, 14)) for _ in range(rng.choice([1, 1, 2, 7, 30, 128]))],
+                      n_q=rng.choice([1, 1, 2, 4, 9, 30]), h_q=h_kv * rng.choice([1, 2, 4, 5]), h_kv=h_kv)
+        for weights in (False, True):
+            if weights and sh.n_q * (sh.h_q // h_kv) > 128:
+                continue
+            need = jq.attend_workspace_bytes(sh, weights)
+            assert call("attend_quantized", sh=sh, q=Q + 8, w=W if weights else None, ws_bytes=need) == UNSUPPORTED, sh
+
+
 @pytest.mark.parametrize("bits", [(8, 8), (8, 4), (4, 4)])
 def test_nothing_may_overlap_what_is_written(bits):
     kb, vb = bits
