@@ -801,9 +801,9 @@ __device__ __forceinline__ void attend_few_rows(const Args& a, int bx, int layer
     if (KEEP) weigher.add(lse2, true);
 }
 
-template <class Rows, int RT, int MASK, bool KEEP>
-__global__ __launch_bounds__(64 * Rows::waves(RT, KEEP), Rows::least_waves(RT)) void jq_attend_kernel(AttendArgs a) {
-    attend_few_rows<Rows, RT, MASK, KEEP, Rows::waves(RT, KEEP)>(kernel_args<AttendArgs>(), (int)blockIdx.x, (int)blockIdx.y);
+template <class Rows, int RT, int MASK, bool KEEP, int WAVES>
+__global__ __launch_bounds__(64 * WAVES, Rows::least_waves(RT)) void jq_attend_kernel(AttendArgs a) {
+    attend_few_rows<Rows, RT, MASK, KEEP, WAVES>(kernel_args<AttendArgs>(), (int)blockIdx.x, (int)blockIdx.y);
 }
 
 // Many query rows (more than 32 a KV head).  A wave still holds 32 of them, but the eight waves of a workgroup share the keys: R waves
@@ -1138,17 +1138,17 @@ __global__ __launch_bounds__(Wide<R>::kThreads, 2) void jq_attend_wide_kernel(At
 
 // ---- launches ----------------------------------------------------------------------------------------------------------------
 
-template <class Rows, int RT, int MASK, bool KEEP>
+template <class Rows, int RT, int MASK, bool KEEP, int WAVES>
 static hipError_t launch_sweep(const AttendArgs& a, dim3 grid, hipStream_t st) {
-    constexpr int waves = Rows::waves(RT, KEEP), sums = waves * RT * kTileRows * (kOutStride * 4 + 8);
-    constexpr int most = sums + (KEEP ? kMostHeld + (waves - kAttendWaves) * 32 * kTileRows * RT * 4 : 0);  // (whole turns of all waves are held)
+    constexpr int sums = WAVES * RT * kTileRows * (kOutStride * 4 + 8);
+    constexpr int most = sums + (KEEP ? kMostHeld + (WAVES - kAttendWaves) * 32 * kTileRows * RT * 4 : 0);  // (whole turns of all waves are held)
     const int lds = sums + (KEEP ? a.rows * a.hold_keys * 4 : 0);
     if (most > 65536) {
         static std::atomic<uint64_t> done{0};
-        const hipError_t e = allow_dynamic_lds((const void*)jq_attend_kernel<Rows, RT, MASK, KEEP>, most, done);
+        const hipError_t e = allow_dynamic_lds((const void*)jq_attend_kernel<Rows, RT, MASK, KEEP, WAVES>, most, done);
         if (e != hipSuccess) return e;
     }
-    return launch_kernel(jq_attend_kernel<Rows, RT, MASK, KEEP>, grid, dim3(64 * waves), lds, st, nullptr, -1, a);
+    return launch_kernel(jq_attend_kernel<Rows, RT, MASK, KEEP, WAVES>, grid, dim3(64 * WAVES), lds, st, nullptr, -1, a);
 }
 
 template <class Rows, int R, int MASK, bool KEEP>
@@ -1163,10 +1163,13 @@ static hipError_t launch_wide(const AttendArgs& a, dim3 grid, hipStream_t st) {
 }
 
 template <class Rows, int MASK, bool KEEP>
-static hipError_t launch_rows(const AttendArgs& a, int row_tiles, dim3 grid, hipStream_t st) {
+static hipError_t launch_rows(const AttendArgs& a, int row_tiles, int waves, dim3 grid, hipStream_t st) {
+    constexpr int kWaves1 = Rows::waves(1, KEEP), kWaves2 = Rows::waves(2, KEEP);
     switch (row_tiles) {
-        case 1: return launch_sweep<Rows, 1, MASK, KEEP>(a, grid, st);
-        case 2: return launch_sweep<Rows, 2, MASK, KEEP>(a, grid, st);
+        case 1:
+            if (waves == kAttendWaves) return launch_sweep<Rows, 1, MASK, KEEP, kAttendWaves>(a, grid, st);
+            return launch_sweep<Rows, 1, MASK, KEEP, kWaves1>(a, grid, st);
+        case 2: return launch_sweep<Rows, 2, MASK, KEEP, kWaves2>(a, grid, st);
         case 4: return launch_wide<Rows, 2, MASK, KEEP>(a, grid, st);
         case 8: return launch_wide<Rows, 4, MASK, KEEP>(a, grid, st);
         default:  // more than 128 query rows: without weights
@@ -1177,11 +1180,11 @@ static hipError_t launch_rows(const AttendArgs& a, int row_tiles, dim3 grid, hip
 
 // The sweep of a call over caches of one kind.  (One new token sees every live row, its own among them: no mask either way.)
 template <class Rows>
-hipError_t launch_sweeps(const AttendArgs& a, int row_tiles, bool causal, dim3 grid, hipStream_t st) {
+hipError_t launch_sweeps(const AttendArgs& a, int row_tiles, int waves, bool causal, dim3 grid, hipStream_t st) {
     const bool weights = a.weights != nullptr;
-    if (a.seen) return launch_rows<Rows, kSeeTree, false>(a, row_tiles, grid, st);
-    if (causal) return weights ? launch_rows<Rows, kSeeCausal, true>(a, row_tiles, grid, st) : launch_rows<Rows, kSeeCausal, false>(a, row_tiles, grid, st);
-    return weights ? launch_rows<Rows, kSeeAll, true>(a, row_tiles, grid, st) : launch_rows<Rows, kSeeAll, false>(a, row_tiles, grid, st);
+    if (a.seen) return launch_rows<Rows, kSeeTree, false>(a, row_tiles, waves, grid, st);
+    if (causal) return weights ? launch_rows<Rows, kSeeCausal, true>(a, row_tiles, waves, grid, st) : launch_rows<Rows, kSeeCausal, false>(a, row_tiles, waves, grid, st);
+    return weights ? launch_rows<Rows, kSeeAll, true>(a, row_tiles, waves, grid, st) : launch_rows<Rows, kSeeAll, false>(a, row_tiles, waves, grid, st);
 }
 
 }  // namespace jq

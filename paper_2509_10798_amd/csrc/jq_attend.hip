@@ -5,9 +5,9 @@
 namespace jq {
 
 // (their kernels are compiled in files of their own)
-extern template hipError_t launch_sweeps<RowsCoded<8, 8>>(const AttendArgs&, int, bool, dim3, hipStream_t);
-extern template hipError_t launch_sweeps<RowsCoded<8, 4>>(const AttendArgs&, int, bool, dim3, hipStream_t);
-extern template hipError_t launch_sweeps<RowsCoded<4, 4>>(const AttendArgs&, int, bool, dim3, hipStream_t);
+extern template hipError_t launch_sweeps<RowsCoded<8, 8>>(const AttendArgs&, int, int, bool, dim3, hipStream_t);
+extern template hipError_t launch_sweeps<RowsCoded<8, 4>>(const AttendArgs&, int, int, bool, dim3, hipStream_t);
+extern template hipError_t launch_sweeps<RowsCoded<4, 4>>(const AttendArgs&, int, int, bool, dim3, hipStream_t);
 
 // A row's statistics over the ns shares of its sequence, a lane a share: (m, z) in every lane, and the lane's own factor (of share
 // `lane`; those of further shares are formed where they are needed).
@@ -170,6 +170,7 @@ static void plan_splits(const Plan& p, bool weights, int waves, int64_t step, At
         tiles = std::max(tiles, ((L + 31) / 32 + waves * ns[s] - 1) / (waves * ns[s]));  // of 32 keys, a wave
     }
     ap->waves = waves;
+    ap->most_rows = (int32_t)std::min<int64_t>(share * unit, INT32_MAX);
     ap->hold_keys = weights && row_tiles <= 2 ? (int32_t)(tiles * 32 * waves) : 0;
     // (without shares there is nothing to join, and the weights are the sweep's)
     ap->one_launch = row_tiles <= 2 && (most_ns == 1 || (p.rows <= kMostJoinRows && most_ns <= kMostJoined && most_ns * p.rows <= kMostSums &&
@@ -196,10 +197,15 @@ static void plan_attend(const Plan& p, bool weights, int waves, int64_t step, At
     ap->ws_bytes = ap->off_logits + (weights ? up((size_t)p.n_layers * p.h_kv * p.rows * ap->logit_T * sizeof(float)) : 0);
 }
 
+// Over codes a workgroup has eight waves (RowsCoded::waves says why), but four where its share is two tiles a wave of four or less: such a
+// call is its start and its join, which take longer with eight.  Us of the kernel, four / eight waves, 8 KV heads of 4 query rows in 8 bits:
+// one token over 1000 rows 9.7 / 11.2, 2000 10.4 / 11.4, 8 x 1024 11.7 / 12.4, 8192 (shares of 256) 8.4 / 8.5, 12288 (384) 10.2 / 9.6, 16384
+// (512) 12.2 / 10.5; 1000 rows of 2 heads with weights 11.1 / 13.5.
+constexpr int kShortShare = 256;
 void plan_attend(const Plan& p, bool weights, bool coded, AttendPlan* ap) {
     plan_attend(p, weights, kAttendWaves, 32 * kAttendWaves, ap);
     const int waves = coded ? RowsCoded<8, 8>::waves(ap->row_tiles, weights) : kAttendWaves;
-    if (waves == kAttendWaves) return;
+    if (waves == kAttendWaves || (ap->row_tiles == 1 && ap->most_rows <= kShortShare)) return;
     const size_t most = ap->ws_bytes;
     plan_attend(p, weights, waves, 32 * waves, ap);
     if (ap->ws_bytes > most) plan_attend(p, weights, waves, 32 * kAttendWaves, ap);  // (callers have one size for either kind of cache)
@@ -247,10 +253,10 @@ hipError_t launch_attend(const Plan& p, const AttendPlan& ap, const int32_t* len
     for (int s = 0; s <= p.n_seq; ++s) { a.cu_seq[s] = p.tab.cu_seq[s]; a.cu_split[s] = ap.cu_split[s]; }
     const dim3 grid((unsigned)sweep_groups(p, ap), (unsigned)p.n_layers);
     const bool causal = p.window && p.n_q > 1;
-    const hipError_t e = !codes            ? launch_sweeps<Rows16>(a, ap.row_tiles, causal, grid, st)
-                         : codes->k_bits == 4 ? launch_sweeps<RowsCoded<4, 4>>(a, ap.row_tiles, causal, grid, st)
-                         : codes->v_bits == 4 ? launch_sweeps<RowsCoded<8, 4>>(a, ap.row_tiles, causal, grid, st)
-                                              : launch_sweeps<RowsCoded<8, 8>>(a, ap.row_tiles, causal, grid, st);
+    const hipError_t e = !codes            ? launch_sweeps<Rows16>(a, ap.row_tiles, ap.waves, causal, grid, st)
+                         : codes->k_bits == 4 ? launch_sweeps<RowsCoded<4, 4>>(a, ap.row_tiles, ap.waves, causal, grid, st)
+                         : codes->v_bits == 4 ? launch_sweeps<RowsCoded<8, 4>>(a, ap.row_tiles, ap.waves, causal, grid, st)
+                                              : launch_sweeps<RowsCoded<8, 8>>(a, ap.row_tiles, ap.waves, causal, grid, st);
     if (e != hipSuccess) return e;
     const Finish f = finish_groups(p, ap, weights != nullptr);
     if (f.groups == 0) return e;

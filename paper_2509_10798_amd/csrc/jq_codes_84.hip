@@ -2,5 +2,5 @@
 #include "jq_codes.h"
 
 namespace jq {
-template hipError_t launch_sweeps<RowsCoded<8, 4>>(const AttendArgs&, int, bool, dim3, hipStream_t);
+template hipError_t launch_sweeps<RowsCoded<8, 4>>(const AttendArgs&, int, int, bool, dim3, hipStream_t);
 }  // namespace jq

@@ -356,6 +356,7 @@ struct AttendPlan {
     int32_t hold_keys;                  // rows of the cache whose logits a workgroup holds, with weights
     int32_t row_tiles, row_groups;      // tiles of 16 query rows a workgroup takes, workgroups over the same keys
     int32_t waves;                      // of a workgroup that takes one or two tiles
+    int32_t most_rows;                  // of the cache, a workgroup's share at most
     int32_t cu_split[JQ_MAX_SEQ + 1];   // workgroups that share a sequence (per layer, KV head and group of rows), summed up
     bool one_launch;                    // the workgroup that completes a sequence joins it (and weighs)
     int64_t logit_T;
