@@ -10,8 +10,8 @@ ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libjq.so")
 OBJ = os.path.join(PKG, "_build")
-# the eviction path is one translation unit (csrc/jq_lib.hip says why), the kernels of decoding on a pruned cache another; the
-# other .hip files are their parts
+# the eviction path is one translation unit (csrc/jq_lib.hip says why), the kernels of decoding on a pruned cache another, those over
+# codes one a format (they compile side by side); the other .hip files are their parts
 SOURCES = ["jq_lib.hip", "jq_decode.hip", "jq_codes.hip", "jq_codes_88.hip", "jq_codes_84.hip", "jq_codes_44.hip", "jq_shared.hip"]
 FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall",

@@ -20,6 +20,9 @@
 // is V transposed: lane l loads 16 bytes (d = 8 * (l % 16) .. + 7) of the rows 4 * (l / 16) + e, a wave's load covers whole rows, and
 // byte permutes inside the lane pair the rows up: no value passes through LDS, and no workgroup barrier stands in the sweep.
 // out comes out transposed too: lane l holds d = 32 * (l / 16) .. + 31 of query row l % 16, in line with m and z.
+//
+// The sweeps are templates of how a cache's rows lie and come into registers (Rows16 here, RowsCoded in jq_codes.h) and bodies that more
+// than one kernel has (jq_shared.hip).
 #pragma once
 #include <type_traits>
 

@@ -1,4 +1,4 @@
-// The eviction path of libjq.so is built from this ONE translation unit (decoding on a pruned cache is the other, jq_decode.hip).
+// The eviction path of libjq.so is built from this ONE translation unit (decoding on a pruned cache is in others: jq_decode.hip, jq_codes*.hip, jq_shared.hip).
 //
 // Why: the kernels of an eviction step over more than 32768 tokens (both passes over K in one, pooling, selection +
 // gather) run back to back, thousands of times, and the instruction cache of a compute-unit pair (64 KB) keeps its
