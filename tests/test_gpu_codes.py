@@ -524,3 +524,35 @@ def test_calls_on_another_stream():
     torch.cuda.synchronize()
     for r in got:
         assert all(torch.equal(a, b) for a, b in zip(r, ref + back))
+
+
+def test_calls_of_several_host_threads():
+    import threading
+    import torch
+    rng, Q, codes, rows, cu, live = make(43, 1, [5000, 77], 16, 4, 1, None, (8, 4))
+    shapes = [jq.Shape(n_layers=1, seq_lens=[5000, 77], n_q=1, h_q=16, h_kv=4, budgets=[600, 70]) for _ in range(4)]
+    c, _ = on_device(codes, [5000, 77], 0, 0)
+    q = to_dev_bf16(Q)
+    ref = jq.attend_quantized(shapes[0], q, c) + jq.dequantize(shapes[0], c)
+    torch.cuda.synchronize()
+    got = [[] for _ in shapes]
+
+    def work(i):
+        side = torch.cuda.Stream()
+        for _ in range(10):
+            got[i].append(jq.attend_quantized(shapes[i], q, c, stream=side) + jq.dequantize(shapes[i], c, stream=side))
+        side.synchronize()
+    threads = [threading.Thread(target=work, args=(i,)) for i in range(len(shapes))]
+    [t.start() for t in threads]
+    [t.join() for t in threads]
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for g in got for r in g for a, b in zip(r, ref)) and all(len(g) == 10 for g in got)
+
+
+@pytest.mark.parametrize("bits", FORMATS)
+@pytest.mark.parametrize("n_q", [1, 5])
+def test_shares_from_one_tile_a_wave_to_many(bits, n_q):
+    """Workgroups of four and of eight waves, one launch and two, lengths that end inside a tile, inside a turn and at its end."""
+    for L in (255, 1279, 3000, 8191, 8192 + 257, 20011):
+        attend(L, 1, [L], 8, 2, n_q, bits=bits, mode="causal" if n_q > 1 else "all", weigh=True)
+    attend(7, 1, [9000, 300, 5000], 4, 1, n_q, bits=bits, lens=np.array([[8997, 0, 31]], np.int32), weigh=True, page=32)
