@@ -399,7 +399,7 @@ int jq_evict_traced(const jq_shape* shape, const void* Q, const void* K, const v
  * (2^-16 of p is lost), with more than 64 query rows per KV head in one (2^-8; out's own rounding is 2^-8 too).  A
  * value of V that is not finite makes the outputs of its own dimension infinite or NaN, of the queries that see its
  * row; everything else is as if it were finite.  `ws` (DEVICE, 16-byte aligned) must hold jq_attend_workspace_bytes
- * (`with_weights`: 0, or 1 for calls that pass weights). shape->budgets is not used. */
+ * (`with_weights`: 0, or 1 for calls that pass weights; enough for a cache of codes too). shape->budgets is not used. */
 int jq_attend_workspace_bytes(const jq_shape* shape, int32_t with_weights, size_t* bytes);
 int jq_attend(const jq_shape* shape, const int32_t* lens, const void* Q, const void* K, const void* V, void* out,
               float* lse, float* weights, void* ws, size_t ws_bytes, void* stream);

@@ -728,6 +728,8 @@ int jq_attend_workspace_bytes(const jq_shape* shape, int32_t with_weights, size_
     const int rc = attend_plan(shape, with_weights != 0, &p, &ap);
     if (rc != JQ_OK) return rc;
     *bytes = ap.ws_bytes;
+    // over codes the work is shared out in another way; what it would refuse asks for nothing
+    if (attend_plan(shape, with_weights != 0, &p, &ap, true) == JQ_OK) *bytes = std::max(*bytes, ap.ws_bytes);
     return JQ_OK;
 }
 

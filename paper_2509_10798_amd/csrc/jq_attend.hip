@@ -106,6 +106,9 @@ __global__ __launch_bounds__(kAttendThreads) void jq_attend_finish_kernel(Attend
 // many query rows have to be joined afterwards.  In rows of the cache, fitted to (whole sequences / as chosen) one token, 40 x 4099 rows
 // 158 / 133 us, 36 x 2000 78 / 65, 64 ragged sequences of 80 to 7000 203 / 128; trees of 20 over those 257 / 161, 12 x 40 x 4099 189 /
 // 177, and as they are 25 x 40 x 2099 103 (125 in smaller shares), 64 x 40 x 1099 96 (133).
+// Over codes smaller shares are also looked for where whole sequences would do, for ragged ones (us, one round / up to four, 8 KV heads: 31
+// sequences of 306 to 14833 rows, 8 bits, two causal tokens 100 / 63, of 313 to 15234 rows, 31 tokens 240 / 108; 4 bits, 344 to
+// 10543 rows 59 / 38).
 constexpr int kChip = 256, kRounds = 4;
 constexpr int kStart = 320, kWideStart = 1500;
 // What a sequence's last workgroup joins, and weighs, instead of a second launch.  Its time grows with the shares, whose statistics and
@@ -123,7 +126,7 @@ constexpr int kMostJoined = 20;          // shares (a lane each in the join)
 constexpr int kMostSums = 64;            // shares times query rows
 constexpr int64_t kMostWeighed = 8192;   // logits of a (sequence, head)
 // `waves` of a workgroup that takes 32 or fewer query rows; shares of multiples of `step` rows of the cache.
-static void plan_splits(const Plan& p, bool weights, int waves, int64_t step, AttendPlan* ap) {
+static void plan_splits(const Plan& p, bool weights, bool coded, int waves, int64_t step, AttendPlan* ap) {
     const int row_tiles = (p.rows + kTileRows - 1) / kTileRows;
     ap->row_tiles = row_tiles <= 1 ? 1 : row_tiles <= 2 ? 2 : row_tiles <= 4 ? 4 : row_tiles <= 8 ? 8 : 16;
     ap->row_groups = (row_tiles + ap->row_tiles - 1) / ap->row_tiles;
@@ -139,8 +142,8 @@ static void plan_splits(const Plan& p, bool weights, int waves, int64_t step, At
     int64_t most = (p.T + unit - 1) / unit;
     if (weights && row_tiles <= 2) most = std::min(most, (int64_t)kMostHeld / (p.rows * 4) / unit);  // its logits have to fit the LDS that is theirs
     int64_t share = most, best = INT64_MAX, slots = 0;
-    const int64_t start = ap->row_tiles > 2 ? kWideStart : kStart;
-    for (int rounds = 1; rounds <= (p.n_seq * heads > kChip ? kRounds : 1); ++rounds) {
+    const int64_t start = ap->row_tiles > 2 ? kWideStart : (coded ? 2 : 1) * kStart;  // (rows of codes take half as long)
+    for (int rounds = 1; rounds <= (p.n_seq * heads > kChip || (coded && p.n_seq > 1) ? kRounds : 1); ++rounds) {
         int64_t lo = 1, hi = most;
         while (lo < hi) {
             const int64_t mid = (lo + hi) / 2;
@@ -185,8 +188,8 @@ static uint64_t next_tag() {
     return (x ? x : 1) << 24;
 }
 
-static void plan_attend(const Plan& p, bool weights, int waves, int64_t step, AttendPlan* ap) {
-    plan_splits(p, weights, waves, step, ap);
+static void plan_attend(const Plan& p, bool weights, bool coded, int waves, int64_t step, AttendPlan* ap) {
+    plan_splits(p, weights, coded, waves, step, ap);
     const size_t parts = (size_t)p.n_layers * ap->cu_split[p.n_seq] * p.h_kv * p.rows;
     auto up = [](size_t x) { return (x + 255) / 256 * 256; };
     ap->logit_T = 32 * (p.T / 32 + p.n_seq);
@@ -203,12 +206,10 @@ static void plan_attend(const Plan& p, bool weights, int waves, int64_t step, At
 // (512) 12.2 / 10.5; 1000 rows of 2 heads with weights 11.1 / 13.5.
 constexpr int kShortShare = 256;
 void plan_attend(const Plan& p, bool weights, bool coded, AttendPlan* ap) {
-    plan_attend(p, weights, kAttendWaves, 32 * kAttendWaves, ap);
+    plan_attend(p, weights, coded, kAttendWaves, 32 * kAttendWaves, ap);
     const int waves = coded ? RowsCoded<8, 8>::waves(ap->row_tiles, weights) : kAttendWaves;
     if (waves == kAttendWaves || (ap->row_tiles == 1 && ap->most_rows <= kShortShare)) return;
-    const size_t most = ap->ws_bytes;
-    plan_attend(p, weights, waves, 32 * waves, ap);
-    if (ap->ws_bytes > most) plan_attend(p, weights, waves, 32 * kAttendWaves, ap);  // (callers have one size for either kind of cache)
+    plan_attend(p, weights, coded, waves, 32 * waves, ap);
 }
 
 // Workgroups of a layer's sweep, and of the launch behind it: those that join, blocks of weights a (sequence, head).

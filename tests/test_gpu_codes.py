@@ -312,6 +312,14 @@ def test_many_tiles_a_wave(bits, n_q):
         attend(L, 1, [L], 512, 256, n_q // 2 + 1, bits=bits, weigh=True)
 
 
+@pytest.mark.parametrize("n_q", [1, 16])
+def test_ragged_sequences_in_shares_of_several_rounds(n_q):
+    """248 (sequence, head) pairs, one of them far longer than the others."""
+    caps = [40 + (53 * i) % 400 for i in range(30)] + [6000]
+    attend(70, 1, caps, 8, 8, n_q, weigh=True, bits=(8, 8), lens=np.array([[max(c - i, n_q) for i, c in enumerate(caps)]], np.int32), mode="causal" if n_q > 1 else "all")
+    attend(71, 1, caps, 8, 8, 3 * n_q, bits=(4, 4), page=64, mode="tree")
+
+
 def test_more_sequences_than_the_chip_takes_at_a_time():
     caps = [5, 2000, 37, 700, 1, 333] * 15
     attend(24, 1, caps, 3, 3, 1, weigh=True, bits=(8, 4), page=32)
