@@ -317,7 +317,7 @@ def test_ragged_sequences_in_shares_of_several_rounds(n_q):
     """248 (sequence, head) pairs, one of them far longer than the others."""
     caps = [40 + (53 * i) % 400 for i in range(30)] + [6000]
     attend(70, 1, caps, 8, 8, n_q, weigh=True, bits=(8, 8), lens=np.array([[max(c - i, n_q) for i, c in enumerate(caps)]], np.int32), mode="causal" if n_q > 1 else "all")
-    attend(71, 1, caps, 8, 8, 3 * n_q, bits=(4, 4), page=64, mode="tree")
+    attend(71, 1, [c + 3 * n_q for c in caps], 8, 8, 3 * n_q, bits=(4, 4), page=64, mode="tree")  # (room for the drafted tokens' rows)
 
 
 def test_more_sequences_than_the_chip_takes_at_a_time():
