@@ -503,8 +503,8 @@ typedef struct jq_codes {
 /* Rows K, V (DEVICE bf16 [n_layers, TB, h_kv, d], TB = sum of budgets: the layout of a pruned cache that jq_evict leaves, or,
  * with budgets of 1, of one new token a sequence) written into a cache of codes: row b of sequence s, b < budgets[s] (or
  * layer_budgets[l, s], if that is smaller; none where it is 0 or less), becomes row first[l, s] + b of the sequence (first: DEVICE
- * int32 [n_layers, n_seq], its live rows before the call; NULL: 0).  Rows that fall outside 0 .. L_s - 1 are not written; no other
- * row of the cache changes.  Per group of 32 dimensions x is the smallest integer for which 448 * 2^x (8 bits) or 6 * 2^x (4
+ * int32 [n_layers, n_seq], its live rows before the call; NULL: 0).  Rows that fall outside 0 .. L_s - 1, or on a page whose
+ * block-table entry lies outside 0 .. n_pages - 1 (it is not clamped here), are not written; no other row of the cache changes.  Per group of 32 dimensions x is the smallest integer for which 448 * 2^x (8 bits) or 6 * 2^x (4
  * bits) reaches the largest magnitude, at least -100, and values are rounded to the nearest code, ties to the even one; magnitudes
  * above 1.75 * 2^127 (8 bits) or 1.5 * 2^127 (4 bits) become that.  A group with a value that is not finite gets the scale byte
  * 255: all its values read back as NaN.  shape->window must be 0; keep_first and keep_last are not used; pool_k, n_q, h_q and scale (beyond their checks) do not
@@ -515,7 +515,7 @@ int jq_quantize_paged(const jq_shape* shape, const jq_pages* pages, const int32_
 
 /* The reverse: rows first[l, s] .. first[l, s] + budgets[s] - 1 of every sequence, as the bf16 values that their codes stand for
  * (exactly: a code has at most four significant bits).  Rows of K_out and V_out (DEVICE bf16 [n_layers, TB, h_kv, d]) that have no
- * row in the cache are left as they were. */
+ * row in the cache, or none that jq_quantize_paged would write, are left as they were. */
 int jq_dequantize(const jq_shape* shape, const int32_t* first, const jq_codes* codes, void* K_out, void* V_out, void* stream);
 int jq_dequantize_paged(const jq_shape* shape, const jq_pages* pages, const int32_t* first, const jq_codes* codes, void* K_out,
                         void* V_out, void* stream);

@@ -848,7 +848,8 @@ def quantize(shape: Shape, K, V, codes: Codes, first=None, stream=None):
 
 
 def quantize_paged(shape: Shape, pages: Pages, K, V, codes: Codes, first=None, stream=None):
-    """quantize() into a paged cache of codes."""
+    """quantize() into a paged cache of codes.  Rows on a page that the block table does not name (an entry outside the pool) are not
+    written."""
     _rows_of_codes("jq_quantize_paged", shape, pages, K, V, codes, first, stream)
     return codes
 

@@ -56,7 +56,8 @@ struct CodeRows {
                 at[i] = ((int64_t)layer * a.h_kv + g) * a.T + a.tab.cu_seq[s] + pos;
             } else {
                 const int32_t e = a.pm.block_table[(int64_t)s * a.pm.max_pages + (pos >> a.pm.page_shift)];
-                const int64_t page = (int64_t)layer * a.pm.n_pages + clamp_page(e, a.pm.n_pages);
+                if ((uint32_t)e >= (uint32_t)a.pm.n_pages) continue;  // no page: clamped, the row would go over somebody's
+                const int64_t page = (int64_t)layer * a.pm.n_pages + e;
                 at[i] = ((page * a.h_kv + g) << a.pm.page_shift) + (pos & ((1 << a.pm.page_shift) - 1));
             }
         }

@@ -564,3 +564,40 @@ def test_shares_from_one_tile_a_wave_to_many(bits, n_q):
     for L in (255, 1279, 3000, 8191, 8192 + 257, 20011):
         attend(L, 1, [L], 8, 2, n_q, bits=bits, mode="causal" if n_q > 1 else "all", weigh=True)
     attend(7, 1, [9000, 300, 5000], 4, 1, n_q, bits=bits, lens=np.array([[8997, 0, 31]], np.int32), weigh=True, page=32)
+
+
+@pytest.mark.parametrize("bits", FORMATS)
+@pytest.mark.parametrize("below,beyond", [(-1, 9), (-2 ** 31, 2 ** 31 - 1)])
+def test_rows_whose_page_is_not_handed_out(bits, below, beyond):
+    """Rows within a sequence's room whose page the block table does not name yet: neither written, over whoever has the first or the last
+    page of the pool, nor read."""
+    import torch
+    assert torch.cuda.is_available(), "this test needs the GPU"
+    nl, h, page, n, caps, buds, first = 2, 3, 32, 9, [96, 64, 96], [40, 10, 30], [[20, 0, 60], [30, 3, 64]]
+    table = np.array([[3, below, 8], [5, 0, -1], [6, 4, beyond]], np.int32)   # (rows of pages 0 and 8 are nobody's to write in this call)
+    rng = np.random.default_rng(70)
+    rows = [bf16(rng, nl, sum(buds), h, 128) for _ in range(2)]
+    sh = jq.Shape(n_layers=nl, seq_lens=caps, n_q=1, h_q=h, h_kv=h, pool_k=1, budgets=buds)
+    pages, f = jq.Pages(page, n, dev_i32(table)), dev_i32(first)
+    codes = filled(sh, bits, pages)
+    outs = [torch.full((nl, sum(buds), h, 128), 7.0, dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    print("not handed out", bits, below, beyond, flush=True)
+    jq.quantize_paged(sh, pages, *(to_dev_bf16(x) for x in rows), codes, first=f)
+    jq.dequantize_paged(sh, pages, codes, first=f, K_out=outs[0], V_out=outs[1])
+    torch.cuda.synchronize()
+    got = host(codes)
+    for x, out, b, g, gs in zip(rows, outs, bits, got[:2], got[2:]):
+        c, scales = encode(x, b)
+        ref = decode(c, scales, b)
+        want, want_s, want_out = (np.full(y.shape, v, y.dtype) for y, v in ((g, OLD), (gs, OLD), (ref, 7.0)))
+        for l in range(nl):
+            i = 0
+            for s in range(3):
+                for at in range(first[l][s], first[l][s] + buds[s]):
+                    if at < caps[s] and 0 <= table[s, at // page] < n:
+                        want[l, table[s, at // page], :, at % page], want_s[l, table[s, at // page], :, at % page] = c[l, i], scales[l, i]
+                        want_out[l, i] = ref[l, i]
+                    i += 1
+        np.testing.assert_array_equal(gs, want_s)
+        np.testing.assert_array_equal(g, want)
+        np.testing.assert_array_equal(f64(from_dev_bf16(out)), want_out)
