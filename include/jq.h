@@ -464,9 +464,8 @@ int jq_replace_lightest_paged(const jq_shape* shape, const jq_pages* pages, cons
  * room for cu_rows[p+1] - cu_rows[p] rows, of which lens[l, p] are live, and lie in K_prefix, V_prefix (DEVICE bf16
  * [n_layers, cu_rows[n_prefix], h_kv, d]); a sequence that shares none is the only one to continue a prefix of its own, which may
  * have no live rows.  Paged: prefixes and sequences lie in the same pools, each behind a block table of their own.  Conditions,
- * accuracy and values of V that are not finite as for jq_attend, with the query rows of all sequences that continue the prefix
- * with most of them for those of one KV head: if these are more than 64, the rows of every prefix of the call are multiplied by p
- * in one bf16 part (2^-8 of p); `ws` must hold jq_attend_shared_workspace_bytes. */
+ * accuracy and values of V that are not finite as for jq_attend of up to 64 query rows, however many meet a prefix: V is multiplied
+ * by p in two bf16 parts (2^-16 of p is lost).  `ws` must hold jq_attend_shared_workspace_bytes. */
 typedef struct jq_prefixes {
     int32_t n_prefix;             /* 1..n_seq                                                           */
     const int32_t* cu_members;    /* HOST [n_prefix+1]; 0 first, strictly increasing, n_seq last        */

@@ -847,6 +847,8 @@ __device__ __forceinline__ void attend_many_rows(const Args& a, int bx, int laye
     using W = Wide<R>;
     constexpr int KW = W::KW;
     constexpr bool kParts = Args::kShare != 0;
+    // Shared prefixes: most of the query rows are other sequences', and a sequence's outputs do not lose a part to their number.
+    constexpr bool kExact = W::kExact || kParts;
     uint8_t* marked = (uint8_t*)wide_lds + W::kFlags;  // [kWaves]: the wave has cleared values of V, or has sums that are not finite
     bool was_cleared = false;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
@@ -1004,7 +1006,7 @@ __device__ __forceinline__ void attend_many_rows(const Args& a, int bx, int laye
                         const float y = __builtin_amdgcn_exp2f(__builtin_fmaf(x[r][i][e], a.scale2, -mm));
                         sum[r] += y;
                         p[r][4 * i + e] = (__bf16)y;
-                        if (W::kExact) rest[r][4 * i + e] = (__bf16)(y - (float)p[r][4 * i + e]);
+                        if (kExact) rest[r][4 * i + e] = (__bf16)(y - (float)p[r][4 * i + e]);
                     }
             }
         };
@@ -1036,7 +1038,7 @@ __device__ __forceinline__ void attend_many_rows(const Args& a, int bx, int laye
             const bf16x8 vt = __builtin_bit_cast(bf16x8, __builtin_shufflevector(v[d][0], v[d][1], 0, 1, 2, 3, 4, 5, 6, 7));
 #pragma unroll
             for (int r = 0; r < 2; ++r) o[r][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vt, p[r], o[r][d], 0, 0, 0);
-            if (W::kExact) {
+            if (kExact) {
 #pragma unroll
                 for (int r = 0; r < 2; ++r) o[r][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vt, rest[r], o[r][d], 0, 0, 0);
             }

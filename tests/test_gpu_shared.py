@@ -352,3 +352,25 @@ def test_several_groups_of_query_rows_beside_few(h_kv, page):
     members = [120, 5, 3]
     run(61, 2, [1300, 40, 900], members, caps, 4 * h_kv, h_kv, n_q=1, page=page)
     run(62, 1, [500, 1300], [9, 1], [30 + i for i in range(10)], 4 * h_kv, h_kv, n_q=17, causal=True, page=page)
+
+
+@pytest.mark.parametrize("room", [16, 2048, 30000])    # (how rows and keys are shared out goes by the room, not by what is live)
+@pytest.mark.parametrize("members,n_q", [([17], 1), ([32], 1), ([33], 1), ([64], 1), ([12, 5, 1], 4), ([40, 1], 1), ([1], 20), ([2, 1], 17)])
+def test_probabilities_are_two_parts_whatever_the_number_of_query_rows(members, n_q, room):
+    """Sixteen rows of a prefix, so that what a second bf16 part adds to out (2^-8 p without it) stands out against the other roundings: bounds of
+    two parts, 2^-16 p, for every sequence, those alone on a prefix beside a crowded one among them."""
+    import torch
+    n, G = sum(members), 4
+    c = Case(70 + n_q, 1, [room] * len(members), members, [n_q + 2] * n, 8, 2, n_q=n_q, lens=np.array([[i % 3 for i in range(n)]], np.int32),
+             prefix_lens=np.full((1, len(members)), 16, np.int32), peak=0.5)
+    out, lse = (x.cpu() for x in c.call())
+    out = f64(from_dev_bf16(out))
+    for s in range(n):
+        for g in range(2):
+            k, v, see = c.rows_of(0, s, g)
+            q = f64(c.Q[0, s, :, g * G:(g + 1) * G]).reshape(n_q * G, 128)
+            o, e = out[0, s, :, g * G:(g + 1) * G].reshape(-1, 128), lse[0, s, :, g * G:(g + 1) * G].reshape(-1).double().numpy()
+            for r in range(0, n_q * G, 64):
+                ro, rl, _, to, tl, _ = attend_ref(q[r:r + 64], k, v, see[r:r + 64], 128 ** -0.5)   # (its bounds for up to 64 rows)
+                assert (np.abs(o[r:r + 64] - ro) <= to).all(), "sequence %d: out off by %g of its bound" % (s, (np.abs(o[r:r + 64] - ro) / to).max())
+                assert (np.abs(e[r:r + 64] - rl) <= tl).all(), s
