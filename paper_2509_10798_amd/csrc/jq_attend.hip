@@ -200,14 +200,15 @@ static void plan_attend(const Plan& p, bool weights, bool coded, int waves, int6
     ap->ws_bytes = ap->off_logits + (weights ? up((size_t)p.n_layers * p.h_kv * p.rows * ap->logit_T * sizeof(float)) : 0);
 }
 
-// Over codes a workgroup has eight waves (RowsCoded::waves says why), but four where its share is two tiles a wave of four or less: such a
-// call is its start and its join, which take longer with eight.  Us of the kernel, four / eight waves, 8 KV heads of 4 query rows in 8 bits:
-// one token over 1000 rows 9.7 / 11.2, 2000 10.4 / 11.4, 8 x 1024 11.7 / 12.4, 8192 (shares of 256) 8.4 / 8.5, 12288 (384) 10.2 / 9.6, 16384
-// (512) 12.2 / 10.5; 1000 rows of 2 heads with weights 11.1 / 13.5.
+// Over codes a workgroup that takes 32 or fewer query rows has eight waves (RowsCoded::waves says why), but four where it takes 16 or fewer
+// and its share is two tiles a wave of four or less: such a call is its start and its join, which take longer with eight.  Us of the kernel,
+// four / eight waves, 8 KV heads of 4 query rows in 8 bits: one token over 1000 rows 9.7 / 11.2, 2000 10.4 / 11.4, 8 x 1024 11.7 / 12.4, 8192
+// (shares of 256) 8.4 / 8.5, 12288 (384) 10.2 / 9.6, 16384 (512) 12.2 / 10.5; 1000 rows of 2 heads with weights 11.1 / 13.5.  (The wide sweeps
+// have eight waves whatever the cache, over 128 or 64 keys together: Wide.)
 constexpr int kShortShare = 256;
 void plan_attend(const Plan& p, bool weights, bool coded, AttendPlan* ap) {
     plan_attend(p, weights, coded, kAttendWaves, 32 * kAttendWaves, ap);
-    const int waves = coded ? RowsCoded<8, 8>::waves(ap->row_tiles, weights) : kAttendWaves;
+    const int waves = coded && ap->row_tiles <= 2 ? RowsCoded<8, 8>::waves(ap->row_tiles, weights) : kAttendWaves;
     if (waves == kAttendWaves || (ap->row_tiles == 1 && ap->most_rows <= kShortShare)) return;
     plan_attend(p, weights, coded, waves, 32 * waves, ap);
 }

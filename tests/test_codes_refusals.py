@@ -153,3 +153,26 @@ def test_the_binding_checks_tensors():
     for f in (jq.attend_tree_quantized,):
         with pytest.raises(jq.JQError):
             f(sh, None, rows, c)
+
+
+def _parts(sh, coded):
+    """Shares times sequences that a call plans for, out of the bytes of workspace that it asks for: 520 a query row, head and share."""
+    lo, hi = 0, 1 << 40
+    while lo < hi:
+        mid = (lo + hi) // 2
+        if coded:
+            rc = call("attend_quantized", sh=sh, q=Q + 8, w=None, ws_bytes=mid)
+        else:
+            rc = jq.lib().jq_attend(ctypes.byref(sh.c_struct()), FIRST, Q + 8, K, V, OUT, LSE, None, WS, mid, None)
+        assert rc in (WORKSPACE, UNSUPPORTED)   # (too small, or gone on to the address that is misaligned)
+        lo, hi = (mid + 1, hi) if rc == WORKSPACE else (lo, mid)
+    return lo // (520 * sh.n_layers * sh.n_q * sh.h_q)
+
+
+@pytest.mark.parametrize("rows", [33, 36, 48, 64])
+@pytest.mark.parametrize("L", [129, 1000, 4096, 9000, 40000])
+def test_shares_of_a_wide_sweep_do_not_depend_on_the_cache(rows, L):
+    """33 to 64 query rows a KV head take the keys 128 at a time, out of codes as out of bf16: as many workgroups as there are such stages, up
+    to one a CU."""
+    sh = jq.Shape(n_layers=1, seq_lens=[L], n_q=rows, h_q=8, h_kv=8)
+    assert _parts(sh, True) == _parts(sh, False) == -(-L // (128 * max(1, -(-L // (128 * 32)))))
