@@ -38,7 +38,6 @@ typedef uint32_t au32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kAttendWaves = 4;
 constexpr int kAttendThreads = 64 * kAttendWaves;
-constexpr int kTileRows = 16;   // query rows of one MFMA tile
 constexpr int kOutStride = kHeadDim + 4;  // floats a row of partial output takes in LDS: rows of 128 would meet in the same banks
 constexpr int kMostJoinRows = 8;  // query rows whose shares the last workgroup of a sequence joins
 constexpr int kMostHeld = 65536;  // bytes of logits that a workgroup holds in LDS
@@ -72,7 +71,7 @@ struct AttendArgs {
 
 // Sequences that continue shared prefixes (jq_shared.hip): a sweep over the prefixes, whose query rows are those of all the sequences
 // that continue one, and a sweep over the sequences' own rows.  Both always leave parts.
-struct PrefixArgs : AttendArgs {  // n_seq, lens, cu_seq: of prefixes; cu_split: in place of splits, eighths of their workgroups
+struct PrefixArgs : AttendArgs {  // n_seq, lens, cu_seq: of prefixes; cu_split: in place of splits, their workgroups
     static constexpr int kShare = 1;
     int32_t cu_member[JQ_MAX_SEQ + 1];  // sequences that continue a prefix
     int32_t cu_part[JQ_MAX_SEQ + 1];    // parts of a prefix: splits times query rows, of each layer and KV head
@@ -138,16 +137,21 @@ __device__ __forceinline__ KeyShare key_share_of(const AttendArgs& a, int bx, in
 // Prefixes have as many groups as their own rows ask for (`rows` each): with as many as the largest, workgroups that had nothing to do
 // stood between the others, and some CUs were left two of these (three prefixes with 192, 80 and 16 query rows 92 us for 64).
 __device__ __forceinline__ KeyShare key_share_of(const PrefixArgs& a, int bx, int rows, int lane) {
-    int s = 0, ns = a.n_splits, per = 8 * a.row_groups;  // of one prefix
+    int s = 0, ns = a.n_splits, groups = a.row_groups;  // of one prefix
     if (a.n_seq > 1) {
-        s = seq_of_split(a, bx >> 3, lane);
+        s = seq_of_split(a, bx, lane);
         const int mine_rows = (a.cu_member[s + 1] - a.cu_member[s]) * a.n_q * a.group;
         ns = (a.cu_part[s + 1] - a.cu_part[s]) / mine_rows;
-        per = 8 * ((mine_rows + rows - 1) / rows);
+        groups = (mine_rows + rows - 1) / rows;
     }
-    const int at = bx - 8 * a.cu_split[s];
-    const int u = at / per * 8 + (at & 7), mine = u / a.h_kv;
-    return KeyShare{s, 0, ns, mine, u - mine * a.h_kv, (at % per) >> 3, u >= ns * a.h_kv};
+    const UnitAt at = unit_at(bx - a.cu_split[s], ns * a.h_kv, groups);
+    const int mine = at.unit / a.h_kv;
+    return KeyShare{s, 0, ns, mine, at.unit - mine * a.h_kv, at.group, false};
+}
+__device__ __forceinline__ KeyShare key_share_of(const OwnArgs& a, int bx, int, int lane) {
+    const UnitAt at = unit_at(bx, a.units, a.row_groups);
+    const int split = at.unit / a.h_kv, s = seq_of_split(a, split, lane);
+    return KeyShare{s, split, a.cu_split[s + 1] - a.cu_split[s], split - a.cu_split[s], at.unit - split * a.h_kv, at.group, false};
 }
 
 // log2 of a sum: v_log_f32 rounds towards zero and is off by more the larger its result, so it only sees the mantissa.

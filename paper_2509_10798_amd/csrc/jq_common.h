@@ -8,6 +8,7 @@
 
 #include <atomic>
 
+#include "jq_shares.h"
 #include "jq_sweep.h"
 
 namespace jq {
@@ -372,19 +373,7 @@ struct Codes {
 };
 hipError_t launch_attend(const Plan& p, const AttendPlan& ap, const int32_t* lens, const uint32_t* seen, const void* Q, const void* K, const void* V,
                          void* out, float* lse, float* weights, char* ws, hipStream_t st, const Codes* codes = nullptr);
-// Sequences that continue shared prefixes (jq_shared.hip); `pp`: the plan of the prefixes.
-struct SharedPlan {
-    int32_t prefix_tiles, own_tiles, own_groups;  // tiles of 16 query rows a workgroup takes, workgroups over the same keys
-    int32_t first_groups, first_splits;           // of the first prefix
-    int32_t cu_split[JQ_MAX_SEQ + 1];             // eighths of a prefix's workgroups (of a layer), summed up
-    int32_t own_split[JQ_MAX_SEQ + 1];            // workgroups that share a sequence, summed up
-    int32_t cu_part[JQ_MAX_SEQ + 1];                              // splits times query rows of the prefixes, summed up
-    bool fits;                                                    // every launch stays below 2^32 threads
-    size_t off_prefix_stats, off_prefix_part, off_own_stats, off_own_part, ws_bytes;
-};
-// Workgroups of a sweep; eight heads or shares side by side lie on eight XCDs, groups of query rows over the same keys on one.
-inline int64_t shared_blocks(int64_t splits, int h_kv, int groups) { return (splits * h_kv + 7) / 8 * 8 * groups; }
-void plan_shared(const Plan& p, const Plan& pp, const int32_t* cu_members, SharedPlan* sp);
+// Sequences that continue shared prefixes (jq_shared.hip, jq_shares.h); `pp`: the plan of the prefixes.
 hipError_t launch_attend_shared(const Plan& p, const Plan& pp, const SharedPlan& sp, const int32_t* cu_members, const int32_t* lens, const int32_t* prefix_lens,
                                 const void* Q, const void* K_prefix, const void* V_prefix, const void* K, const void* V, void* out, float* lse, char* ws,
                                 hipStream_t st);

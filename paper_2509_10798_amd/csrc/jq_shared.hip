@@ -14,14 +14,13 @@
 
 namespace jq {
 
-constexpr int kSharedWaves = 8, kSharedThreads = 64 * kSharedWaves;
-
 struct SharedArgs {
     PrefixArgs prefix;
     OwnArgs own;
     int32_t prefix_blocks, own_blocks;  // shares of either sweep; a workgroup may take one of each
 };
 static_assert(sizeof(SharedArgs) <= 4096, "a kernel's arguments");
+static_assert(kSharedJoinThreads == kAttendThreads, "what the plan counts");
 
 // P: tiles of 16 query rows of a prefix that a workgroup takes, RT: of a sequence.
 template <class Rows, int P, int RT>
@@ -32,8 +31,7 @@ __global__ __launch_bounds__(kSharedThreads, 2) void jq_attend_shared_kernel(Sha
         if constexpr (P <= 2) attend_few_rows<Rows, P, kSeeAll, false, kSharedWaves>(a.prefix, bx, (int)blockIdx.y);
         else attend_many_rows<Rows, P / 2, kSeeAll, false>(a.prefix, bx, (int)blockIdx.y);
     }
-    // Shares of the sequences go to the workgroups that have none of a prefix, then around.
-    for (int u = bx - a.prefix_blocks + (bx < a.prefix_blocks ? grid : 0); u < a.own_blocks; u += grid) {
+    for (int u = first_own(bx, a.prefix_blocks, grid); u < a.own_blocks; u += grid) {
         __syncthreads();  // (LDS: what the sums before lie in)
         attend_few_rows<Rows, RT, kSeeCausal, false, kSharedWaves>(a.own, u, (int)blockIdx.y);
     }
@@ -108,99 +106,6 @@ __global__ __launch_bounds__(kAttendThreads) void jq_attend_shared_join_kernel(S
 
 // ---- host ------------------------------------------------------------------------------------------------------------------
 
-constexpr int kSharedChip = 256;  // workgroups that run at a time, one a CU
-
-// How the work is shared out.  Prefixes and sequences are cut into shares, either side by side, on CUs of their own, or, where there is
-// much of both, one behind the other on all of them: what a CU reads in a given time is limited, some 25 GB/s, however many of its
-// waves ask, so a sweep that has few CUs takes long.  Fewer shares leave fewer parts to write and to join; fewer query rows a workgroup
-// (and the prefix read twice, which meets in an XCD's L2) halve them too.  In nanoseconds, as measured on one MI355X.
-constexpr int64_t kSharedStart = 6000, kSharedNext = 3000, kOwnRow = 22, kPartBytes = 4000;  // (the last: bytes a nanosecond, there and back)
-static int64_t prefix_row_time(int tiles) { return tiles <= 8 ? 25 : 36; }
-void plan_shared(const Plan& p, const Plan& pp, const int32_t* cu_members, SharedPlan* sp) {
-    const int own_tiles = (p.rows + kTileRows - 1) / kTileRows;
-    sp->own_tiles = own_tiles <= 1 ? 1 : 2;
-    sp->own_groups = (own_tiles + sp->own_tiles - 1) / sp->own_tiles;
-    const int64_t heads = (int64_t)p.n_layers * p.h_kv;
-    int32_t longest = 0, longest_own = 0, most_rows = 0;
-    int32_t length[JQ_MAX_SEQ], own_length[JQ_MAX_SEQ], rows[JQ_MAX_SEQ];
-    for (int i = 0; i < pp.n_seq; ++i) {
-        length[i] = pp.tab.cu_seq[i + 1] - pp.tab.cu_seq[i];
-        rows[i] = (cu_members[i + 1] - cu_members[i]) * p.rows;
-        longest = std::max(longest, length[i]);
-        most_rows = std::max(most_rows, rows[i]);
-    }
-    for (int s = 0; s < p.n_seq; ++s) {
-        own_length[s] = p.tab.cu_seq[s + 1] - p.tab.cu_seq[s];
-        longest_own = std::max(longest_own, own_length[s]);
-    }
-    auto split = [](int32_t rows, int64_t share) { return (int64_t)(((uint32_t)rows + (uint32_t)share - 1) / (uint32_t)share); };
-    // The smallest share, in multiples of `unit` rows, that makes no more than `most` workgroups, if any does.
-    auto smallest = [](auto blocks, int32_t rows, int64_t unit, int64_t most) {
-        int64_t lo = 1, hi = (rows + unit - 1) / unit;
-        while (lo < hi) {
-            const int64_t mid = (lo + hi) / 2;
-            if (blocks(mid * unit) <= most) hi = mid; else lo = mid + 1;
-        }
-        return lo * unit;
-    };
-    auto own_blocks = [&](int64_t share) {
-        int64_t n = 0;
-        for (int s = 0; s < p.n_seq; ++s) n += split(own_length[s], share);
-        return n * heads * sp->own_groups;
-    };
-    constexpr int kChoices = 4;  // all CUs for both, or three, two, one quarter for the prefixes
-    int64_t own_of[kChoices], own_n[kChoices];
-    for (int c = 0; c < kChoices; ++c) {
-        own_of[c] = smallest(own_blocks, longest_own, 256, c ? c * kSharedChip / kChoices : kSharedChip);
-        own_n[c] = own_blocks(own_of[c]);
-    }
-    const int tiles = (most_rows + kTileRows - 1) / kTileRows, natural = tiles <= 1 ? 1 : tiles <= 2 ? 2 : tiles <= 4 ? 4 : tiles <= 8 ? 8 : 16;
-    int64_t best = INT64_MAX, share = 1, own_share = 1;
-    for (int each = natural; each >= std::max(natural / 2, std::min(natural, 4)); each /= 2) {
-        int64_t groups[JQ_MAX_SEQ];
-        for (int i = 0; i < pp.n_seq; ++i) groups[i] = (rows[i] + each * kTileRows - 1) / (each * kTileRows);
-        auto prefix_blocks = [&](int64_t share) {
-            int64_t n = 0;
-            for (int i = 0; i < pp.n_seq; ++i) n += split(length[i], share) * groups[i];
-            return n * heads;
-        };
-        for (int c = 0; c < kChoices; ++c) {
-            const int64_t size = smallest(prefix_blocks, longest, each <= 2 ? 256 : each == 4 ? 128 : 64, kSharedChip - c * kSharedChip / kChoices);
-            const int64_t n = prefix_blocks(size), m = own_n[c];
-            const int64_t time = std::min(size, (int64_t)longest) * prefix_row_time(each), own_time = std::min(own_of[c], (int64_t)longest_own) * kOwnRow;
-            const int64_t rounds = (n + kSharedChip - 1) / kSharedChip, own_rounds = (m + kSharedChip - 1) / kSharedChip;
-            int64_t cost = n + m <= kSharedChip ? kSharedStart + std::max(time, own_time) : rounds * (kSharedStart + time) + own_rounds * (kSharedNext + own_time);
-            int64_t parts = 0;
-            for (int i = 0; i < pp.n_seq; ++i) parts += split(length[i], size) * rows[i];
-            cost += (parts * heads + m * p.rows) * (2 * kHeadDim * (int64_t)sizeof(float)) / kPartBytes;
-            if (cost < best) { best = cost; share = size; own_share = own_of[c]; sp->prefix_tiles = each; }
-        }
-    }
-    sp->cu_split[0] = sp->cu_part[0] = sp->own_split[0] = 0;
-    int64_t parts = 0, eighths = 0;
-    for (int i = 0; i < pp.n_seq; ++i) {
-        const int64_t ns = split(length[i], share);
-        const int64_t groups = (rows[i] + sp->prefix_tiles * kTileRows - 1) / (sp->prefix_tiles * kTileRows);
-        eighths += (ns * p.h_kv + 7) / 8 * groups;
-        if (i == 0) { sp->first_groups = (int32_t)groups; sp->first_splits = (int32_t)ns; }
-        sp->cu_split[i + 1] = (int32_t)eighths;
-        parts += ns * rows[i];
-        sp->cu_part[i + 1] = (int32_t)parts;
-    }
-    for (int s = 0; s < p.n_seq; ++s) sp->own_split[s + 1] = sp->own_split[s] + (int32_t)split(own_length[s], own_share);
-    sp->fits = parts <= INT32_MAX && eighths <= INT32_MAX / 8;
-    auto up = [](size_t x) { return (x + 255) / 256 * 256; };
-    const size_t pre = (size_t)heads * (size_t)parts, own = (size_t)heads * sp->own_split[p.n_seq] * p.rows;
-    sp->off_prefix_stats = 0;
-    sp->off_prefix_part = up(pre * sizeof(float2));
-    sp->off_own_stats = sp->off_prefix_part + up(pre * kHeadDim * sizeof(float));
-    sp->off_own_part = sp->off_own_stats + up(own * sizeof(float2));
-    sp->ws_bytes = sp->off_own_part + up(own * kHeadDim * sizeof(float));
-    const int64_t blocks = 8 * eighths + shared_blocks(sp->own_split[p.n_seq], p.h_kv, sp->own_groups);
-    const int64_t joins = (int64_t)p.n_seq * p.h_kv * p.rows;
-    sp->fits = sp->fits && blocks * kSharedThreads <= UINT32_MAX && joins * kAttendThreads <= UINT32_MAX;
-}
-
 static void common_args(const Plan& p, AttendArgs* a) {
     a->n_layers = p.n_layers; a->n_seq = p.n_seq; a->h_kv = p.h_kv;
     a->T = p.T;
@@ -246,11 +151,9 @@ hipError_t launch_attend_shared(const Plan& p, const Plan& pp, const SharedPlan&
     for (int i = 0; i <= pp.n_seq; ++i) { a.prefix.cu_split[i] = sp.cu_split[i]; a.prefix.cu_part[i] = sp.cu_part[i]; a.prefix.cu_member[i] = cu_members[i]; }
     for (int s = 0; s <= p.n_seq; ++s) a.own.cu_split[s] = sp.own_split[s];
     a.own.causal = p.window && p.n_q > 1;
-    a.prefix_blocks = 8 * sp.cu_split[pp.n_seq];
-    a.own_blocks = (int32_t)shared_blocks(a.own.n_splits, p.h_kv, sp.own_groups);
-    // more than the CUs take at a time, with layers on top: all in one round of workgroups if the prefixes are
-    const int64_t all = (int64_t)a.prefix_blocks + a.own_blocks, most = std::max<int64_t>(kSharedChip / p.n_layers, 1);
-    const dim3 grid((unsigned)(all <= most || a.prefix_blocks > most ? all : most), (unsigned)p.n_layers);
+    a.prefix_blocks = sp.prefix_blocks;
+    a.own_blocks = sp.own_blocks;
+    const dim3 grid((unsigned)sp.grid, (unsigned)p.n_layers);
     hipError_t e;
     switch (sp.prefix_tiles) {
         case 1: e = launch_shared_sweep<1>(a, sp.own_tiles, grid, st); break;
