@@ -401,8 +401,11 @@ int jq_evict_traced(const jq_shape* shape, const void* Q, const void* K, const v
  * (2^-16 of p is lost), with more than 64 query rows per KV head in one (2^-8; out's own rounding is 2^-8 too).  A
  * value of V that is not finite makes the outputs of its own dimension infinite or NaN, of the queries that see its
  * row; everything else is as if it were finite.  `ws` (DEVICE, 16-byte aligned) must hold jq_attend_workspace_bytes
- * (`with_weights`: 0, or 1 for calls that pass weights; enough for a cache of codes too). shape->budgets is not used. */
+ * (`with_weights`: 0, or 1 for calls that pass weights; enough for a cache of codes too), or, for bf16 caches alone,
+ * jq_attend_uncoded_workspace_bytes: for ragged batches down to a quarter, and all that calls over them look at.
+ * shape->budgets is not used. */
 int jq_attend_workspace_bytes(const jq_shape* shape, int32_t with_weights, size_t* bytes);
+int jq_attend_uncoded_workspace_bytes(const jq_shape* shape, int32_t with_weights, size_t* bytes);
 int jq_attend(const jq_shape* shape, const int32_t* lens, const void* Q, const void* K, const void* V, void* out,
               float* lse, float* weights, void* ws, size_t ws_bytes, void* stream);
 int jq_attend_paged(const jq_shape* shape, const jq_pages* pages, const int32_t* lens, const void* Q, const void* K_pool,
@@ -412,8 +415,8 @@ int jq_attend_paged(const jq_shape* shape, const jq_pages* pages, const int32_t*
  * drafted token j in row lens - n_q + j.  Every token sees all rows before those, and drafted token i sees drafted token j
  * where bit j % 32 of seen[s, i, j / 32] is set (DEVICE uint32 [n_seq, n_q, ceil(n_q / 32)]; its own bit too if it is to
  * see itself; bits from n_q on are ignored).  A sequence that drafted fewer tokens leaves the others' bits clear: rows
- * that a token does not see do not reach its output, whatever they hold.  shape->window must be 0.  Workspace:
- * jq_attend_workspace_bytes with 0. */
+ * that a token does not see do not reach its output, whatever they hold.  shape->window must be 0.  Workspace: as for
+ * jq_attend with 0. */
 #define JQ_MAX_DRAFT 1024
 int jq_attend_tree(const jq_shape* shape, const int32_t* lens, const uint32_t* seen, const void* Q, const void* K,
                    const void* V, void* out, float* lse, void* ws, size_t ws_bytes, void* stream);

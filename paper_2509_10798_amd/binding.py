@@ -23,7 +23,7 @@ JQ_MAX_SEQ = 128
 STATUS = {0: "JQ_OK", -1: "JQ_ERR_NULL", -2: "JQ_ERR_SHAPE", -3: "JQ_ERR_BUDGET", -4: "JQ_ERR_UNSUPPORTED",
           -5: "JQ_ERR_WORKSPACE", -6: "JQ_ERR_ALIAS", -7: "JQ_ERR_LAUNCH"}
 EXPORTS = ("jq_workspace_bytes", "jq_score", "jq_score_lse", "jq_evict_lse", "jq_score_tail", "jq_evict_tail", "jq_pool", "jq_select_topk", "jq_compact", "jq_compact_inplace_workspace_bytes", "jq_compact_inplace", "jq_evict", "jq_evict_inplace_workspace_bytes", "jq_evict_inplace", "jq_evict_stream", "jq_evict_static", "jq_score_paged", "jq_evict_paged", "jq_evict_paged_inplace_workspace_bytes", "jq_evict_paged_inplace", "jq_evict_traced", "jq_hit_rate", "jq_map_mse", "jq_map_mse_fused_workspace_bytes", "jq_map_mse_fused",
-           "jq_attend_workspace_bytes", "jq_attend", "jq_attend_paged", "jq_attend_tree", "jq_attend_tree_paged",
+           "jq_attend_workspace_bytes", "jq_attend_uncoded_workspace_bytes", "jq_attend", "jq_attend_paged", "jq_attend_tree", "jq_attend_tree_paged",
            "jq_evict_weight_workspace_bytes", "jq_evict_weight", "jq_evict_weight_paged", "jq_replace_lightest", "jq_replace_lightest_paged",
            "jq_attend_shared_workspace_bytes", "jq_attend_shared", "jq_attend_shared_paged",
            "jq_quantize", "jq_quantize_paged", "jq_dequantize", "jq_dequantize_paged",
@@ -102,7 +102,7 @@ def lib() -> ctypes.CDLL:
         L.jq_evict_paged_inplace_workspace_bytes.argtypes = [shp, pgp, ctypes.POINTER(sz)]
         L.jq_evict_paged_inplace.argtypes = [shp, pgp, pgp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
         L.jq_evict_traced.argtypes = [shp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp, ctypes.POINTER(vp), ctypes.c_int]
-        L.jq_attend_workspace_bytes.argtypes = [shp, ctypes.c_int32, ctypes.POINTER(sz)]
+        L.jq_attend_workspace_bytes.argtypes = L.jq_attend_uncoded_workspace_bytes.argtypes = [shp, ctypes.c_int32, ctypes.POINTER(sz)]
         L.jq_attend.argtypes = [shp] + [vp] * 8 + [sz, vp]
         L.jq_attend_paged.argtypes = [shp, pgp] + [vp] * 8 + [sz, vp]
         L.jq_attend_tree.argtypes = [shp] + [vp] * 8 + [sz, vp]
@@ -567,15 +567,17 @@ def _workspace(ws, need, device, stream):
     return _tensor("ws", ws, torch.uint8, (ws.numel(),), device), ws.numel(), ws
 
 
-def attend_workspace_bytes(shape: Shape, weights: bool = False) -> int:
+def attend_workspace_bytes(shape: Shape, weights: bool = False, codes: bool = True) -> int:
+    """Bytes of workspace that attend() and its like need; `codes` False: over bf16 caches alone."""
     n = ctypes.c_size_t(0)
-    _check(lib().jq_attend_workspace_bytes(ctypes.byref(shape.c_struct()), int(bool(weights)), ctypes.byref(n)), "jq_attend_workspace_bytes")
+    name = "jq_attend_workspace_bytes" if codes else "jq_attend_uncoded_workspace_bytes"
+    _check(getattr(lib(), name)(ctypes.byref(shape.c_struct()), int(bool(weights)), ctypes.byref(n)), name)
     return int(n.value)
 
 
-def alloc_attend_workspace(shape: Shape, weights: bool = False, device="cuda"):
+def alloc_attend_workspace(shape: Shape, weights: bool = False, device="cuda", codes: bool = True):
     import torch
-    return torch.empty(attend_workspace_bytes(shape, weights), dtype=torch.uint8, device=device)
+    return torch.empty(attend_workspace_bytes(shape, weights, codes), dtype=torch.uint8, device=device)
 
 
 def _attend(name, shape: Shape, pages, seen, Q, K, V, lens, out, lse, want_lse, weights, ws, stream, codes=None):
@@ -599,7 +601,7 @@ def _attend(name, shape: Shape, pages, seen, Q, K, V, lens, out, lse, want_lse, 
         front += (_tensor("seen", seen, i32, (shape.n_seq, shape.n_q, -(-shape.n_q // 32)), dev),)
     else:
         ins += (_tensor("weights", weights, f32, (shape.n_layers, shape.h_kv, shape.T), dev),)
-    sp, n, ws = _workspace(ws, lambda: attend_workspace_bytes(shape, weights is not None), dev, stream)
+    sp, n, ws = _workspace(ws, lambda: attend_workspace_bytes(shape, weights is not None, codes is not None), dev, stream)
     _call(name, shape, pages, dev, stream, *front, *ins, sp, n)
     return out, lse
 

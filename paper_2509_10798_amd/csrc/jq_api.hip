@@ -721,14 +721,22 @@ int attend_plan(const jq_shape* shape, bool weights, Plan* p, AttendPlan* ap, bo
 }
 }  // namespace
 
-int jq_attend_workspace_bytes(const jq_shape* shape, int32_t with_weights, size_t* bytes) {
+int jq_attend_uncoded_workspace_bytes(const jq_shape* shape, int32_t with_weights, size_t* bytes) {
     if (!bytes) return JQ_ERR_NULL;
     Plan p;
     AttendPlan ap;
     const int rc = attend_plan(shape, with_weights != 0, &p, &ap);
     if (rc != JQ_OK) return rc;
     *bytes = ap.ws_bytes;
+    return JQ_OK;
+}
+
+int jq_attend_workspace_bytes(const jq_shape* shape, int32_t with_weights, size_t* bytes) {
+    const int rc = jq_attend_uncoded_workspace_bytes(shape, with_weights, bytes);
+    if (rc != JQ_OK) return rc;
     // over codes the work is shared out in another way; what it would refuse asks for nothing
+    Plan p;
+    AttendPlan ap;
     if (attend_plan(shape, with_weights != 0, &p, &ap, true) == JQ_OK) *bytes = std::max(*bytes, ap.ws_bytes);
     return JQ_OK;
 }
