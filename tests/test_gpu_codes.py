@@ -601,3 +601,47 @@ def test_rows_whose_page_is_not_handed_out(bits, below, beyond):
         np.testing.assert_array_equal(gs, want_s)
         np.testing.assert_array_equal(g, want)
         np.testing.assert_array_equal(f64(from_dev_bf16(out)), want_out)
+
+
+@pytest.mark.parametrize("caps,h,n_q", [([4000, 90, 1500, 700, 2500, 33], 2, 2), ([900], 2, 1), ([40, 300], 4, 1), ([700, 5000, 260], 2, 12)])
+def test_calls_over_either_kind_of_cache_in_turn_on_one_workspace(caps, h, n_q):
+    """Eager and captured, with weights and without: the two kinds lay the workspace out in their own ways, and neither leaves there what
+    misleads the other."""
+    import torch
+    assert torch.cuda.is_available(), "this test needs the GPU"
+    print("in turn", caps, h, n_q, flush=True)
+    rng = np.random.default_rng(80)
+    K, V = (to_dev_bf16(bf16(rng, 1, sum(caps), h, 128)) for _ in range(2))
+    sh = jq.Shape(n_layers=1, seq_lens=caps, n_q=n_q, h_q=4 * h, h_kv=h, pool_k=1, budgets=caps)
+    codes = jq.quantize(sh, K, V, jq.alloc_codes(sh))
+    Q = to_dev_bf16(bf16(rng, 1, len(caps), n_q, 4 * h, 128))
+
+    def call(kind, weigh, ws):
+        w = torch.zeros((1, h, sum(caps)), device="cuda") if weigh else None
+        o = jq.attend(sh, Q, K, V, weights=w, ws=ws) if kind == "rows" else jq.attend_quantized(sh, Q, codes, weights=w, ws=ws)
+        return o if w is None else o + (w,)
+    kinds = [(k, w) for k in ("rows", "codes") for w in (False, True)]
+    want = [call(*x, jq.alloc_attend_workspace(sh, weights=x[1]).fill_(0xFF)) for x in kinds]
+    ws = jq.alloc_attend_workspace(sh, weights=True).fill_(0xFF)
+    torch.cuda.synchronize()
+    same = lambda got, ref: all(torch.equal(a, b) for a, b in zip(got, ref))
+    for _ in range(3):
+        got = [call(*x, ws) for x in kinds]
+        torch.cuda.synchronize()
+        assert all(map(same, got, want))
+    side, graphs = torch.cuda.Stream(), []
+    side.wait_stream(torch.cuda.current_stream())
+    for x in kinds:
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, stream=side):
+            got = call(*x, ws)
+        graphs.append((g, got))
+    torch.cuda.synchronize()
+    for _ in range(4):
+        for (g, got), ref, x in zip(graphs, want, kinds):
+            g.replay()
+            torch.cuda.synchronize()
+            assert same(got, ref), x
+            eager = [call(*y, ws) for y in reversed(kinds)]
+            torch.cuda.synchronize()
+            assert all(map(same, eager, reversed(want))), x

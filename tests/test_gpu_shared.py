@@ -374,3 +374,32 @@ def test_probabilities_are_two_parts_whatever_the_number_of_query_rows(members, 
                 ro, rl, _, to, tl, _ = attend_ref(q[r:r + 64], k, v, see[r:r + 64], 128 ** -0.5)   # (its bounds for up to 64 rows)
                 assert (np.abs(o[r:r + 64] - ro) <= to).all(), "sequence %d: out off by %g of its bound" % (s, (np.abs(o[r:r + 64] - ro) / to).max())
                 assert (np.abs(e[r:r + 64] - rl) <= tl).all(), s
+
+
+def test_the_last_row_of_a_prefix_past_31_bits_of_offset():
+    """Three layers of a prefix of 500 000 rows of 8 heads, 3 GB each of K and V.  The last row's score is ahead of all others together by more than
+    2^24 for every sequence, so that its values are the outputs, to the bit: parts of p (2^-16) and fp32 sums stay far within half a step of bf16."""
+    import torch
+    assert torch.cuda.is_available(), "this test needs the GPU"
+    nl, P, h = 3, 500_003, 8
+    gen = torch.Generator(device="cuda").manual_seed(4)
+    K, V = (torch.empty((nl, P, h, 128), dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    for x in (K, V):
+        for a in range(0, P, 100_000):
+            b = min(P, a + 100_000)
+            x[:, a:b] = torch.randn((nl, b - a, h, 128), generator=gen, device="cuda").to(torch.bfloat16)
+    one = torch.randn((nl, 1, 1, h, 128), generator=gen, device="cuda").to(torch.bfloat16)
+    k, v = (torch.randn((nl, 30, h, 128), generator=gen, device="cuda").to(torch.bfloat16) for _ in range(2))
+    K[:, -1] = 4 * one[:, 0, 0]
+    V[:, -1] = 8 * torch.randn((nl, h, 128), generator=gen, device="cuda").to(torch.bfloat16)
+    sh = jq.Shape(n_layers=nl, seq_lens=[10] * 3, n_q=1, h_q=h, h_kv=h)
+    out, lse = jq.attend_shared(sh, jq.Prefixes([P], [3]), one.expand(nl, 3, 1, h, 128).contiguous(), K, V, k, v)
+    torch.cuda.synchronize()
+    top = 4 * (one[:, :, 0].double() ** 2).sum(-1) / 128 ** 0.5       # [nl, 1, h], some 45
+    for g in range(h):                                                # (what the inputs are meant to be, before what comes of them)
+        for l in range(nl):
+            x = (K[l, :-1, g].float() @ one[l, 0, 0, g].float()).double() / 128 ** 0.5
+            assert float(torch.logsumexp(x, 0)) + 24 * np.log(2) < float(top[l, 0, g])
+    assert torch.equal(out, V[:, -1][:, None, None].expand(nl, 3, 1, h, 128))
+    u = 2.0 ** -24
+    assert ((lse[:, :, 0].double() - top).abs() <= 132 * u * top + 4 * u * (top + 16) + 404 * u * (1 + top)).all()   # (a score, and its log-sum-exp)
