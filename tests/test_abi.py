@@ -238,3 +238,8 @@ def test_knobs_are_read_once_and_again_on_request(monkeypatch):
     monkeypatch.undo()
     jq.reload_knobs()
     assert jq.workspace_bytes(sh) == base
+
+
+def test_status_strings_cover_what_the_header_says_of_codes_and_prefixes():
+    assert "bits of codes" in jq.status_string(-2) and "prefixes" in jq.status_string(-2)
+    assert "2^20 query rows" in jq.status_string(-4) and "fewer bits for keys than for values" in jq.status_string(-4)
