@@ -10,7 +10,7 @@
 // second launch where that is much.  All sums and statistics are fp32.  Measured on one MI355X, whole calls, 8 KV heads of 4 query
 // heads: one token over 131072 rows 97 us (5.5 TB/s; a plain read reaches 6.2), 32 sequences of 2048 rows with weights 55
 // (bound by memory), one token over 1000 rows of 2 heads 11 (bound by the round trips of a join), 25 drafted tokens over eight
-// paged caches of 29909 rows together 41, 64 over 32832 rows 53 (matrix and vector instructions, which take turns).
+// paged caches of 29909 rows together 41, 64 over 32832 rows 53 (both: matrix and vector instructions, and waits in step).
 //
 // Layout.  Both products are v_mfma_f32_16x16x32_bf16, of which lane l holds row (or column) l % 16 and the eight products'
 // terms 8 * (l / 16) .. + 7 of either operand, and of the result column l % 16 and rows 4 * (l / 16) .. + 3.  Scores are
@@ -654,7 +654,7 @@ __device__ __forceinline__ void attend_few_rows(const Args& a, int bx, int layer
                 for (int e = 0; e < 4; ++e) st.o[r][d][e] = marks[r][d][e] == 0.0f ? st.o[r][d][e] : marks[r][d][e];
     }
 
-    // The four waves' sums, in wave order.
+    // The waves' sums, in wave order.
 #pragma unroll
     for (int r = 0; r < RT; ++r) {
         if (lane < 16) lds_stats[(wave * RT + r) * kTileRows + lane] = make_float2(st.m[r], st.z[r]);
@@ -820,9 +820,10 @@ __global__ __launch_bounds__(64 * WAVES, Rows::least_waves(RT)) void jq_attend_k
 // K's rows are read sixteen lanes a row of 256 bytes, piece p of row k at p ^ (k & 15), so that eight lanes' pieces meet in eight
 // different bank groups; V is read transposed (ds_read_b64_tr_b16: a lane receives four keys' values of one dimension out of four
 // rows of sixteen), piece p of row k at p ^ 2 (k & 7) for the same reason (no bank conflicts are counted).
-// What bounds it: with 128 rows a group memory, and the 20 us that two launches of this size cost whatever they do; with 256 the
-// instructions of a tile of 32 keys and 32 rows, 512 cycles of the matrix cores and some 420 of the vector ALU, which add up
-// also across the two waves of a SIMD.  Tried without gain: four stages ahead, two tiles' terms together, more of V's reads early,
+// What bounds it: waits.  By the counters, us at 2.4 GHz, of a wave's life / of matrix instructions / of vector instructions a SIMD, and the
+// share of wave time that waits: 100 rows over eight caches 26 / 6 / 8, 40 %; 128 behind four prompts 40 / 11 / 12, 39 %; 256 over 32832 38 / 14 / 13,
+// 32 %.  With R = 4 and 8 a wave has one tile between two barriers (64 keys a stage), so the two waves of a SIMD go through the same chain in
+// step: deposit, barrier, reads from LDS, first product, terms, second product.  Tried without gain: four stages ahead, two tiles' terms together, more of V's reads early,
 // wave priorities, half of the waves held back behind each barrier.
 template <int R>
 struct Wide {
@@ -833,7 +834,8 @@ struct Wide {
     static constexpr int kAhead = KW == 4 ? 1 : 2;             // stages requested ahead: 64 KB
     // Probabilities in one bf16 part, off by 2^-8 of each at most, or in two, 2^-16, for which the second product doubles.  With one, out is
     // off by 1.4 times its own rounding (2-norm against 64 bits 0.0023, 0.0017 with two).  Us a call with one / two: 64 rows over 32832
-    // 39.3 / 40.4, 128 behind four prompts 58.8 / 65.2, 100 over eight caches 41.5 / 45.3, 256 over 32832 56 / 68: two while they cost 3 percent.
+    // 39.3 / 40.4, 128 behind four prompts 58.8 / 65.2, 100 over eight caches 41.5 / 45.3, 256 over 32832 56 / 68: two while they cost 3 percent, and
+    // over shared prefixes always (kExact below says why; 32 sequences behind 32768 rows 59 / 63).
     static constexpr bool kExact = R == 2;
     static constexpr int kEarly = 2;                           // blocks of V requested ahead of their use
     static constexpr int kRequests = kKeys / 2 / kWaves;       // of 1 KB, a wave and stage

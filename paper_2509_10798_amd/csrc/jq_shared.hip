@@ -5,8 +5,8 @@
 // A prefix is swept once for all the sequences that continue it: their query rows, which each would have brought alone, meet its keys
 // together, as many query rows of one sequence do in jq_attend (jq_attend.h has both sweeps).  The sequences' own rows are swept in the
 // same launch, by other workgroups or behind the prefixes, and a second launch joins the parts (m, z, unnormalised out) of both.
-// Measured on one MI355X, whole calls, 8 KV heads of 4 query heads: 8 sequences of 40 rows behind 2048 rows 15.4 us (two launches, 11.9
-// and 4), 32 of 700 behind 32768 58 (the sweeps 52, one behind the other; 17 MB of parts; the join 7.7), 16 of 500 behind 131072 119 (memory: 4.7
+// Measured on one MI355X, whole calls, 8 KV heads of 4 query heads: 8 sequences of 40 rows behind 2048 rows 15.3 us (two launches, 12
+// and 4), 32 of 700 behind 32768 62 (the sweeps 57, one behind the other; 17 MB of parts; the join 7.7), 16 of 500 behind 131072 119 (memory: 4.7
 // TB/s over the sweeps).
 #include <algorithm>
 
