@@ -307,8 +307,9 @@ struct Rows16 {
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
             const uint32_t at = row0 + (uint32_t)min(16 * i + (lane & 15), last);
+            const char* k = K + (at * stride + kb);  // (the rest in the instructions)
 #pragma unroll
-            for (int c = 0; c < 4; ++c) t.k[i][c] = *(const au32x4*)(K + (at * stride + kb + 64u * c));
+            for (int c = 0; c < 4; ++c) t.k[i][c] = *(const au32x4*)(k + 64 * c);
         }
 #pragma unroll
         for (int i = 0; i < 2; ++i)
