@@ -125,14 +125,16 @@ __device__ __forceinline__ int seq_of_split(const AttendArgs& a, int split, int 
 // Groups of query rows over the same keys lie eight workgroups apart, so that they meet in one XCD's L2.
 struct KeyShare {
     int s, split, ns, mine, g, rg;  // sequence, share among all, shares of the sequence, share among these, KV head, group
-    bool none;
 };
+// (Apart from the share itself: one found behind a branch is waited for field by field, in front of the first request.)
+__device__ __forceinline__ bool has_share(const AttendArgs& a, int bx) { return bx / (8 * a.row_groups) * 8 + (bx & 7) < a.units; }
+__device__ __forceinline__ bool has_share(const PrefixArgs&, int) { return true; }
+__device__ __forceinline__ bool has_share(const OwnArgs&, int) { return true; }
 __device__ __forceinline__ KeyShare key_share_of(const AttendArgs& a, int bx, int, int lane) {
     const int per = 8 * a.row_groups;
     const int u = bx / per * 8 + (bx & 7), rg = (bx % per) >> 3;
-    if (u >= a.units) return KeyShare{0, 0, 0, 0, 0, 0, true};
     const int split = u / a.h_kv, g = u - split * a.h_kv, s = seq_of_split(a, split, lane);
-    return KeyShare{s, split, a.cu_split[s + 1] - a.cu_split[s], split - a.cu_split[s], g, rg, false};
+    return KeyShare{s, split, a.cu_split[s + 1] - a.cu_split[s], split - a.cu_split[s], g, rg};
 }
 // Prefixes have as many groups as their own rows ask for (`rows` each): with as many as the largest, workgroups that had nothing to do
 // stood between the others, and some CUs were left two of these (three prefixes with 192, 80 and 16 query rows 92 us for 64).
@@ -146,12 +148,12 @@ __device__ __forceinline__ KeyShare key_share_of(const PrefixArgs& a, int bx, in
     }
     const UnitAt at = unit_at(bx - a.cu_split[s], ns * a.h_kv, groups);
     const int mine = at.unit / a.h_kv;
-    return KeyShare{s, 0, ns, mine, at.unit - mine * a.h_kv, at.group, false};
+    return KeyShare{s, 0, ns, mine, at.unit - mine * a.h_kv, at.group};
 }
 __device__ __forceinline__ KeyShare key_share_of(const OwnArgs& a, int bx, int, int lane) {
     const UnitAt at = unit_at(bx, a.units, a.row_groups);
     const int split = at.unit / a.h_kv, s = seq_of_split(a, split, lane);
-    return KeyShare{s, split, a.cu_split[s + 1] - a.cu_split[s], split - a.cu_split[s], at.unit - split * a.h_kv, at.group, false};
+    return KeyShare{s, split, a.cu_split[s + 1] - a.cu_split[s], split - a.cu_split[s], at.unit - split * a.h_kv, at.group};
 }
 
 // log2 of a sum: v_log_f32 rounds towards zero and is off by more the larger its result, so it only sees the mantissa.
@@ -554,8 +556,8 @@ __device__ __forceinline__ void attend_few_rows(const Args& a, int bx, int layer
     static_assert(!(KEEP && kParts), "weights are those of one sweep");
     float2* lds_stats = (float2*)(lds + WAVES * RT * kTileRows * kOutStride);
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+    if (!has_share(a, bx)) return;
     const KeyShare share = key_share_of(a, bx, RT * kTileRows, lane);
-    if (share.none) return;
     const int split = share.split, g = share.g, s = share.s, rg = share.rg, ns = share.ns, mine = share.mine;
     const int row0 = rg * RT * kTileRows;
 
@@ -859,8 +861,8 @@ __device__ __forceinline__ void attend_many_rows(const Args& a, int bx, int laye
     uint8_t* marked = (uint8_t*)wide_lds + W::kFlags;  // [kWaves]: the wave has cleared values of V, or has sums that are not finite
     bool was_cleared = false;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+    if (!has_share(a, bx)) return;
     const KeyShare share = key_share_of(a, bx, W::kRows, lane);
-    if (share.none) return;
     const int split = share.split, g = share.g, s = share.s, rg = share.rg, ns = share.ns, mine = share.mine;
     const int cap = a.cu_seq[s + 1] - a.cu_seq[s];
     const int rw = wave % R, kw = wave / R;
