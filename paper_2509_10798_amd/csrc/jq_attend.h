@@ -473,8 +473,15 @@ __device__ __forceinline__ void tile_step(RowState<RT>& st, Tile& t, const Atten
     add_values(std::integral_constant<int, 3>{});
 }
 
+// Where outputs go.  What a kernel needs of its arguments while it stores is copied first: through the reference the compiler has to
+// take every store for one to them, and loads them again behind it.
+struct OutArgs {
+    uint16_t* out; float* lse;
+    int32_t n_seq, n_q, h_q, group;
+    __device__ __forceinline__ OutArgs(const AttendArgs& a) : out(a.out), lse(a.lse), n_seq(a.n_seq), n_q(a.n_q), h_q(a.h_q), group(a.group) {}
+};
 // Four dimensions of a query row's output out of its sums; a row that has seen nothing: zeros, and -inf for its log-sum-exp.
-__device__ __forceinline__ void store_out(const AttendArgs& a, int layer, int s, int g, int row, int d, f32x4 o, float m, float z) {
+__device__ __forceinline__ void store_out(const OutArgs& a, int layer, int s, int g, int row, int d, f32x4 o, float m, float z) {
     const int i = row / a.group, h = g * a.group + row - i * a.group;
     const int64_t q_row = (((int64_t)layer * a.n_seq + s) * a.n_q + i) * a.h_q + h;
     const float inv = z == 0.0f ? 0.0f : 1.0f / z;
@@ -683,6 +690,12 @@ __device__ __forceinline__ void attend_few_rows(const Args& a, int bx, int layer
     __syncthreads();
     const int64_t part_row = part_at(a, layer, s, split, mine, g);
     const int rows_here = min(query_rows(a, s) - row0, RT * kTileRows);
+    const OutArgs outs(a);
+    float* const parts_to = a.part + part_row * kHeadDim;
+    float2* const stats_to = a.stats + part_row;
+    float* const logits_to = KEEP ? a.logits + ((int64_t)layer * a.h_kv + g) * a.rows * a.logit_T + logit_at(a.cu_seq, s) : nullptr;
+    const int64_t logit_T = a.logit_T;
+    const int rows_all = a.rows, hold_keys = a.hold_keys;
     for (int item = threadIdx.x; item < rows_here * 32; item += kThreads) {
         const int r = item >> 5, d = (item & 31) * 4, row = row0 + r;
         float m = -__builtin_inff(), z = 0.0f;
@@ -696,18 +709,18 @@ __device__ __forceinline__ void attend_few_rows(const Args& a, int bx, int layer
             o += *(const f32x4*)(lds + (w * RT * kTileRows + r) * kOutStride + d);
         }
         if (ns == 1 && !kParts) {
-            store_out(a, layer, s, g, row, d, o, m, z);
+            store_out(outs, layer, s, g, row, d, o, m, z);
         } else {
-            float* to = a.part + (part_row + row) * kHeadDim + d;
+            float* to = parts_to + row * kHeadDim + d;
             put_pair(to, o[0], o[1]);
             put_pair(to + 2, o[2], o[3]);
         }
-        if (d == 0 && (ns > 1 || KEEP || kParts)) put_pair((float*)(a.stats + part_row + row), m, z);
+        if (d == 0 && (ns > 1 || KEEP || kParts)) put_pair((float*)(stats_to + row), m, z);
     }
     if (KEEP && ns == 1) {  // all of the sequence is here
         float* lse2 = lds;  // (the sums above have been read by the threads that wait here)
         __syncthreads();
-        if ((int)threadIdx.x < a.rows) {
+        if ((int)threadIdx.x < rows_all) {
             float m = -__builtin_inff(), z = 0.0f;
 #pragma unroll
             for (int w = 0; w < WAVES; ++w) m = fmaxf(m, lds_stats[w * RT * kTileRows + threadIdx.x].x);
@@ -722,18 +735,18 @@ __device__ __forceinline__ void attend_few_rows(const Args& a, int bx, int layer
         float* w = a.weights + ((int64_t)layer * a.h_kv + g) * a.T + a.cu_seq[s];
         for (int j = threadIdx.x; j < n; j += kThreads) {  // (one workgroup: row j of the cache is held at j)
             float sum = 0.0f;
-            for (int r = 0; r < a.rows; ++r) sum += __builtin_amdgcn_exp2f(held[r * a.hold_keys + j] - lse2[r]);
+            for (int r = 0; r < rows_all; ++r) sum += __builtin_amdgcn_exp2f(held[r * hold_keys + j] - lse2[r]);
             w[j] += sum;
         }
         return;
     }
     if (KEEP) {  // the whole share's logits at once, to where the workgroup that weighs finds them
-        const int64_t to = ((int64_t)layer * a.h_kv + g) * a.rows * a.logit_T + logit_at(a.cu_seq, s);
-        const int pairs = a.hold_keys / 2;
-        for (int item = threadIdx.x; item < a.rows * pairs; item += kThreads) {
-            const int r = item / pairs, j = (item - r * pairs) * 2, tile = j >> 5;
-            const int at = (tile / WAVES * ns + mine) * 32 * WAVES + 32 * (tile % WAVES) + (j & 31);
-            if (at < ((n + 31) & ~31)) put_pair(a.logits + to + r * a.logit_T + at, held[r * a.hold_keys + j], held[r * a.hold_keys + j + 1]);
+        const int pairs = hold_keys / 2;
+        for (int item = threadIdx.x; item < rows_all * pairs; item += kThreads) {
+            const int r = item / pairs, j = (item - r * pairs) * 2;
+            const uint32_t tile = (uint32_t)j >> 5;
+            const int at = (int)(tile / WAVES * ns + mine) * 32 * WAVES + 32 * (int)(tile % WAVES) + (j & 31);
+            if (at < ((n + 31) & ~31)) put_pair(logits_to + r * logit_T + at, held[r * hold_keys + j], held[r * hold_keys + j + 1]);
         }
     }
     if (RT > 1 || kParts || !a.tag || ns == 1) return;
@@ -807,7 +820,7 @@ __device__ __forceinline__ void attend_few_rows(const Args& a, int bx, int layer
         if (part == 0)
             for (int k = 1; k < parts; ++k) o += *(const f32x4*)(sums + 4 * (k * items + item));
     }
-    if (part == 0) store_out(a, layer, s, g, row0 + r, d, o, lds_stats[r].x, lds_stats[r].y);
+    if (part == 0) store_out(outs, layer, s, g, row0 + r, d, o, lds_stats[r].x, lds_stats[r].y);
     if (KEEP) weigher.add(lse2, true);
 }
 
@@ -1096,6 +1109,7 @@ __device__ __forceinline__ void attend_many_rows(const Args& a, int bx, int laye
                 for (int e = 0; e < 4; ++e) o[r][d][e] = marks[r][d][e] == 0.0f ? o[r][d][e] : marks[r][d][e];
     }
     const int64_t part_row = part_at(a, layer, s, split, mine, g);
+    const OutArgs outs(a);
     if (KW > 1) {  // the waves over other keys of the same rows
         float* sums = (float*)wide_lds;                                         // [kWaves - R][32][kOutStride]
         float2* stats = (float2*)(sums + (W::kWaves - R) * 32 * kOutStride);    // [kWaves - R][32]
@@ -1139,7 +1153,7 @@ __device__ __forceinline__ void attend_many_rows(const Args& a, int bx, int laye
 #pragma unroll
         for (int d = 0; d < 8; ++d) {
             const int at = 16 * d + 4 * (lane >> 4);
-            if (ns == 1 && !kParts) store_out(a, layer, s, g, row, at, o[r][d], m[r], z[r]);
+            if (ns == 1 && !kParts) store_out(outs, layer, s, g, row, at, o[r][d], m[r], z[r]);
             else *(f32x4*)(a.part + (part_row + row) * kHeadDim + at) = o[r][d];
         }
     }
